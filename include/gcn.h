@@ -395,6 +395,104 @@ gcn_status gcn_loss(int64_t n, int64_t C, int64_t ld, int32_t prec, const void* 
                     int32_t* n_correct, int32_t* overflow, void* workspace, size_t workspace_bytes,
                     void* stream);
 
+/* ===========================================================================
+ * Teacher and student, drawn labels: the operators on rows of class scores
+ * (logits, n x C, ld, prec) beside gcn_loss, for semi-supervised training of
+ * the vertex classification of Section "Experimental Setup" (few labelled
+ * vertices, scores for all of them): a trained model's largest scores are kept
+ * as the teacher (gcn_top_logits), a student learns from them (gcn_distill),
+ * and labels of unlabelled vertices are drawn from a model's own distribution
+ * (gcn_sample_labels) for use as labels of gcn_loss.
+ *
+ * The order of a row's classes is by falling score, the lower class first
+ * among equal scores (-0 equals +0).  A score of -infinity takes a class out
+ * of the row; the lowest finite number is a score like any other.  C is at
+ * most 2^30 and n at most 2^31 - 1 (GCN_ERR_UNSUPPORTED above).  Results do
+ * not depend on the timing of the run.
+ * ======================================================================== */
+
+/* Most entries a row of a teacher's top scores has. */
+#define GCN_MAX_TOP 256
+/* Range of a temperature. */
+#define GCN_MIN_TEMPERATURE 0.0009765625f
+#define GCN_MAX_TEMPERATURE 1024.0f
+
+/* gcn_top_logits: the first K classes of every row in the order above.
+ *   top_classes[i * ld_top + j] = class, top_values[i * ld_top + j] = score
+ *                                 (prec; both n x K, ld_top)
+ * A row of fewer than K classes (C < K, scores of -infinity) ends in entries
+ * with class -1 and score -infinity.  A NaN is no score: its class is left
+ * out and *overflow is set to 1, as it is by a score of +infinity (which is
+ * listed).  Columns [K, ld_top) are not written.  1 <= K <= GCN_MAX_TOP
+ * (GCN_ERR_UNSUPPORTED above).  workspace: at least
+ * gcn_top_logits_workspace_size() bytes.  Asynchronous. */
+gcn_status gcn_top_logits_workspace_size(int64_t n, int64_t C, int64_t K, int32_t prec, size_t* bytes);
+gcn_status gcn_top_logits(int64_t n, int64_t C, int64_t ld, int32_t prec, const void* logits, int64_t K,
+                          int64_t ld_top, void* top_values, int32_t* top_classes, int32_t* overflow,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* gcn_distill: loss and gradient of a student (logits) against a teacher's
+ * top scores (top_values in top_prec and top_classes, n x K, ld_top, as
+ * gcn_top_logits writes them) at temperature T.  Entries of class -1 (any
+ * negative class) or of score -infinity are absent; the others may come in
+ * any order, and a class may occur twice (its weights add).  With
+ *   q_i = softmax over the present entries of top_values[i] / T,
+ *   p_i = softmax over the C classes of logits[i] / T:
+ *   *loss   = weight T^2 / n_mask * sum over counted rows of
+ *             sum_j q_ij (ln q_ij - ln p_i[class of j])      (fp32, unscaled)
+ *   dlogits = S weight T / n_mask * (p_i - q_i at its classes) on counted
+ *             rows, 0 on the others, plus dlogits_base if not NULL, rounded
+ *             once; S is *loss_scale (device float; NULL means 1)
+ *   dlogits_colsum = column sums of that gradient before it is rounded (fp32
+ *             [ld], entries [C, ld) set to 0; may be NULL): the output layer's
+ *             bias gradient (see gcn_loss).  Only with dlogits, and for rows
+ *             of at most 256 (GCN_F32) or 512 (16-bit) classes, the widths of
+ *             gcn_loss (GCN_ERR_UNSUPPORTED above: gcn_layer_bwd's dbias is
+ *             then the way)
+ * A row is counted if mask selects it (uint8, NULL = every row; n_mask = its
+ * nonzero entries, > 0, as in gcn_loss) and it has an entry that is present.
+ * dlogits_base (n x C, ld, prec) may be dlogits itself: gcn_loss followed by
+ * this call on the same buffer gives the gradient of both losses together.
+ * dlogits may be NULL (the loss alone; dlogits_base and dlogits_colsum must
+ * then be NULL).  A class >= C is left out and sets *overflow, as does a
+ * loss, gradient or column sum that is not finite.  T in
+ * [GCN_MIN_TEMPERATURE, GCN_MAX_TEMPERATURE], weight positive and finite.
+ * The loss and the column sums are reduced in a fixed order.  workspace: at
+ * least gcn_distill_workspace_size() bytes.  Asynchronous. */
+gcn_status gcn_distill_workspace_size(int64_t n, int64_t C, int64_t K, int32_t prec, size_t* bytes);
+gcn_status gcn_distill(int64_t n, int64_t C, int64_t ld, int32_t prec, const void* logits, int64_t K,
+                       int64_t ld_top, int32_t top_prec, const void* top_values, const int32_t* top_classes,
+                       const uint8_t* mask, int64_t n_mask, float temperature, float weight,
+                       const float* loss_scale, const void* dlogits_base, float* loss, void* dlogits,
+                       float* dlogits_colsum, int32_t* overflow, void* workspace, size_t workspace_bytes,
+                       void* stream);
+
+/* gcn_sample_labels: one class drawn from every selected row (mask uint8, NULL
+ * = every row), at temperature T, from the uniform numbers u (fp32 [n], in
+ * [0, 1)).  With weights w_c = exp((z_c - max z) / T), each filter keeps the
+ * beginning of the row's order:
+ *   top_k:  its first top_k classes (0: all of them);
+ *   top_p:  of those, the fewest whose weights sum to at least top_p times
+ *           the weights of those (1: all of them);
+ *   min_p:  the classes with w_c >= min_p (0: all of them),
+ * and a class is kept if every filter keeps it (the first one always is).
+ *   labels[i] = the first kept class, in order of class number, at which the
+ *               running sum of the kept weights exceeds u[i] times their sum
+ *   prob[i]   = its weight over that sum (fp32 [n]; may be NULL)
+ * The label is that of the definition in 64-bit arithmetic, whatever prec is.
+ * T = 0 takes the first class of the order (u is then not read; prob = 1).
+ * A row without classes (every score -infinity) gives label -1 and prob 0;
+ * so does a row that holds NaN or +infinity, or whose u lies outside [0, 1),
+ * and sets *overflow to 1.  Rows that mask does not select keep their labels
+ * and prob.  T otherwise in [GCN_MIN_TEMPERATURE, GCN_MAX_TEMPERATURE],
+ * top_k >= 0, top_p in (0, 1], min_p in [0, 1].  workspace: at least
+ * gcn_sample_labels_workspace_size() bytes.  Asynchronous. */
+gcn_status gcn_sample_labels_workspace_size(int64_t n, int64_t C, int32_t prec, size_t* bytes);
+gcn_status gcn_sample_labels(int64_t n, int64_t C, int64_t ld, int32_t prec, const void* logits,
+                             const uint8_t* mask, const float* u, float temperature, int64_t top_k,
+                             float top_p, float min_p, int32_t* labels, float* prob, int32_t* overflow,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---------------------------------------------------------------------------
  * gcn_optimizer_step: one step of Adam on fp32 master weights with dynamic
  * loss scaling (Section "Background and Motivation", levels O1/O2), on

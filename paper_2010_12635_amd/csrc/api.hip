@@ -685,6 +685,140 @@ gcn_status gcn_loss(int64_t n, int64_t C, int64_t ld, int32_t prec, const void* 
   return finish(hipSuccess, s);
 }
 
+// ---------------------------------------------------------------------------
+// Teacher and student, drawn labels: operators on rows of class scores.
+
+namespace {
+
+// Class ids are int32, and the kernels step past the end of a row by less
+// than 2^30.
+constexpr int64_t MAX_CLASSES = 1 << 30;
+// Rows of more classes than a lane group holds take a workgroup each.
+constexpr int64_t MAX_ROWS = INT32_MAX;
+
+gcn_status check_rows(int64_t n, int64_t C, int64_t ld, int32_t prec) {
+  if (!valid_prec(prec)) return GCN_ERR_INVALID_ARG;
+  if (n <= 0 || C <= 0 || ld < C) return GCN_ERR_SHAPE;
+  if (ld % 8) return GCN_ERR_ALIGNMENT;
+  if (C > MAX_CLASSES || n > MAX_ROWS) return GCN_ERR_UNSUPPORTED;
+  return GCN_OK;
+}
+
+gcn_status check_top(int64_t K, int64_t ld_top) {
+  if (K <= 0 || ld_top < K) return GCN_ERR_SHAPE;
+  if (ld_top % 8) return GCN_ERR_ALIGNMENT;
+  if (K > GCN_MAX_TOP) return GCN_ERR_UNSUPPORTED;
+  return GCN_OK;
+}
+
+bool positive_finite(float x) { return x > 0.f && x <= 3.402823466e38f; }
+
+}  // namespace
+
+gcn_status gcn_top_logits_workspace_size(int64_t n, int64_t C, int64_t K, int32_t prec, size_t* bytes) {
+  if (!bytes) return GCN_ERR_INVALID_ARG;
+  gcn_status st = check_rows(n, C, (C + 7) / 8 * 8, prec);
+  if (st == GCN_OK) st = check_top(K, (K + 7) / 8 * 8);
+  if (st != GCN_OK) return st;
+  *bytes = top_workspace_bytes(prec, n, C, K);
+  return GCN_OK;
+}
+
+gcn_status gcn_top_logits(int64_t n, int64_t C, int64_t ld, int32_t prec, const void* logits, int64_t K,
+                          int64_t ld_top, void* top_values, int32_t* top_classes, int32_t* overflow, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  gcn_status st = check_rows(n, C, ld, prec);
+  if (st == GCN_OK) st = check_top(K, ld_top);
+  if (st != GCN_OK) return st;
+  if (!logits || !top_values || !top_classes) return GCN_ERR_INVALID_ARG;
+  if (!aligned16(logits) || !aligned16(top_values) || !aligned16(top_classes)) return GCN_ERR_ALIGNMENT;
+  if (!workspace || workspace_bytes < top_workspace_bytes(prec, n, C, K)) return GCN_ERR_WORKSPACE;
+  if (!aligned16(workspace)) return GCN_ERR_ALIGNMENT;
+  TopParams p;
+  p.n = n; p.C = C; p.ld = ld; p.K = K; p.ld_top = ld_top;
+  p.logits = logits; p.values = top_values; p.classes = top_classes; p.flag = overflow;
+  GCN_HIP(top_launch(prec, p, workspace, s));
+  return finish(hipSuccess, s);
+}
+
+gcn_status gcn_distill_workspace_size(int64_t n, int64_t C, int64_t K, int32_t prec, size_t* bytes) {
+  if (!bytes) return GCN_ERR_INVALID_ARG;
+  gcn_status st = check_rows(n, C, (C + 7) / 8 * 8, prec);
+  if (st == GCN_OK) st = check_top(K, (K + 7) / 8 * 8);
+  if (st != GCN_OK) return st;
+  *bytes = distill_workspace_bytes(prec, n, C, K);
+  return GCN_OK;
+}
+
+gcn_status gcn_distill(int64_t n, int64_t C, int64_t ld, int32_t prec, const void* logits, int64_t K, int64_t ld_top,
+                       int32_t top_prec, const void* top_values, const int32_t* top_classes, const uint8_t* mask,
+                       int64_t n_mask, float temperature, float weight, const float* loss_scale,
+                       const void* dlogits_base, float* loss, void* dlogits, float* dlogits_colsum, int32_t* overflow,
+                       void* workspace, size_t workspace_bytes, void* stream) {
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  gcn_status st = check_rows(n, C, ld, prec);
+  if (st == GCN_OK) st = check_top(K, ld_top);
+  if (st != GCN_OK) return st;
+  if (!valid_prec(top_prec)) return GCN_ERR_INVALID_ARG;
+  if (n_mask <= 0 || n_mask > n) return GCN_ERR_SHAPE;
+  if (!(temperature >= GCN_MIN_TEMPERATURE && temperature <= GCN_MAX_TEMPERATURE) || !positive_finite(weight))
+    return GCN_ERR_INVALID_ARG;
+  if (!logits || !top_values || !top_classes || !loss) return GCN_ERR_INVALID_ARG;
+  if (!dlogits && (dlogits_base || dlogits_colsum)) return GCN_ERR_INVALID_ARG;
+  if (dlogits_colsum && !distill_colsum_supported(prec, C)) return GCN_ERR_UNSUPPORTED;
+  if (!aligned16(logits) || !aligned16(top_values) || !aligned16(top_classes) || !aligned16(dlogits_base) ||
+      !aligned16(dlogits) || !aligned16(dlogits_colsum))
+    return GCN_ERR_ALIGNMENT;
+  if (!workspace || workspace_bytes < distill_workspace_bytes(prec, n, C, K)) return GCN_ERR_WORKSPACE;
+  if (!aligned16(workspace)) return GCN_ERR_ALIGNMENT;
+  DistillParams p;
+  p.n = n; p.C = C; p.ld = ld; p.K = K; p.ld_top = ld_top;
+  p.logits = logits; p.top_prec = top_prec; p.top_values = top_values; p.top_classes = top_classes;
+  p.mask = mask;
+  const double T = temperature;
+  p.inv_T = (float)(1.0 / T);
+  p.scale = (float)(weight * T / (double)n_mask);
+  p.loss_factor = (float)(weight * T * T / (double)n_mask);
+  p.loss_scale = loss_scale; p.base = dlogits_base; p.dlogits = dlogits;
+  p.flag = overflow;
+  GCN_HIP(distill_launch(prec, p, loss, dlogits_colsum, workspace, s));
+  return finish(hipSuccess, s);
+}
+
+gcn_status gcn_sample_labels_workspace_size(int64_t n, int64_t C, int32_t prec, size_t* bytes) {
+  if (!bytes) return GCN_ERR_INVALID_ARG;
+  const gcn_status st = check_rows(n, C, (C + 7) / 8 * 8, prec);
+  if (st != GCN_OK) return st;
+  *bytes = sample_workspace_bytes(prec, n, C);
+  return GCN_OK;
+}
+
+gcn_status gcn_sample_labels(int64_t n, int64_t C, int64_t ld, int32_t prec, const void* logits, const uint8_t* mask,
+                             const float* u, float temperature, int64_t top_k, float top_p, float min_p,
+                             int32_t* labels, float* prob, int32_t* overflow, void* workspace, size_t workspace_bytes,
+                             void* stream) {
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const gcn_status st = check_rows(n, C, ld, prec);
+  if (st != GCN_OK) return st;
+  if (!(temperature == 0.f || (temperature >= GCN_MIN_TEMPERATURE && temperature <= GCN_MAX_TEMPERATURE)) ||
+      top_k < 0 || !(top_p > 0.f && top_p <= 1.f) || !(min_p >= 0.f && min_p <= 1.f))
+    return GCN_ERR_INVALID_ARG;
+  if (!logits || !u || !labels) return GCN_ERR_INVALID_ARG;
+  if (!aligned16(logits) || !aligned16(u) || !aligned16(labels) || !aligned16(prob)) return GCN_ERR_ALIGNMENT;
+  if (!workspace || workspace_bytes < sample_workspace_bytes(prec, n, C)) return GCN_ERR_WORKSPACE;
+  if (!aligned16(workspace)) return GCN_ERR_ALIGNMENT;
+  SampleParams p;
+  p.n = n; p.C = C; p.ld = ld; p.logits = logits; p.mask = mask; p.u = u;
+  p.T = temperature;
+  p.top_k = top_k == 0 || top_k > C ? C : top_k;
+  p.top_p = top_p;
+  p.ln_min_p = std::log((double)min_p);                  // min_p = 0: -inf, no limit
+  p.labels = labels; p.prob = prob; p.flag = overflow;
+  GCN_HIP(sample_launch(prec, p, workspace, s));
+  return finish(hipSuccess, s);
+}
+
 gcn_status gcn_optimizer_step(int64_t count, float* master, const float* grad, float* m, float* v, void* working,
                               int32_t prec, const gcn_adam_config* cfg, gcn_scaler* state, int32_t* overflow_flag,
                               void* stream) {

@@ -172,6 +172,57 @@ hipError_t loss_launch(int prec, int64_t n, int64_t C, int64_t ld, const void* l
                        const float* loss_scale, float* loss, void* dlogits, float* dlogits_colsum,
                        int32_t* n_correct, int32_t* flag, void* ws, hipStream_t s);
 
+// ------------------------------------------ teacher and student, labels ----
+// The definitions are in gcn.h (gcn_top_logits, gcn_distill,
+// gcn_sample_labels).
+struct TopParams {
+  int64_t n, C, ld, K, ld_top;
+  const void* logits;
+  void* values;
+  int32_t* classes;
+  int32_t* flag;
+};
+size_t top_workspace_bytes(int prec, int64_t n, int64_t C, int64_t K);
+hipError_t top_launch(int prec, const TopParams& p, void* ws, hipStream_t s);
+
+struct DistillParams {
+  int64_t n, C, ld, K, ld_top;
+  const void* logits;
+  int top_prec;
+  const void* top_values;
+  const int32_t* top_classes;
+  const uint8_t* mask;
+  float inv_T;
+  float scale;          // weight T / n_mask, of the gradient
+  float loss_factor;    // weight T^2 / n_mask, of the loss
+  const float* loss_scale;
+  const void* base;     // gradient added to, or NULL
+  void* dlogits;        // or NULL
+  float* part_loss;     // set by distill_launch: loss partials,
+  float* part_cs;       // column-sum partials of the workgroups, or NULL,
+  int64_t ldcs;         // and their row stride
+  int32_t* flag;
+};
+bool distill_colsum_supported(int prec, int64_t C);
+size_t distill_workspace_bytes(int prec, int64_t n, int64_t C, int64_t K);
+hipError_t distill_launch(int prec, DistillParams p, float* loss, float* colsum, void* ws, hipStream_t s);
+
+struct SampleParams {
+  int64_t n, C, ld;
+  const void* logits;
+  const uint8_t* mask;
+  const float* u;
+  double T;             // 0: the largest score
+  int64_t top_k;        // C: no limit
+  double top_p;         // 1: no limit
+  double ln_min_p;      // -inf: no limit
+  int32_t* labels;
+  float* prob;
+  int32_t* flag;
+};
+size_t sample_workspace_bytes(int prec, int64_t n, int64_t C);
+hipError_t sample_launch(int prec, const SampleParams& p, void* ws, hipStream_t s);
+
 // ------------------------------------------------------------ optimiser ----
 struct AdamHyper {
   float lr, beta1, beta2, eps, backoff, growth, min_scale, max_scale;

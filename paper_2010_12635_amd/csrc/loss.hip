@@ -7,6 +7,7 @@
 // inside the group.  Per-row losses are summed per workgroup in row order
 // and the workgroup sums in a second fixed-order pass (deterministic).
 #include "internal.h"
+#include "lanes.h"
 
 namespace gcn {
 
@@ -27,80 +28,11 @@ struct LossParams {
   int32_t* flag;
 };
 
-// Reductions over a lane group of LPR lanes (aligned, a power of two),
-// every lane ending with the result: lanes exchange values through DPP
-// moves inside rows of 16 lanes (quad permutations, then the half-row and
-// row mirrors, each pairing a lane with one of the other half once the
-// halves agree), across rows through lane shuffles.
-template <int CTRL>
-__device__ __forceinline__ float dpp_f(float v) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
-}
-template <int CTRL>
-__device__ __forceinline__ int dpp_i(int v) {
-  return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xF, 0xF, true);
-}
-constexpr int DPP_XOR1 = 0xB1;         // quad_perm [1, 0, 3, 2]
-constexpr int DPP_XOR2 = 0x4E;         // quad_perm [2, 3, 0, 1]
-constexpr int DPP_HALF_MIRROR = 0x141; // lane i <-> 7 - i of each 8
-constexpr int DPP_MIRROR = 0x140;      // lane i <-> 15 - i of each 16
-
-template <int LPR>
-__device__ __forceinline__ float group_sum(float v) {
-  if (LPR >= 2) v += dpp_f<DPP_XOR1>(v);
-  if (LPR >= 4) v += dpp_f<DPP_XOR2>(v);
-  if (LPR >= 8) v += dpp_f<DPP_HALF_MIRROR>(v);
-  if (LPR >= 16) v += dpp_f<DPP_MIRROR>(v);
-  if (LPR >= 32) v += __shfl_xor(v, 16);
-  if (LPR >= 64) v += __shfl_xor(v, 32);
-  return v;
-}
-
-// (maximum, lowest index among the maxima) over the group
-__device__ __forceinline__ void argmax_step(float& mx, int& am, float om, int oa) {
-  const bool take = om > mx || (om == mx && oa < am);
-  mx = take ? om : mx;
-  am = take ? oa : am;
-}
-template <int LPR>
-__device__ __forceinline__ void group_argmax(float& mx, int& am) {
-  if (LPR >= 2) argmax_step(mx, am, dpp_f<DPP_XOR1>(mx), dpp_i<DPP_XOR1>(am));
-  if (LPR >= 4) argmax_step(mx, am, dpp_f<DPP_XOR2>(mx), dpp_i<DPP_XOR2>(am));
-  if (LPR >= 8) argmax_step(mx, am, dpp_f<DPP_HALF_MIRROR>(mx), dpp_i<DPP_HALF_MIRROR>(am));
-  if (LPR >= 16) argmax_step(mx, am, dpp_f<DPP_MIRROR>(mx), dpp_i<DPP_MIRROR>(am));
-  if (LPR >= 32) argmax_step(mx, am, __shfl_xor(mx, 16), __shfl_xor(am, 16));
-  if (LPR >= 64) argmax_step(mx, am, __shfl_xor(mx, 32), __shfl_xor(am, 32));
-}
-
 // Rows handled per lane group and iteration (R): all their loads go out
 // before any is used (one memory latency per iteration instead of one per
 // row).  R = 4 when one row per iteration would give more than
 // LOSS_R4_GROUPS workgroups, else R = 1 (fewer rows keep more workgroups).
 constexpr int64_t LOSS_R4_GROUPS = 16384;
-
-template <typename T> __device__ __forceinline__ float max_finite();
-template <> __device__ __forceinline__ float max_finite<float>() { return 3.40282347e38f; }
-template <> __device__ __forceinline__ float max_finite<f16>() { return 65504.f; }
-template <> __device__ __forceinline__ float max_finite<bf16>() { return 3.38953139e38f; }
-
-// Any non-finite element among the VE packed values (exponent field all ones).
-template <typename T> __device__ __forceinline__ bool packed_nonfinite(uint4 o);
-template <> __device__ __forceinline__ bool packed_nonfinite<float>(uint4 o) {
-  const uint32_t e = 0x7f800000u;
-  return (o.x & e) == e || (o.y & e) == e || (o.z & e) == e || (o.w & e) == e;
-}
-template <uint32_t E>
-__device__ __forceinline__ bool half_pair_nonfinite(uint32_t w) {
-  return (w & E) == E || (w & (E << 16)) == (E << 16);
-}
-template <> __device__ __forceinline__ bool packed_nonfinite<f16>(uint4 o) {
-  return half_pair_nonfinite<0x7c00u>(o.x) || half_pair_nonfinite<0x7c00u>(o.y) ||
-         half_pair_nonfinite<0x7c00u>(o.z) || half_pair_nonfinite<0x7c00u>(o.w);
-}
-template <> __device__ __forceinline__ bool packed_nonfinite<bf16>(uint4 o) {
-  return half_pair_nonfinite<0x7f80u>(o.x) || half_pair_nonfinite<0x7f80u>(o.y) ||
-         half_pair_nonfinite<0x7f80u>(o.z) || half_pair_nonfinite<0x7f80u>(o.w);
-}
 
 // FULL: C = LPR * VE, so every lane holds VE classes and no element needs
 // a bounds test.  The exponentials use the hardware

@@ -23,6 +23,8 @@ __all__ = [
     "gcn_transform_workspace_size", "gcn_transform", "gcn_aggregate_workspace_size", "gcn_aggregate",
     "gcn_sample_pairs", "gcn_pair_loss_workspace_size", "gcn_pair_loss", "gcn_pair_backward_workspace_size",
     "gcn_pair_backward", "gcn_pair_metrics_workspace_size", "gcn_pair_metrics",
+    "gcn_top_logits_workspace_size", "gcn_top_logits", "gcn_distill_workspace_size", "gcn_distill",
+    "gcn_sample_labels_workspace_size", "gcn_sample_labels",
 ]
 
 GCN_F32, GCN_F16, GCN_BF16 = 0, 1, 2
@@ -42,6 +44,8 @@ EXPORTED = (
     "gcn_sample_pairs", "gcn_pair_loss_workspace_size", "gcn_pair_loss", "gcn_pair_backward_workspace_size",
     "gcn_pair_backward", "gcn_pair_metrics_workspace_size", "gcn_pair_metrics",
     "gcn_cast", "gcn_optimizer_step_half",
+    "gcn_top_logits_workspace_size", "gcn_top_logits", "gcn_distill_workspace_size", "gcn_distill",
+    "gcn_sample_labels_workspace_size", "gcn_sample_labels",
 )
 
 _DTYPES = {GCN_F32: torch.float32, GCN_F16: torch.float16, GCN_BF16: torch.bfloat16}
@@ -114,6 +118,7 @@ def lib():
                            "(python -c 'import __graft_entry__ as g; g.build()')")
     L = ctypes.CDLL(LIB_PATH)
     P, I64, I32, SZ = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_size_t
+    F = ctypes.c_float
     PSZ = ctypes.POINTER(ctypes.c_size_t)
     PI64 = ctypes.POINTER(ctypes.c_int64)
     PADJ = ctypes.POINTER(GcnAdj)
@@ -133,6 +138,12 @@ def lib():
         "gcn_layer_bwd_noalloc": (I32, [PADJ, PLAY, I32, P, P, P, I32, ctypes.c_float, P, P, P, P, P, P, P]),
         "gcn_loss_workspace_size": (I32, [I64, I64, PSZ]),
         "gcn_loss": (I32, [I64, I64, I64, I32, P, P, P, I64, P, P, P, P, P, P, P, SZ, P]),
+        "gcn_top_logits_workspace_size": (I32, [I64, I64, I64, I32, PSZ]),
+        "gcn_top_logits": (I32, [I64, I64, I64, I32, P, I64, I64, P, P, P, P, SZ, P]),
+        "gcn_distill_workspace_size": (I32, [I64, I64, I64, I32, PSZ]),
+        "gcn_distill": (I32, [I64, I64, I64, I32, P, I64, I64, I32, P, P, P, I64, F, F, P, P, P, P, P, P, P, SZ, P]),
+        "gcn_sample_labels_workspace_size": (I32, [I64, I64, I32, PSZ]),
+        "gcn_sample_labels": (I32, [I64, I64, I64, I32, P, P, P, F, I64, F, F, P, P, P, P, SZ, P]),
         "gcn_optimizer_step": (I32, [I64, P, P, P, P, P, I32, ctypes.POINTER(GcnAdamConfig), P, P, P]),
         "gcn_transform_workspace_size": (I32, [I64, I64, I64, I32, PSZ]),
         "gcn_transform": (I32, [I64, I64, I64, I32, P, I64, P, I64, P, I64, P, P, SZ, P]),
@@ -268,6 +279,53 @@ def gcn_loss(n, C, ld, prec, logits, labels, mask, n_mask, loss_scale, loss, dlo
                         _ptr(loss), _ptr(dlogits), _ptr(dlogits_colsum), _ptr(n_correct), _ptr(overflow),
                         _ptr(workspace), workspace.numel() * workspace.element_size(), _stream(stream))
     _check(st, "gcn_loss")
+
+
+MAX_TOP = 256             # GCN_MAX_TOP
+MIN_TEMPERATURE, MAX_TEMPERATURE = 2.0 ** -10, 1024.0   # GCN_MIN_TEMPERATURE, GCN_MAX_TEMPERATURE
+
+
+def gcn_top_logits_workspace_size(n, C, K, prec) -> int:
+    b = ctypes.c_size_t(0)
+    _check(lib().gcn_top_logits_workspace_size(n, C, K, prec, ctypes.byref(b)), "gcn_top_logits_workspace_size")
+    return b.value
+
+
+def gcn_top_logits(n, C, ld, prec, logits, K, ld_top, top_values, top_classes, overflow, workspace, stream=None):
+    st = lib().gcn_top_logits(n, C, ld, prec, _ptr(logits), K, ld_top, _ptr(top_values), _ptr(top_classes),
+                              _ptr(overflow), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                              _stream(stream))
+    _check(st, "gcn_top_logits")
+
+
+def gcn_distill_workspace_size(n, C, K, prec) -> int:
+    b = ctypes.c_size_t(0)
+    _check(lib().gcn_distill_workspace_size(n, C, K, prec, ctypes.byref(b)), "gcn_distill_workspace_size")
+    return b.value
+
+
+def gcn_distill(n, C, ld, prec, logits, K, ld_top, top_prec, top_values, top_classes, mask, n_mask, temperature,
+                weight, loss_scale, dlogits_base, loss, dlogits, overflow, workspace, stream=None,
+                dlogits_colsum=None):
+    st = lib().gcn_distill(n, C, ld, prec, _ptr(logits), K, ld_top, top_prec, _ptr(top_values), _ptr(top_classes),
+                           _ptr(mask), n_mask, temperature, weight, _ptr(loss_scale), _ptr(dlogits_base), _ptr(loss),
+                           _ptr(dlogits), _ptr(dlogits_colsum), _ptr(overflow), _ptr(workspace),
+                           workspace.numel() * workspace.element_size(), _stream(stream))
+    _check(st, "gcn_distill")
+
+
+def gcn_sample_labels_workspace_size(n, C, prec) -> int:
+    b = ctypes.c_size_t(0)
+    _check(lib().gcn_sample_labels_workspace_size(n, C, prec, ctypes.byref(b)), "gcn_sample_labels_workspace_size")
+    return b.value
+
+
+def gcn_sample_labels(n, C, ld, prec, logits, mask, u, temperature, top_k, top_p, min_p, labels, prob, overflow,
+                      workspace, stream=None):
+    st = lib().gcn_sample_labels(n, C, ld, prec, _ptr(logits), _ptr(mask), _ptr(u), temperature, top_k, top_p, min_p,
+                                 _ptr(labels), _ptr(prob), _ptr(overflow), _ptr(workspace),
+                                 workspace.numel() * workspace.element_size(), _stream(stream))
+    _check(st, "gcn_sample_labels")
 
 
 def gcn_optimizer_step(count, master, grad, m, v, working, prec, cfg: GcnAdamConfig, state, overflow,
