@@ -138,6 +138,10 @@ class GCN2:
       hold A_hat in fp32, CSR or row-major dense.
     * O3: every tensor in 16 bits, the weights and the Adam moments
       included (gcn_optimizer_step_half); no master copy and no loss scale.
+
+    A model's scores make a teacher (top_logits), a student learns from one
+    beside its labels (set_teacher), and labels can be drawn from a model's own
+    distribution (sample_labels).
     """
 
     def __init__(self, graph: DeviceGraph, X, labels, mask, W1, W2, b1=None, b2=None, prec=G.GCN_F16,
@@ -267,9 +271,17 @@ class GCN2:
                  0 if self.featureless else G.gcn_transform_workspace_size(n, self.f_in, self.f_h, prec),
                  G.gcn_transform_workspace_size(n, self.f_h, self.C, prec),
                  G.gcn_aggregate_workspace_size(self.adj, self.f_h, prec),
-                 G.gcn_aggregate_workspace_size(self.adj, self.C, prec))
+                 G.gcn_aggregate_workspace_size(self.adj, self.C, prec),
+                 G.gcn_distill_workspace_size(n, self.C, G.MAX_TOP, G.GCN_F32 if level == "O1" else prec),
+                 G.gcn_top_logits_workspace_size(n, self.C, G.MAX_TOP, prec),
+                 G.gcn_sample_labels_workspace_size(n, self.C, prec))
         self.ws = torch.empty(ws // 4 + 64, dtype=torch.float32, device=dev)
         self.adam_c = self.adam.c()
+        self.teacher = None
+        # raised by top_logits and sample_labels (scores that are not finite);
+        # `overflow` is the training step's, which the optimiser answers by
+        # skipping the step
+        self.scores_overflow = torch.zeros(1, dtype=torch.int32, device=dev)
 
     # parameter views
     def _view(self, buf, k, shape):
@@ -337,14 +349,18 @@ class GCN2:
             G.gcn_cast(self.n, self.C, self.prec, self.Z2, self.ld_c, G.GCN_F32, self.Z2f, self.ld_c, None, stream)
             G.gcn_loss(self.n, self.C, self.ld_c, G.GCN_F32, self.Z2f, self.labels, self.mask, self.n_mask,
                        self.scale_ptr(), self.loss, self.dZ2f, self.n_correct, self.overflow, self.ws, stream)
+            if self.teacher is not None:
+                self._distill(G.GCN_F32, self.Z2f, self.dZ2f, None, stream)
             G.gcn_cast(self.n, self.C, G.GCN_F32, self.dZ2f, self.ld_c, self.prec, self.dZ2, self.ld_c,
                        self.overflow, stream)
             db2 = self.db2()
         else:
-            # db2 (the column sums of dZ2) comes from the loss kernel
+            # db2 (the column sums of dZ2) comes from the last loss kernel
             G.gcn_loss(self.n, self.C, self.ld_c, self.prec, self.Z2, self.labels, self.mask, self.n_mask,
                        self.scale_ptr(), self.loss, self.dZ2, self.n_correct, self.overflow, self.ws, stream,
-                       dlogits_colsum=self.db2())
+                       dlogits_colsum=self.db2() if self.teacher is None else None)
+            if self.teacher is not None:
+                self._distill(self.prec, self.Z2, self.dZ2, self.db2(), stream)
             db2 = None
         # db1 (the column sums of dZ1) comes from the call that writes dZ1
         G.gcn_layer_bwd(a, self.L2, self.prec, self.H1, self.W2w(), self.dZ2, G.GCN_ACT_RELU, self.p,
@@ -352,6 +368,79 @@ class GCN2:
                         dbias_below=self.db1())
         G.gcn_layer_bwd(a, self.L1, self.prec, self.X, self.W1w(), self.dZ1, G.GCN_ACT_NONE, 0.0,
                         self.dW1(), None, None, self.SG1, self.overflow, self.ws, stream)
+
+    def set_teacher(self, top_values, top_classes, mask=None, temperature: float = 2.0, weight: float = 1.0):
+        """From now on every step also learns from a teacher's top scores
+        (device tensors n x ld_top as top_logits returns them, or None to
+        stop): the loss of gcn_distill at ``temperature``, times ``weight``,
+        over the rows of ``mask`` (uint8, None = every row) is added to the
+        cross-entropy.  ``distill_loss`` holds its value after a step, ``loss``
+        the cross-entropy's as before.  Not while an epoch is captured: the
+        graph would go on with what it recorded."""
+        if self.graph is not None:
+            raise ValueError("the captured epoch keeps its own losses: set the teacher before capture()")
+        if top_values is None:
+            self.teacher = None
+            return
+        dev = self.loss.device
+        precs = {dt: p for p, dt in ((p, G.torch_dtype(p)) for p in (G.GCN_F32, G.GCN_F16, G.GCN_BF16))}
+        if (top_values.dim() != 2 or top_values.shape[0] != self.n or top_values.shape != top_classes.shape
+                or top_classes.dtype != torch.int32 or top_values.dtype not in precs
+                or not (top_values.is_contiguous() and top_classes.is_contiguous())
+                or top_values.device != dev or top_classes.device != dev):
+            raise ValueError(f"a teacher is two contiguous tensors {self.n} x K on {dev}: scores and int32 classes")
+        n_mask = self.n
+        if mask is not None:
+            mask = torch.as_tensor(mask).to(dev, torch.uint8).contiguous()
+            if tuple(mask.shape) != (self.n,):
+                raise ValueError(f"the mask holds one entry for each of the {self.n} rows")
+            n_mask = int(torch.count_nonzero(mask).item())
+        K = top_values.shape[1]
+        if K % 8:      # the library's layout: rows padded to a multiple of 8
+            pad = round8(K)
+            v = torch.full((self.n, pad), float("-inf"), dtype=top_values.dtype, device=dev)
+            c = torch.full((self.n, pad), -1, dtype=torch.int32, device=dev)
+            v[:, :K], c[:, :K] = top_values, top_classes
+            top_values, top_classes = v, c
+        self.distill_loss = torch.zeros(1, dtype=torch.float32, device=dev)
+        self.teacher = dict(prec=precs[top_values.dtype], values=top_values, classes=top_classes, K=K, mask=mask,
+                            n_mask=n_mask, temperature=float(temperature), weight=float(weight))
+
+    def _distill(self, prec, Z, dZ, colsum, stream):
+        t = self.teacher
+        G.gcn_distill(self.n, self.C, self.ld_c, prec, Z, t["K"], t["values"].shape[1], t["prec"], t["values"],
+                      t["classes"], t["mask"], t["n_mask"], t["temperature"], t["weight"], self.scale_ptr(), dZ,
+                      self.distill_loss, dZ, self.overflow, self.ws, stream, dlogits_colsum=colsum)
+
+    def top_logits(self, K: int, stream=None):
+        """The K largest scores of every vertex from the last forward pass and
+        their classes (two tensors n x round8(K), entries past K empty): a
+        teacher for another model's set_teacher."""
+        ld = round8(K)
+        v = torch.full((self.n, ld), float("-inf"), dtype=self.dt, device=self.Z2.device)
+        c = torch.full((self.n, ld), -1, dtype=torch.int32, device=self.Z2.device)
+        if stream is not None:      # the fills above ran on the current stream
+            stream.wait_stream(torch.cuda.current_stream())
+            v.record_stream(stream)
+            c.record_stream(stream)
+        G.gcn_top_logits(self.n, self.C, self.ld_c, self.prec, self.Z2, K, ld, v, c, self.scores_overflow, self.ws,
+                         stream)
+        return v, c
+
+    def sample_labels(self, u, labels, prob=None, mask=None, temperature: float = 1.0, top_k: int = 0,
+                      top_p: float = 1.0, min_p: float = 0.0, stream=None):
+        """Draws a label for every vertex of ``mask`` (uint8, None = all) from
+        the scores of the last forward pass into ``labels`` (int32 [n]) and
+        its probability into ``prob`` (fp32 [n]), from the uniform numbers
+        ``u`` (fp32 [n]); the other entries keep their values, so that
+        ``labels`` may be the training labels.  Asynchronous."""
+        for name, t, dt in (("u", u, torch.float32), ("labels", labels, torch.int32), ("prob", prob, torch.float32),
+                            ("mask", mask, torch.uint8)):
+            if t is not None and (t.dtype != dt or tuple(t.shape) != (self.n,) or not t.is_contiguous()
+                                  or t.device != self.Z2.device):
+                raise ValueError(f"{name}: a contiguous {dt} tensor of {self.n} elements on {self.Z2.device}")
+        G.gcn_sample_labels(self.n, self.C, self.ld_c, self.prec, self.Z2, mask, u, temperature, top_k, top_p, min_p,
+                            labels, prob, self.scores_overflow, self.ws, stream)
 
     def optimizer_step(self, stream=None):
         if self.level == "O3":
