@@ -1,62 +1,337 @@
 // The K largest scores of every row with their classes, in falling order, the
-// lower class first among equals.
+// lower class first among equals.  Scores are turned into items (sorted.h), of
+// which no two are equal, so that ties need no care.
 //
-// One workgroup takes a row.  Round j finds the largest (key, class) pair that
-// comes after the one round j - 1 found, so no list is kept and rows of any
-// length and any number of equal scores are right.
+// Bound by the read of the scores; what has to be kept small is the number of
+// comparisons a score takes part in.
+#include <algorithm>
+
 #include "internal.h"
-#include "rows.h"
+#include "sorted.h"
 
 namespace gcn {
 
 namespace {
 
-// score key above, complement of the class below: the larger pair comes first
-__device__ __forceinline__ uint64_t pair_of(uint32_t key, int64_t c) {
-  return ((uint64_t)key << 32) | (uint32_t)~(uint32_t)c;
+template <typename T, typename I>
+__device__ __forceinline__ void put_entry(const TopParams& p, int64_t row, int64_t j, I a) {
+  const bool here = item_present<T>(a);
+  reinterpret_cast<T*>(p.values)[row * p.ld_top + j] = here ? item_score<T>(a) : from_f32<T>(-INFINITY);
+  p.classes[row * p.ld_top + j] = here ? item_class(a) : -1;
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void top_rounds_kernel(TopParams p) {
-  __shared__ uint64_t sh[4];
-  const int64_t row = blockIdx.x;
-  const T* __restrict__ z = reinterpret_cast<const T*>(p.logits) + row * p.ld;
-  T* __restrict__ vals = reinterpret_cast<T*>(p.values) + row * p.ld_top;
-  int32_t* __restrict__ ids = p.classes + row * p.ld_top;
+// Joins the lists of lanes W apart, W = 1, 2, 4, ...: H items are in use.
+template <int LPR, int L, int W, int H, typename I>
+__device__ __forceinline__ void list_levels(I (&a)[L]) {
+  if constexpr (W < LPR) {
+    if constexpr (2 * H <= L) {
+      // both lists whole: the larger halves of the pairs, then the smaller
+      I hi[H], lo[H];
+#pragma unroll
+      for (int i = 0; i < H; ++i) {
+        const I o = lane_xor<W>(a[H - 1 - i]);
+        hi[i] = item_max(a[i], o);
+        lo[i] = item_min(a[i], o);
+      }
+      merge_bitonic<H>(hi);
+      merge_bitonic<H>(lo);
+#pragma unroll
+      for (int i = 0; i < H; ++i) { a[i] = hi[i]; a[H + i] = lo[i]; }
+      list_levels<LPR, L, 2 * W, 2 * H>(a);
+    } else {
+      static_assert(H == L, "list lengths are powers of two");
+      I hi[L];
+#pragma unroll
+      for (int i = 0; i < L; ++i) hi[i] = item_max(a[i], lane_xor<W>(a[L - 1 - i]));
+      merge_bitonic<L>(hi);
+#pragma unroll
+      for (int i = 0; i < L; ++i) a[i] = hi[i];
+      list_levels<LPR, L, 2 * W, L>(a);
+    }
+  }
+}
+
+// Rows of up to 64 vectors of 16 bytes: a group of LPR lanes owns a row.
+//
+// L > 0: the first L >= K items only.  Each lane sorts its own, then lists are
+// merged pairwise across lanes: of two sorted lists of L, the larger of item
+// i of one and item L - 1 - i of the other are the L largest of both, in
+// bitonic order, so a merge costs L maxima and log2 L steps; every lane of the
+// group ends with the row's list.  (Shorter lists are joined whole until they
+// have L items.)
+// L = 0: the row is sorted over the group.
+template <typename T, int LPR, int L, int R>
+__global__ __launch_bounds__(256) void top_group_kernel(TopParams p) {
+  constexpr int VE = Vec<T>::N;
+  constexpr int RG = 4 * (64 / LPR);
+  typedef typename ItemOf<T>::type I;
+  const int lane = threadIdx.x & 63, li = lane % LPR;
+  const int slot = (threadIdx.x >> 6) * (64 / LPR) + lane / LPR;
+  const int col0 = li * VE;
+  const bool col_ok = col0 < p.C;
+  const int nv = (int)(p.C - col0 < VE ? (p.C - col0 > 0 ? p.C - col0 : 0) : VE);
+  const T* __restrict__ logits = reinterpret_cast<const T*>(p.logits);
   bool bad = false;
-  uint64_t last = ~0ull;
-  for (int64_t j = 0; j < p.K; ++j) {
-    uint64_t best = 0;
-    for (int64_t c = threadIdx.x; c < p.C; c += 256) {
-      const float v = to_f32<T>(z[c]);
-      if (!(v < INFINITY)) bad = true;
-      if (!(v > -INFINITY)) continue;                    // -inf and NaN are no candidates
-      const uint64_t q = pair_of(score_key(v), c);
-      if (q < last && q > best) best = q;
+  for (int64_t first = (int64_t)blockIdx.x * (R * RG); first < p.n; first += (int64_t)gridDim.x * (R * RG)) {
+    uint4 raw[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      int64_t row = first + r * RG + slot;
+      row = row < p.n ? row : p.n - 1;               // in bounds; not stored below
+      raw[r] = ldg16(logits + row * p.ld + (col_ok ? col0 : 0));
     }
-    best = block_reduce<4>(best, sh, MaxF());
-    if (threadIdx.x == 0) {
-      vals[j] = from_f32<T>(best ? key_score((uint32_t)(best >> 32)) : -INFINITY);
-      ids[j] = best ? (int32_t)~(uint32_t)best : -1;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int64_t row = first + r * RG + slot;
+      const bool row_ok = row < p.n;
+      I a[VE];
+      bad |= make_items<T>(raw[r], col0, nv, a);
+      if constexpr (L > 0) {
+        I list[L];
+        sort_items<VE>(a);
+#pragma unroll
+        for (int i = 0; i < L; ++i) list[i] = i < VE ? a[i < VE ? i : 0] : I{0};
+        list_levels<LPR, L, 1, VE>(list);
+        // entry j is written by lane j mod LPR
+#pragma unroll
+        for (int q = 0; q < (L + LPR - 1) / LPR; ++q) {
+          const int j = q * LPR + li;
+          I e = list[q * LPR < L ? q * LPR : 0];
+#pragma unroll
+          for (int i = 1; i < LPR && q * LPR + i < L; ++i) e = item_pick(li == i, list[q * LPR + i], e);
+          if (row_ok && j < L && j < p.K) put_entry<T>(p, row, j, e);
+        }
+      } else {
+        group_sort<LPR, VE>(a, li);
+#pragma unroll
+        for (int i = 0; i < VE; ++i)
+          if (row_ok && col0 + i < p.K) put_entry<T>(p, row, col0 + i, a[i]);
+      }
+      // entries past the classes the group holds
+      constexpr int HELD = L > 0 ? L : LPR * VE;
+      if (HELD < GCN_MAX_TOP && row_ok)
+        for (int64_t j = HELD + li; j < p.K; j += LPR) put_entry<T>(p, row, j, I{0});
     }
-    last = best;
   }
   if (bad) raise_flag(p.flag);
 }
 
+// Longer rows: a workgroup of NT threads takes a row and holds it in its
+// registers, NV vectors a thread (NV = 0: the row is read again from the
+// caches whenever it is needed).
+//   1. Every thread finds the largest of its scores.
+//   2. In each wave the r-th largest of these, r = ceil(K / waves), is a score
+//      that r classes of the wave reach; the smallest over the waves, b, is one
+//      that at least K classes of the row reach.  (Only waves whose lanes all
+//      hold scores are asked.)
+//   3. The classes that reach b are listed in shared memory: for scores in no
+//      particular order a few times K.  Where they are too many (rows sorted by
+//      class, many equal scores), b is raised by bisection between what K
+//      items reach and what fewer do, until the list holds them.
+//   4. An entry's place is the number of listed items above it.
+constexpr int TOP_LIST = 1024;
+
+template <typename T, int NT, int NV>
+struct TopRow {
+  static constexpr int VE = Vec<T>::N;
+  static constexpr int NW = NT / 64;
+  const T* __restrict__ z;
+  int C;
+  uint4 raw[NV > 0 ? NV : 1];
+
+  // f(vector, first class, classes of it in the row) over this thread's vectors
+  template <typename F>
+  __device__ __forceinline__ void each(F f) const {
+    if constexpr (NV > 0) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const int c0 = (v * NT + (int)threadIdx.x) * VE;
+        if (c0 < C) f(raw[v], c0, C - c0 < VE ? C - c0 : VE);
+      }
+    } else {
+      for (int c0 = (int)threadIdx.x * VE; c0 < C; c0 += NT * VE)
+        f(ldg16(z + c0), c0, C - c0 < VE ? C - c0 : VE);
+    }
+  }
+  __device__ __forceinline__ void load() {
+    if constexpr (NV > 0) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const int c0 = (v * NT + (int)threadIdx.x) * VE;
+        raw[v] = ldg16(z + (c0 < C ? c0 : 0));
+      }
+    }
+  }
+};
+
+// A score's item with 64 bits, whatever its type.
+__device__ __forceinline__ Item64 score_item(float v, int c) { return item64(score_key(v), (uint32_t)c); }
+
+template <typename T, int NT, int NV>
+__global__ __launch_bounds__(NT) void top_row_kernel(TopParams p) {
+  constexpr int VE = Vec<T>::N;
+  constexpr int NW = NT / 64;
+  __shared__ float sh_b[NW];
+  __shared__ int sh_n[NW];
+  __shared__ int s_count;
+  __shared__ double s_list[TOP_LIST];
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int64_t row = blockIdx.x;
+  TopRow<T, NT, NV> r;
+  r.z = reinterpret_cast<const T*>(p.logits) + row * p.ld;
+  r.C = (int)p.C;
+  r.load();
+  if (t == 0) s_count = 0;
+  bool bad = false;
+  float mx = -INFINITY;
+  r.each([&](uint4 raw, int, int nv) {
+    float v[VE];
+    unpack<T>(raw, v);
+#pragma unroll
+    for (int i = 0; i < VE; ++i) {
+      const bool here = i < nv;
+      bad |= here && !(v[i] < INFINITY);
+      mx = here && v[i] > mx ? v[i] : mx;
+    }
+  });
+  if (bad) raise_flag(p.flag);
+  // the r-th largest of the wave's 64 maxima, or -inf
+  const int K = (int)p.K;
+  const int full = r.C / (64 * VE) < NW ? r.C / (64 * VE) : NW;   // at least 1: shorter rows have a lane group
+  const int rounds = (K + full - 1) / full;
+  float left = mx, b = -INFINITY;
+  if (rounds <= 64) {
+    for (int i = 0; i < rounds; ++i) {
+      b = group_max<64>(left);
+      const uint64_t who = __ballot(left == b);
+      if (lane == __ffsll((unsigned long long)who) - 1) left = -INFINITY;
+    }
+  }
+  if (lane == 0) sh_b[wave] = b;
+  __syncthreads();
+  b = sh_b[0];
+  for (int i = 1; i < full; ++i) b = fminf(b, sh_b[i]);
+  // list what reaches b (all finite scores if b is -inf)
+  auto list = [&](double from) {
+    r.each([&](uint4 raw, int c0, int nv) {
+      float v[VE];
+      unpack<T>(raw, v);
+      bool any = false;
+#pragma unroll
+      for (int i = 0; i < VE; ++i) any |= v[i] >= b && v[i] > -INFINITY && i < nv;
+      if (!any) return;
+#pragma unroll
+      for (int i = 0; i < VE; ++i) {
+        if (!(v[i] >= b && v[i] > -INFINITY) || i >= nv) continue;
+        const Item64 e = score_item(v[i], c0 + i);
+        if (e.v < from) continue;
+        const int at = atomicAdd(&s_count, 1);
+        if (at < TOP_LIST) s_list[at] = e.v;
+      }
+    });
+  };
+  list(0.0);
+  __syncthreads();
+  int cnt = s_count;
+  if (cnt > TOP_LIST) {
+    // items from `from` on are K at least and, at the end, TOP_LIST at most
+    uint64_t lo = (uint64_t)__double_as_longlong(score_item(b > -INFINITY ? b : -3.402823466e38f, 0x3fffffff).v);
+    uint64_t hi = (uint64_t)__double_as_longlong(item64(0xffffffffu, 0).v);
+    if (b == -INFINITY) lo = 0;
+    while (cnt > TOP_LIST) {
+      const uint64_t mid = lo + (hi - lo) / 2 + 1;
+      const double m = __longlong_as_double((long long)mid);
+      int n = 0;
+      r.each([&](uint4 raw, int c0, int nv) {
+        float v[VE];
+        unpack<T>(raw, v);
+#pragma unroll
+        for (int i = 0; i < VE; ++i)
+          if (i < nv && v[i] >= b && v[i] > -INFINITY) n += score_item(v[i], c0 + i).v >= m ? 1 : 0;
+      });
+      n = block_reduce<NW>(n, sh_n, AddF());
+      if (n >= K) { lo = mid; cnt = n; }
+      else hi = mid - 1;
+    }
+    if (t == 0) s_count = 0;
+    __syncthreads();
+    list(__longlong_as_double((long long)lo));
+    __syncthreads();
+    cnt = s_count;
+  }
+  // places: several threads count for one item where the list is short
+  int per = 1;
+  while (per < 64 && 2 * per * cnt <= NT) per *= 2;
+  const int sub = t % per;
+  for (int i = t / per; i < cnt; i += NT / per) {
+    const double e = s_list[i];
+    int above = 0;
+    for (int j = sub; j < cnt; j += per) above += s_list[j] > e ? 1 : 0;
+    for (int m = 1; m < per; m <<= 1) above += __shfl_xor(above, m);
+    if (sub == 0 && above < K) put_entry<T>(p, row, above, Item64{e});
+  }
+  for (int j = cnt + t; j < K; j += NT) put_entry<T>(p, row, j, Item64{0.0});
+}
+
+// ------------------------------------------------------------- launches ----
+
+constexpr int64_t MAX_BLOCKS = 65536;
+// Rows a lane group takes per iteration (their loads go out together): 4 when
+// that still leaves this many workgroups, else 1.
+constexpr int64_t R4_GROUPS = 16384;
+
+template <typename T, int LPR, int L>
+hipError_t launch_l(const TopParams& p, hipStream_t s) {
+  constexpr int64_t RG = 4 * (64 / LPR);
+  const int r = (p.n + RG - 1) / RG > R4_GROUPS ? 4 : 1;
+  const int64_t nb = std::min<int64_t>((p.n + r * RG - 1) / (r * RG), MAX_BLOCKS);
+  if (r == 4)
+    hipLaunchKernelGGL((top_group_kernel<T, LPR, L, 4>), dim3((unsigned)nb), dim3(256), 0, s, p);
+  else
+    hipLaunchKernelGGL((top_group_kernel<T, LPR, L, 1>), dim3((unsigned)nb), dim3(256), 0, s, p);
+  return hipGetLastError();
+}
+template <typename T, int LPR>
+hipError_t launch_lpr(const TopParams& p, hipStream_t s) {
+  if (p.K <= 8) return launch_l<T, LPR, 8>(p, s);
+  if (p.K <= 16) return launch_l<T, LPR, 16>(p, s);
+  return launch_l<T, LPR, 0>(p, s);
+}
+template <typename T>
+hipError_t launch_rows(const TopParams& p, hipStream_t s) {
+  const int64_t nvec = (p.C + Vec<T>::N - 1) / Vec<T>::N;
+  const dim3 grid((unsigned)p.n);
+  // the bound of step 2 is close where K is small against the threads
+  if (nvec <= 8 * 256 && p.K <= 32) hipLaunchKernelGGL((top_row_kernel<T, 256, 8>), grid, dim3(256), 0, s, p);
+  else if (nvec <= 8 * 512 && p.K <= 64) hipLaunchKernelGGL((top_row_kernel<T, 512, 8>), grid, dim3(512), 0, s, p);
+  else if (nvec <= 8 * 1024) hipLaunchKernelGGL((top_row_kernel<T, 1024, 8>), grid, dim3(1024), 0, s, p);
+  else hipLaunchKernelGGL((top_row_kernel<T, 1024, 0>), grid, dim3(1024), 0, s, p);
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t launch_t(const TopParams& p, hipStream_t s) {
+  const int64_t nvec = (p.C + Vec<T>::N - 1) / Vec<T>::N;
+  if (nvec <= 1) return launch_lpr<T, 1>(p, s);
+  if (nvec <= 2) return launch_lpr<T, 2>(p, s);
+  if (nvec <= 4) return launch_lpr<T, 4>(p, s);
+  if (nvec <= 8) return launch_lpr<T, 8>(p, s);
+  if (nvec <= 16) return launch_lpr<T, 16>(p, s);
+  if (nvec <= 32) return launch_lpr<T, 32>(p, s);
+  if (nvec <= 64) return launch_lpr<T, 64>(p, s);
+  return launch_rows<T>(p, s);
+}
+
 }  // namespace
 
-size_t top_workspace_bytes(int prec, int64_t n, int64_t C, int64_t K) { return 256; }
+size_t top_workspace_bytes(int, int64_t, int64_t, int64_t) { return 256; }
 
-hipError_t top_launch(int prec, const TopParams& p, void* ws, hipStream_t s) {
-  const dim3 grid((unsigned)p.n);
+hipError_t top_launch(int prec, const TopParams& p, void*, hipStream_t s) {
   switch (prec) {
-    case 0: hipLaunchKernelGGL((top_rounds_kernel<float>), grid, dim3(256), 0, s, p); break;
-    case 1: hipLaunchKernelGGL((top_rounds_kernel<f16>), grid, dim3(256), 0, s, p); break;
-    case 2: hipLaunchKernelGGL((top_rounds_kernel<bf16>), grid, dim3(256), 0, s, p); break;
+    case 0: return launch_t<float>(p, s);
+    case 1: return launch_t<f16>(p, s);
+    case 2: return launch_t<bf16>(p, s);
     default: return hipErrorInvalidValue;
   }
-  return hipGetLastError();
 }
 
 }  // namespace gcn
