@@ -212,7 +212,9 @@ struct SampleParams {
   const void* logits;
   const uint8_t* mask;
   const float* u;
-  double T;             // 0: the largest score
+  double T;
+  float k;              // log2(e) / T
+  bool greedy;          // the first class of the order: u is not read
   int64_t top_k;        // C: no limit
   double top_p;         // 1: no limit
   double ln_min_p;      // -inf: no limit

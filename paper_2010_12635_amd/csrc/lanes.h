@@ -46,6 +46,54 @@ __device__ __forceinline__ float group_max(float v) {
   return v;
 }
 
+// Sum over the lanes of the group before this one (li: the lane's place in it),
+// 0 for the first: never the difference of a sum and this lane's own share,
+// which would lose what is small beside it.
+template <int M>
+__device__ __forceinline__ float lane_before(float v) {
+  return dpp_f<0x110 + M>(v);                            // row_shr, M < 16: within rows of 16
+}
+template <int M>
+__device__ __forceinline__ double lane_before(double v) { return __shfl_up(v, M); }
+template <int LPR, int M, typename W>
+__device__ __forceinline__ W group_scan_steps(W v, int li) {
+  if constexpr (M < LPR) {
+    W o;
+    if constexpr (LPR > 16) o = __shfl_up(v, M);         // groups of several rows of 16 lanes
+    else o = lane_before<M>(v);
+    v += li >= M ? o : W(0);
+    return group_scan_steps<LPR, 2 * M>(v, li);
+  } else {
+    return v;
+  }
+}
+template <int LPR, typename W>
+__device__ __forceinline__ W group_sum_before(W v, int li) {
+  if constexpr (LPR == 1) return W(0);
+  const W upto = group_scan_steps<LPR, 1>(v, li);
+  W o;
+  if constexpr (LPR > 16) o = __shfl_up(upto, 1);
+  else o = lane_before<1>(upto);
+  return li >= 1 ? o : W(0);
+}
+
+template <int LPR>
+__device__ __forceinline__ double group_sum(double v) {
+#pragma unroll
+  for (int m = 1; m < LPR; m <<= 1) v += __shfl_xor(v, m);
+  return v;
+}
+template <int LPR>
+__device__ __forceinline__ int group_sum(int v) {
+  if (LPR >= 2) v += dpp_i<DPP_XOR1>(v);
+  if (LPR >= 4) v += dpp_i<DPP_XOR2>(v);
+  if (LPR >= 8) v += dpp_i<DPP_HALF_MIRROR>(v);
+  if (LPR >= 16) v += dpp_i<DPP_MIRROR>(v);
+  if (LPR >= 32) v += __shfl_xor(v, 16);
+  if (LPR >= 64) v += __shfl_xor(v, 32);
+  return v;
+}
+
 // Whether any lane of the group holds true.
 template <int LPR>
 __device__ __forceinline__ bool group_any(bool v) {

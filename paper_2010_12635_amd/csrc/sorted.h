@@ -177,6 +177,22 @@ __device__ __forceinline__ void sort_items(I* a) {
           if (i + j + k < N && (i + j) / (2 * p) == (i + j + k) / (2 * p)) order2(a[i + j], a[i + j + k]);
 }
 
+// The largest item of a lane group.
+template <int LPR, int M = 1, typename I>
+__device__ __forceinline__ I group_max_item(I a) {
+  if constexpr (M < LPR) return group_max_item<LPR, 2 * M>(item_max(a, lane_xor<M>(a)));
+  else return a;
+}
+template <int LPR, int M = 1>
+__device__ __forceinline__ int group_max_int(int a) {
+  if constexpr (M < LPR) {
+    const int o = lane_xor<M>(a);
+    return group_max_int<LPR, 2 * M>(a > o ? a : o);
+  } else {
+    return a;
+  }
+}
+
 // The LPR * N items of a lane group, N a lane, into order over the whole
 // group: lane li then holds items li N .. li N + N - 1 of the order.  Merge
 // sort whose first step of each merge pairs an item with its mirror image, so

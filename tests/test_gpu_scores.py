@@ -344,10 +344,12 @@ def check_sample(rng, n, C, prec, T, k=0, p=1.0, m=0.0, kind="normal", masked=Fa
     wy, wp = S.sample_labels(z, u.astype(np.float64), T, k, p, m, mask)
     got = y.cpu().numpy()
     assert np.array_equal(got, wy), (np.flatnonzero(got != wy)[:5], got[got != wy][:5], wy[got != wy][:5])
-    # a weight carries 2^-21 at most, their sum 2^-20 (the bounds that a draw
-    # in 32 bits is certified with), the quotient 4 roundings; what 32 bits
-    # hold only as a subnormal number may come out as 0
-    assert (np.abs(pr.double().cpu().numpy() - wp) <= 2.0 ** -19 * np.abs(wp) + 2.0 ** -126).all()
+    # a weight exp(x) carries 3 E |x| log2(e) + 4 E, the kept weights' sum 2^-18
+    # at most (the bound that a draw in 32 bits is certified with), the
+    # quotient 4 E; what 32 bits hold only as a subnormal number may come out
+    # as 0.  |x| is at most ln C - ln prob above the sum's own ln C.
+    x = np.where(wp > 0, -np.log(np.maximum(wp, 1e-300)), 0) + np.log(C)
+    assert (np.abs(pr.double().cpu().numpy() - wp) <= (2.0 ** -18 + (5 * x + 8) * E) * np.abs(wp) + 2.0 ** -126).all()
     assert ov.item() == 0
     y2, _, _ = run_sample(zt, n, C, prec, torch.as_tensor(u).cuda(), T, k, p, m, mt, prob=False)
     assert torch.equal(y, y2)
