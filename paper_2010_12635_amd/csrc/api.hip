@@ -812,7 +812,8 @@ gcn_status gcn_sample_labels(int64_t n, int64_t C, int64_t ld, int32_t prec, con
   p.n = n; p.C = C; p.ld = ld; p.logits = logits; p.mask = mask; p.u = u;
   p.greedy = temperature == 0.f;                         // a draw among one class, at any temperature
   p.T = p.greedy ? 1.0 : (double)temperature;
-  p.k = (float)(1.4426950408889634074 / p.T);
+  p.kd = 1.4426950408889634074 / p.T;
+  p.k = (float)p.kd;
   p.top_k = p.greedy ? 1 : top_k == 0 || top_k > C ? C : top_k;
   p.top_p = top_p;
   p.ln_min_p = std::log((double)min_p);                  // min_p = 0: -inf, no limit

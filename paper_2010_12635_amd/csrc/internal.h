@@ -214,6 +214,7 @@ struct SampleParams {
   const float* u;
   double T;
   float k;              // log2(e) / T
+  double kd;            // the same
   bool greedy;          // the first class of the order: u is not read
   int64_t top_k;        // C: no limit
   double top_p;         // 1: no limit

@@ -10,165 +10,12 @@
 #include <algorithm>
 
 #include "internal.h"
-#include "lanes.h"
-#include "rows.h"
+#include "longrow.h"
 #include "sorted.h"
 
 namespace gcn {
 
 namespace {
-
-// The weights in 64 bits, each sum in a fixed order, for a row taken by NW
-// waves.  The borders of top-k and top-p are found by bisection of the key:
-// every step counts (or sums) the classes whose key lies in half of what is
-// left.
-template <typename T, int NW>
-struct ExactRow {
-  const SampleParams& p;
-  const T* __restrict__ z;
-  double* shd;        // [NW] shared
-  int64_t* shi;       // [NW] shared
-  uint32_t* shu;      // [NW] shared
-  float zmax;
-  static constexpr int NT = 64 * NW;
-
-  __device__ int tid() const { return NW == 1 ? threadIdx.x & 63 : threadIdx.x; }
-  __device__ double weight(float v) const { return exp(((double)v - (double)zmax) / p.T); }
-
-  // Classes with lo < key <= hi.
-  __device__ int64_t count(uint32_t lo, uint32_t hi) const {
-    int64_t m = 0;
-    for (int64_t c = tid(); c < p.C; c += NT) {
-      const uint32_t key = score_key(to_f32<T>(z[c]));
-      m += key > lo && key <= hi ? 1 : 0;
-    }
-    return block_reduce<NW>(m, shi, AddF());
-  }
-  // Their weights.
-  __device__ double mass(uint32_t lo, uint32_t hi) const {
-    double m = 0;
-    for (int64_t c = tid(); c < p.C; c += NT) {
-      const float v = to_f32<T>(z[c]);
-      const uint32_t key = score_key(v);
-      if (key > lo && key <= hi) m += weight(v);
-    }
-    return block_reduce<NW>(m, shd, AddF());
-  }
-
-  // Draws for a row whose maximum is finite and whose scores are not NaN.
-  __device__ void draw(float u, int32_t* label, float* prob) {
-    const uint32_t top = score_key(zmax);
-    uint32_t border = KEY_NEG_INF + 1;   // smallest key kept
-    int64_t take = p.C;                  // classes of that key kept
-    if (p.top_k < p.C) {
-      // the largest key that at least top_k classes reach; with fewer finite
-      // scores than top_k every one is kept
-      if (count(KEY_NEG_INF, top) > p.top_k) {
-        uint32_t lo = KEY_NEG_INF + 1, hi = top;
-        int64_t above = 0;               // classes with key > hi
-        while (lo < hi) {
-          const uint32_t mid = lo + (hi - lo) / 2;
-          const int64_t m = count(mid, hi);
-          if (above + m >= p.top_k) lo = mid + 1;
-          else { hi = mid; above += m; }
-        }
-        border = lo;
-        take = p.top_k - above;
-      }
-    }
-    if (p.top_p < 1.0) {
-      const int64_t here = count(border - 1, border);
-      const int64_t avail = take < here ? take : here;
-      const double w_border = weight(key_score(border));
-      const double kept = mass(border, top) + (double)avail * w_border;
-      const double want = p.top_p * kept;
-      // the largest key whose classes, and those above, reach `want`
-      uint32_t lo = border, hi = top;
-      double above = 0;                  // weight of the keys > hi
-      while (lo < hi) {
-        const uint32_t mid = lo + (hi - lo) / 2;
-        const double m = mass(mid, hi);
-        if (above + m >= want) lo = mid + 1;
-        else { hi = mid; above += m; }
-      }
-      const int64_t ties = lo == border ? avail : count(lo - 1, lo);
-      double r = ceil((want - above) / weight(key_score(lo)));
-      r = r < 1.0 ? 1.0 : r;
-      border = lo;
-      take = r < (double)ties ? (int64_t)r : ties;
-    }
-    // each wave owns a range of classes; how many classes of the border's key
-    // come before it, then the weight it keeps
-    const int lane = threadIdx.x & 63;
-    const int wave = NW == 1 ? 0 : threadIdx.x >> 6;
-    const int64_t per = (p.C + NT - 1) / NT * 64;
-    const int64_t c0 = wave * per, c1 = c0 + per < p.C ? c0 + per : p.C;
-    int64_t t = 0;
-    for (int64_t c = c0 + lane; c < c1; c += 64) t += score_key(to_f32<T>(z[c])) == border ? 1 : 0;
-    t = block_reduce<1>(t, (int64_t*)nullptr, AddF());
-    int64_t rank = 0;
-    if constexpr (NW > 1) {
-      if (lane == 0) shi[wave] = t;
-      __syncthreads();
-      for (int i = 0; i < wave; ++i) rank += shi[i];
-      __syncthreads();
-    }
-    double run = 0, before = 0, total = 0;
-    int64_t last = -1;                   // last class kept in this wave's range
-    for (int pass = 0; pass < 2; ++pass) {
-      int64_t rk = rank;
-      double at = before;
-      for (int64_t b = c0; b < c1; b += 64) {
-        const int64_t c = b + lane;
-        const float v = c < c1 ? to_f32<T>(z[c]) : -INFINITY;
-        const uint32_t key = score_key(v);
-        const uint64_t tie = __ballot(c < c1 && key == border);
-        const int64_t my = rk + __popcll(tie & ((1ull << lane) - 1));
-        rk += __popcll(tie);
-        const double x = ((double)v - (double)zmax) / p.T;
-        const bool kept = c < c1 && (key > border || (key == border && my < take)) && x >= p.ln_min_p;
-        const double w = kept ? exp(x) : 0.0;
-        const double s = wave_scan(w);
-        if (pass == 0) {
-          const uint64_t k = __ballot(w > 0.0);
-          if (k) last = b + 63 - __clzll(k);
-        } else {
-          const uint64_t hit = __ballot(w > 0.0 && at + s > (double)u * total);
-          if (hit || (last >= b && last < b + 64)) {
-            const int64_t c = hit ? b + __ffsll((unsigned long long)hit) - 1 : last;
-            if (lane == (int)(c - b)) {
-              *label = (int32_t)c;
-              if (prob) *prob = (float)(w / total);
-            }
-            return;
-          }
-        }
-        at += __shfl(s, 63);
-      }
-      if (pass == 0) {
-        run = at;
-        total = run;
-        if constexpr (NW > 1) {
-          if (lane == 0) { shd[wave] = run; shi[wave] = last; }
-          __syncthreads();
-          total = 0;
-          int owner = -1, last_kept = 0;
-          for (int i = 0; i < NW; ++i) total += shd[i];
-          double acc = 0;
-          for (int i = 0; i < NW; ++i) {
-            if (shi[i] >= 0) last_kept = i;
-            if (owner < 0 && shi[i] >= 0 && acc + shd[i] > (double)u * total) owner = i;
-            if (i < wave) before += shd[i];
-            acc += shd[i];
-          }
-          if (owner < 0) owner = last_kept;
-          __syncthreads();
-          if (owner != wave) return;
-        }
-      }
-    }
-  }
-};
 
 // ------------------------------------------------ rows in lane groups ----
 //
@@ -366,36 +213,424 @@ __global__ __launch_bounds__(256) void sample_group_kernel(SampleParams p) {
   if (report) raise_flag(p.flag);
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void sample_exact_kernel(SampleParams p) {
-  __shared__ double shd[4];
-  __shared__ int64_t shi[4];
-  __shared__ uint32_t shu[4];
+// ---------------------------------------------------------- longer rows ----
+
+// A workgroup's row: whether it can be drawn from, else its answer is written.
+__device__ __forceinline__ bool row_answerable(const SampleParams& p, int64_t row, bool bad, float zmax) {
+  if (!bad && zmax > -INFINITY) return true;
+  if (threadIdx.x == 0) {
+    p.labels[row] = -1;
+    if (p.prob) p.prob[row] = 0.f;
+    if (bad) raise_flag(p.flag);
+  }
+  return false;
+}
+
+// top_k <= GCN_MAX_TOP: the first top_k items of the row are listed and put in
+// order (longrow.h); what follows concerns at most 256 numbers, all in 64 bits.
+template <typename T, int NT>
+__global__ __launch_bounds__(NT) void sample_top_kernel(SampleParams p) {
+  constexpr int NW = NT / 64;
+  __shared__ TopList<NT> sh;
+  __shared__ double s_item[GCN_MAX_TOP], s_w[GCN_MAX_TOP], s_d[NW];
+  __shared__ int s_cls[GCN_MAX_TOP];
   const int64_t row = blockIdx.x;
   if (p.mask && p.mask[row] == 0) return;
-  const T* __restrict__ z = reinterpret_cast<const T*>(p.logits) + row * p.ld;
-  float mx = -INFINITY;
-  bool bad = false;
-  for (int64_t c = threadIdx.x; c < p.C; c += 256) {
-    const float v = to_f32<T>(z[c]);
-    bad |= !(v < INFINITY);
-    mx = v > mx ? v : mx;
-  }
+  const int t = threadIdx.x;
+  const LongRow<T, NT> r(reinterpret_cast<const T*>(p.logits) + row * p.ld, (int)p.C);
   const float u = p.greedy ? 0.f : p.u[row];
+  const int K = (int)p.top_k;
+  float mx;
+  bool bad;
+  const int cnt = list_top(r, K, sh, mx, bad);
+  rank_list<NT>(sh, cnt, K, [&](int place, double e) { s_item[place] = e; });
+  const float zmax = block_reduce<NW>(mx, sh.b, MaxF());
   bad = __syncthreads_or(bad) || !(u >= 0.f && u < 1.f);
-  const float zmax = block_reduce<4>(mx, reinterpret_cast<float*>(shu), MaxF());
+  if (!row_answerable(p, row, bad, zmax)) return;
+  int m = cnt < K ? cnt : K;
+  // item t of the order; NT >= GCN_MAX_TOP
+  const float z = t < m ? key_score(item_key(Item64{s_item[t < m ? t : 0]})) : 0.f;
+  const int cls = t < m ? item_class(Item64{s_item[t < m ? t : 0]}) : 0;
+  const double w = t < m ? Draw<double>::weight(z, zmax, p) : 0.0;
+  if (t < m) s_w[t] = w;
+  if (p.top_p < 1.0) {
+    const double total = block_reduce<NW>(w, s_d, AddF());
+    double before = 0.0;
+    for (int j = 0; j < t && j < m; ++j) before += s_w[j];
+    m = block_reduce<NW>(t < m && before < p.top_p * total ? 1 : 0, sh.n, AddF());
+    m = m > 1 ? m : 1;
+  }
+  const bool kept = t < m && z >= least_kept(p, zmax);
+  const double wk = kept ? w : 0.0;
+  __syncthreads();
+  if (t < m) { s_w[t] = wk; s_cls[t] = cls; }
+  const double total = block_reduce<NW>(wk, s_d, AddF());
+  double run = 0.0;
+  if (wk > 0.0)
+    for (int j = 0; j < m; ++j) run += s_cls[j] <= cls ? s_w[j] : 0.0;
+  // the lowest class that passes, or the last one where rounding leaves none
+  const int first = block_reduce<NW>(wk > 0.0 && run > (double)u * total ? cls : INT32_MAX, sh.n, MinF());
+  const int last = block_reduce<NW>(wk > 0.0 ? cls : -1, sh.n, MaxF());
+  if (wk > 0.0 && cls == (first < last ? first : last)) {
+    p.labels[row] = cls;
+    if (p.prob) p.prob[row] = (float)(w / total);
+  }
+}
+
+// Other limits.  The classes kept are described by the last of them, the border
+// item, found by histograms in shared memory: the members of a range of scores
+// fall into 1024 bins by score, each with the sum of its members' weights; the
+// bin in which the running sum reaches what is wanted is the next range, until
+// its members are few enough to be compared with one another or all have the
+// same score.  The first histogram is linear in max - z, the next ones in the
+// key.  Then the classes are walked in their own order, a range of them a
+// wave.  For top_k the weights are 1.
+//
+// W = float: weights carry 2^-22 (the exponent in 64 bits, the base-2
+// exponential in 32: one unit in its last place and a rounding), sums are in 64
+// bits; where a running sum comes within LONG_EPS of its border the row is done
+// again with W = double.
+template <typename W> struct LongDraw;
+template <> struct LongDraw<float> {
+  static __device__ __forceinline__ double weight(float z, float zmax, const SampleParams& p) {
+    const double y = ((double)z - (double)zmax) * p.kd;
+    if (!(y > -140.0)) return 0.0;                       // below the smallest normal weight
+    const double n = rint(y);
+    return (double)ldexpf(__builtin_amdgcn_exp2f((float)(y - n)), (int)n);
+  }
+  static constexpr double EPS = 4.76837158203125e-7;     // 2^-21
+};
+template <> struct LongDraw<double> {
+  static __device__ __forceinline__ double weight(float z, float zmax, const SampleParams& p) {
+    return Draw<double>::weight(z, zmax, p);
+  }
+  static constexpr double EPS = 0.0;
+};
+
+constexpr int BINS = 1024, MEMBERS = 256;
+
+template <int NT>
+struct LongShared {
+  double bin[BINS];
+  double item[MEMBERS], weight[MEMBERS];
+  double d[NT / 64];
+  int64_t i64[NT / 64];
+  float f[NT / 64];
+  uint32_t u[NT / 64];
+  int n[NT / 64];
+  int count, hit;
+  double above, mass, border;
+};
+
+template <typename W, typename Row>
+struct LongSample {
+  typedef LongDraw<W> D;
+  static constexpr int VE = Row::VE;
+  static constexpr int NT = Row::NT;
+  static constexpr int NW = NT / 64;
+  const SampleParams& p;
+  const Row r;
+  LongShared<NT>& sh;
+  float zmax;
+
+  // The last bin that holds something and before which the running sum is
+  // below `want`: sh.hit, its start added to sh.above, its sum in sh.mass.
+  __device__ __forceinline__ void find_bin(double want) {
+    constexpr int PER = BINS / NT;
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    if (t == 0) sh.hit = -1;
+    double own[PER], sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) sum += own[i] = sh.bin[t * PER + i];
+    const double upto = wave_scan(sum);
+    if (lane == 63) sh.d[wave] = upto;
+    const double above = sh.above;
+    __syncthreads();
+    double run = __shfl_up(upto, 1);
+    if (lane == 0) run = 0.0;
+    for (int i = 0; i < wave; ++i) run += sh.d[i];
+    int held = -1;
+    double start = 0.0, mass = 0.0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      if (own[i] > 0.0 && above + run < want) { held = t * PER + i; start = run; mass = own[i]; }
+      run += own[i];
+    }
+    if (held >= 0) atomicMax(&sh.hit, held);
+    __syncthreads();
+    if (held >= 0 && held == sh.hit) { sh.above = above + start; sh.mass = mass; }
+    __syncthreads();
+  }
+
+  // Moves `border` to the last item that top_k (COUNT) or top_p keeps among
+  // the items from `border` on.  Returns whether that is certain.
+  template <bool COUNT>
+  __device__ __forceinline__ bool select(double& border, float zmin) {
+    const int t = threadIdx.x;
+    const double limit = border;
+    auto weight = [&](float z) -> double { return COUNT ? 1.0 : D::weight(z, zmax, p); };
+    auto inside = [&](float z, int c) { return z > -INFINITY && score_item(z, c).v >= limit; };
+    // Bins of the first histogram.  Under top_p they reach down to weights
+    // 2^-x0 = (1 - top_p) / (2 C): what lies below weighs less than
+    // (1 - top_p) / 2, the whole at least 1, so the border is never there.
+    float scale;
+    if (COUNT) {
+      const float range = zmax - zmin;
+      scale = range > 0.f && range < INFINITY ? (float)BINS / range : 0.f;
+      scale = scale < INFINITY ? scale : 0.f;
+    } else {
+      scale = p.k * ((float)BINS / (1.f + log2f((float)p.C) - log2f((float)(1.0 - p.top_p))));
+    }
+    auto bin1 = [&](float z) -> int {                    // BINS or more: below the bins
+      const float x = (zmax - z) * scale;
+      return COUNT ? (x < (float)BINS ? (int)x : BINS - 1) : x < (float)BINS ? (int)x : BINS;
+    };
+    for (int i = t; i < BINS; i += NT) sh.bin[i] = 0.0;
+    if (t == 0) sh.above = 0.0;
+    __syncthreads();
+    double rest = 0.0;
+    r.each([&](const float (&v)[VE], int c0, int nv) {
+#pragma unroll
+      for (int i = 0; i < VE; ++i) {
+        if (i >= nv || !inside(v[i], c0 + i)) continue;
+        const int b = bin1(v[i]);
+        const double w = weight(v[i]);
+        if (b < BINS) lds_add(&sh.bin[b], w);
+        else rest += w;
+      }
+    });
+    rest = block_reduce<NW>(rest, sh.d, AddF());
+    double want = (double)p.top_k, eps = 0.0;
+    if (!COUNT) {
+      double s = 0.0;
+      for (int i = t; i < BINS; i += NT) s += sh.bin[i];
+      const double total = block_reduce<NW>(s, sh.d, AddF()) + rest;
+      want = p.top_p * total;
+      eps = D::EPS * total;
+    }
+    uint32_t klo = 0, khi = 0;                           // the range of keys, from the first histogram on
+    int shift = -1;
+    for (;;) {
+      find_bin(want);
+      const int hit = sh.hit;
+      const double above = sh.above, mass = sh.mass;
+      // the members of the bin: how many, their keys, and the first MEMBERS
+      auto member = [&](float z, int c) {
+        if (!inside(z, c)) return false;
+        if (shift < 0) return bin1(z) == hit;
+        const uint32_t key = score_key(z);
+        return key >= klo && key <= khi && (int)((khi - key) >> shift) == hit;
+      };
+      if (t == 0) sh.count = 0;
+      __syncthreads();
+      uint32_t lo = 0xffffffffu, hi = 0;
+      r.each([&](const float (&v)[VE], int c0, int nv) {
+#pragma unroll
+        for (int i = 0; i < VE; ++i) {
+          if (i >= nv || !member(v[i], c0 + i)) continue;
+          const uint32_t key = score_key(v[i]);
+          lo = key < lo ? key : lo;
+          hi = key > hi ? key : hi;
+          const int at = atomicAdd(&sh.count, 1);
+          if (at < MEMBERS) { sh.item[at] = score_item(v[i], c0 + i).v; sh.weight[at] = weight(v[i]); }
+        }
+      });
+      lo = block_reduce<NW>(lo, sh.u, MinF());
+      hi = block_reduce<NW>(hi, sh.u, MaxF());
+      const int n = sh.count;
+      if (n <= MEMBERS) {
+        // a member is kept if what comes before it is below `want`
+        const double mine = t < n ? sh.item[t] : 0.0;
+        double before = above, least = 1.7e308, most = mine;
+        if (t < n)
+          for (int j = 0; j < n; ++j) before += sh.item[j] > mine ? sh.weight[j] : 0.0;
+        bool sure = true;
+        if (t < n && before < want) least = mine;
+        if (eps > 0.0 && t < n) sure = fabs(before - want) > eps && fabs(above + mass - want) > eps;
+        least = block_reduce<NW>(least, sh.d, MinF());
+        most = block_reduce<NW>(most, sh.d, MaxF());
+        border = least < 1e308 ? least : most;
+        return !__syncthreads_or(!sure);
+      }
+      if (lo == hi) {
+        // equal scores: the lowest `take` classes
+        const double w = weight(key_score(lo));
+        const double q = (want - above) / w;
+        double take = ceil(q);
+        take = take < 1.0 ? 1.0 : take > (double)n ? (double)n : take;
+        const bool sure = eps == 0.0 || fabs(q - rint(q)) * w > eps;
+        int a = 0, b = r.C - 1;                          // the class up to which they are `take`
+        while (a < b) {
+          const int mid = a + (b - a) / 2;
+          int m = 0;
+          r.each([&](const float (&v)[VE], int c0, int nv) {
+#pragma unroll
+            for (int i = 0; i < VE; ++i)
+              m += i < nv && c0 + i <= mid && inside(v[i], c0 + i) && score_key(v[i]) == lo ? 1 : 0;
+          });
+          m = block_reduce<NW>(m, sh.n, AddF());
+          if ((double)m >= take) b = mid;
+          else a = mid + 1;
+        }
+        border = item64(lo, (uint32_t)a).v;
+        return sure;
+      }
+      // the next histogram, of the members' keys
+      klo = lo;
+      khi = hi;
+      shift = 0;
+      while ((hi - lo) >> shift >= (uint32_t)BINS) ++shift;
+      for (int i = t; i < BINS; i += NT) sh.bin[i] = 0.0;
+      __syncthreads();
+      r.each([&](const float (&v)[VE], int c0, int nv) {
+#pragma unroll
+        for (int i = 0; i < VE; ++i) {
+          if (i >= nv || !inside(v[i], c0 + i)) continue;
+          const uint32_t key = score_key(v[i]);
+          if (key >= klo && key <= khi) lds_add(&sh.bin[(khi - key) >> shift], weight(v[i]));
+        }
+      });
+      __syncthreads();
+    }
+  }
+
+  // The draw among the items from `border` on that min-p keeps.
+  __device__ __forceinline__ bool draw(double border, float u, int32_t* label, float* prob) {
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const float least = least_kept(p, zmax);
+    const float zb = key_score(item_key(Item64{border}));
+    const int cb = item_class(Item64{border});
+    auto weight = [&](float z, int c) -> double {
+      return (z > zb || (z == zb && c <= cb)) && z >= least && z > -INFINITY ? D::weight(z, zmax, p) : 0.0;
+    };
+    double sum = 0.0;
+    int last = -1;
+    r.each([&](const float (&v)[VE], int c0, int nv) {
+#pragma unroll
+      for (int i = 0; i < VE; ++i) {
+        const double w = i < nv ? weight(v[i], c0 + i) : 0.0;
+        sum += w;
+        last = w > 0.0 ? c0 + i : last;
+      }
+    });
+    sum = block_reduce<1>(sum, (double*)nullptr, AddF());
+    last = block_reduce<1>(last, (int*)nullptr, MaxF());
+    if (lane == 0) { sh.d[wave] = sum; sh.n[wave] = last; }
+    __syncthreads();
+    double total = 0.0, run = 0.0;
+    for (int i = 0; i < NW; ++i) total += sh.d[i];
+    const double want = (double)u * total;
+    int owner = -1, fallback = 0;
+    double before = 0.0;
+    for (int i = 0; i < NW; ++i) {
+      if (sh.n[i] >= 0) fallback = i;
+      if (owner < 0 && sh.n[i] >= 0 && run + sh.d[i] > want) { owner = i; before = run; }
+      run += sh.d[i];
+    }
+    const bool none = owner < 0;                         // rounding: the last class kept
+    if (none) owner = fallback;
+    bool sure = true;
+    if (t == 0) sh.hit = 1;
+    __syncthreads();
+    if (wave == owner) {
+      const double eps = D::EPS * total;
+      int at = none ? sh.n[owner] : -1;
+      double w_at = 0.0;
+      bool done = false;
+      r.template each<true>([&](const float (&v)[VE], int c0, int nv) {
+        // every lane comes here for every vector of the wave; done and before are the wave's
+        if (done) return;
+        double w[VE], own = 0.0;
+#pragma unroll
+        for (int i = 0; i < VE; ++i) own += w[i] = i < nv ? weight(v[i], c0 + i) : 0.0;
+        const double upto = wave_scan(own);
+        double x = __shfl_up(upto, 1);
+        x = before + (lane == 0 ? 0.0 : x);
+        bool here = false;
+        if (none) {
+          here = at >= c0 && at < c0 + nv;
+        } else {
+          const uint64_t hits = __ballot(own > 0.0 && before + upto > want);
+          here = hits && lane == __ffsll((unsigned long long)hits) - 1;
+        }
+        // the class in this lane: its sum passes `want` (the lane's last kept one
+        // where the order of additions leaves none)
+        if (here) {
+          int c = -1, kept = -1;
+          double wc = 0.0, wl = 0.0;
+#pragma unroll
+          for (int i = 0; i < VE; ++i) {
+            if (w[i] > 0.0) {
+              const double y = x + w[i];
+              if (c < 0 && (none ? c0 + i == at : y > want)) {
+                c = c0 + i;
+                wc = w[i];
+                if (eps > 0.0) sure = fabs(x - want) > eps && fabs(y - want) > eps;
+              }
+              x = y;
+              kept = c0 + i;
+              wl = w[i];
+            }
+          }
+          at = c >= 0 ? c : kept;
+          w_at = c >= 0 ? wc : wl;
+          if (sure) {
+            *label = at;
+            if (prob) *prob = (float)(w_at / total);
+          } else {
+            sh.hit = 0;
+          }
+        }
+        done = __ballot(here) != 0;
+        before += __shfl(upto, 63);
+      });
+      // sums of the walk and of the wave may differ by a rounding
+      if (!done && lane == 0) {
+        *label = sh.n[owner];
+        if (prob) *prob = (float)(D::weight(to_f32<typename Row::Elem>(r.z[sh.n[owner]]), zmax, p) / total);
+      }
+    }
+    __syncthreads();
+    return sh.hit != 0;
+  }
+
+  __device__ __forceinline__ bool run(float u, float zmin, int32_t* label, float* prob) {
+    double border = item64(KEY_NEG_INF + 1, 0x3fffffff).v;   // every score's item is above
+    bool sure = true;
+    if (p.top_k < p.C) sure &= select<true>(border, zmin);
+    if (p.top_p < 1.0) sure &= select<false>(border, zmin);
+    return sure && draw(border, u, label, prob);
+  }
+};
+
+template <typename T, int NT>
+__global__ __launch_bounds__(NT) void sample_row_kernel(SampleParams p) {
+  typedef LongRow<T, NT, true> Row;
+  constexpr int NW = NT / 64;
+  __shared__ LongShared<NT> sh;
+  const int64_t row = blockIdx.x;
+  if (p.mask && p.mask[row] == 0) return;
+  const Row r(reinterpret_cast<const T*>(p.logits) + row * p.ld, (int)p.C);
+  const float u = p.u[row];
+  float mx = -INFINITY, mn = INFINITY;
+  bool bad = false;
+  r.each([&](const float (&v)[Row::VE], int, int nv) {
+#pragma unroll
+    for (int i = 0; i < Row::VE; ++i) {
+      const bool here = i < nv;
+      bad |= here && !(v[i] < INFINITY);
+      mx = here && v[i] > mx ? v[i] : mx;
+      mn = here && v[i] < mn && v[i] > -INFINITY ? v[i] : mn;
+    }
+  });
+  bad = __syncthreads_or(bad) || !(u >= 0.f && u < 1.f);
+  const float zmax = block_reduce<NW>(mx, sh.f, MaxF());
+  const float zmin = block_reduce<NW>(mn, sh.f, MinF());
+  if (!row_answerable(p, row, bad, zmax)) return;
   int32_t* label = p.labels + row;
   float* prob = p.prob ? p.prob + row : nullptr;
-  if (bad || zmax == -INFINITY) {
-    if (threadIdx.x == 0) {
-      *label = -1;
-      if (prob) *prob = 0.f;
-      if (bad) raise_flag(p.flag);
-    }
-    return;
-  }
-  ExactRow<T, 4> r{p, z, shd, shi, shu, zmax};
-  r.draw(u, label, prob);
+  if (LongSample<float, Row>{p, r, sh, zmax}.run(u, zmin, label, prob)) return;
+  LongSample<double, Row>{p, r, sh, zmax}.run(u, zmin, label, prob);
 }
 
 // ------------------------------------------------------------- launches ----
@@ -419,6 +654,19 @@ hipError_t launch_lpr(const SampleParams& p, hipStream_t s) {
   return p.top_k < p.C || p.top_p < 1.0 ? launch_filter<T, LPR, true>(p, s) : launch_filter<T, LPR, false>(p, s);
 }
 template <typename T>
+hipError_t launch_rows(const SampleParams& p, hipStream_t s) {
+  const int64_t nvec = (p.C + Vec<T>::N - 1) / Vec<T>::N;
+  const dim3 grid((unsigned)p.n);
+  if (p.top_k <= GCN_MAX_TOP) {
+    if (nvec <= 8 * 256 && p.top_k <= 32) hipLaunchKernelGGL((sample_top_kernel<T, 256>), grid, dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((sample_top_kernel<T, 1024>), grid, dim3(1024), 0, s, p);
+  } else {
+    if (nvec <= 8 * 256) hipLaunchKernelGGL((sample_row_kernel<T, 256>), grid, dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((sample_row_kernel<T, 1024>), grid, dim3(1024), 0, s, p);
+  }
+  return hipGetLastError();
+}
+template <typename T>
 hipError_t launch_t(const SampleParams& p, hipStream_t s) {
   const int64_t nvec = (p.C + Vec<T>::N - 1) / Vec<T>::N;
   if (nvec <= 1) return launch_lpr<T, 1>(p, s);
@@ -428,8 +676,7 @@ hipError_t launch_t(const SampleParams& p, hipStream_t s) {
   if (nvec <= 16) return launch_lpr<T, 16>(p, s);
   if (nvec <= 32) return launch_lpr<T, 32>(p, s);
   if (nvec <= 64) return launch_lpr<T, 64>(p, s);
-  hipLaunchKernelGGL((sample_exact_kernel<T>), dim3((unsigned)p.n), dim3(256), 0, s, p);
-  return hipGetLastError();
+  return launch_rows<T>(p, s);
 }
 
 }  // namespace

@@ -7,6 +7,7 @@
 #include <algorithm>
 
 #include "internal.h"
+#include "longrow.h"
 #include "sorted.h"
 
 namespace gcn {
@@ -116,161 +117,20 @@ __global__ __launch_bounds__(256) void top_group_kernel(TopParams p) {
   if (bad) raise_flag(p.flag);
 }
 
-// Longer rows: a workgroup of NT threads takes a row and holds it in its
-// registers, NV vectors a thread (NV = 0: the row is read again from the
-// caches whenever it is needed).
-//   1. Every thread finds the largest of its scores.
-//   2. In each wave the r-th largest of these, r = ceil(K / waves), is a score
-//      that r classes of the wave reach; the smallest over the waves, b, is one
-//      that at least K classes of the row reach.  (Only waves whose lanes all
-//      hold scores are asked.)
-//   3. The classes that reach b are listed in shared memory: for scores in no
-//      particular order a few times K.  Where they are too many (rows sorted by
-//      class, many equal scores), b is raised by bisection between what K
-//      items reach and what fewer do, until the list holds them.
-//   4. An entry's place is the number of listed items above it.
-constexpr int TOP_LIST = 1024;
-
-template <typename T, int NT, int NV>
-struct TopRow {
-  static constexpr int VE = Vec<T>::N;
-  static constexpr int NW = NT / 64;
-  const T* __restrict__ z;
-  int C;
-  uint4 raw[NV > 0 ? NV : 1];
-
-  // f(vector, first class, classes of it in the row) over this thread's vectors
-  template <typename F>
-  __device__ __forceinline__ void each(F f) const {
-    if constexpr (NV > 0) {
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        const int c0 = (v * NT + (int)threadIdx.x) * VE;
-        if (c0 < C) f(raw[v], c0, C - c0 < VE ? C - c0 : VE);
-      }
-    } else {
-      for (int c0 = (int)threadIdx.x * VE; c0 < C; c0 += NT * VE)
-        f(ldg16(z + c0), c0, C - c0 < VE ? C - c0 : VE);
-    }
-  }
-  __device__ __forceinline__ void load() {
-    if constexpr (NV > 0) {
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        const int c0 = (v * NT + (int)threadIdx.x) * VE;
-        raw[v] = ldg16(z + (c0 < C ? c0 : 0));
-      }
-    }
-  }
-};
-
-// A score's item with 64 bits, whatever its type.
-__device__ __forceinline__ Item64 score_item(float v, int c) { return item64(score_key(v), (uint32_t)c); }
-
-template <typename T, int NT, int NV>
+// Longer rows: a workgroup lists what reaches a bound (longrow.h) and counts
+// every listed item into its place.
+template <typename T, int NT>
 __global__ __launch_bounds__(NT) void top_row_kernel(TopParams p) {
-  constexpr int VE = Vec<T>::N;
-  constexpr int NW = NT / 64;
-  __shared__ float sh_b[NW];
-  __shared__ int sh_n[NW];
-  __shared__ int s_count;
-  __shared__ double s_list[TOP_LIST];
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  __shared__ TopList<NT> sh;
   const int64_t row = blockIdx.x;
-  TopRow<T, NT, NV> r;
-  r.z = reinterpret_cast<const T*>(p.logits) + row * p.ld;
-  r.C = (int)p.C;
-  r.load();
-  if (t == 0) s_count = 0;
-  bool bad = false;
-  float mx = -INFINITY;
-  r.each([&](uint4 raw, int, int nv) {
-    float v[VE];
-    unpack<T>(raw, v);
-#pragma unroll
-    for (int i = 0; i < VE; ++i) {
-      const bool here = i < nv;
-      bad |= here && !(v[i] < INFINITY);
-      mx = here && v[i] > mx ? v[i] : mx;
-    }
-  });
-  if (bad) raise_flag(p.flag);
-  // the r-th largest of the wave's 64 maxima, or -inf
+  const LongRow<T, NT> r(reinterpret_cast<const T*>(p.logits) + row * p.ld, (int)p.C);
   const int K = (int)p.K;
-  const int full = r.C / (64 * VE) < NW ? r.C / (64 * VE) : NW;   // at least 1: shorter rows have a lane group
-  const int rounds = (K + full - 1) / full;
-  float left = mx, b = -INFINITY;
-  if (rounds <= 64) {
-    for (int i = 0; i < rounds; ++i) {
-      b = group_max<64>(left);
-      const uint64_t who = __ballot(left == b);
-      if (lane == __ffsll((unsigned long long)who) - 1) left = -INFINITY;
-    }
-  }
-  if (lane == 0) sh_b[wave] = b;
-  __syncthreads();
-  b = sh_b[0];
-  for (int i = 1; i < full; ++i) b = fminf(b, sh_b[i]);
-  // list what reaches b (all finite scores if b is -inf)
-  auto list = [&](double from) {
-    r.each([&](uint4 raw, int c0, int nv) {
-      float v[VE];
-      unpack<T>(raw, v);
-      bool any = false;
-#pragma unroll
-      for (int i = 0; i < VE; ++i) any |= v[i] >= b && v[i] > -INFINITY && i < nv;
-      if (!any) return;
-#pragma unroll
-      for (int i = 0; i < VE; ++i) {
-        if (!(v[i] >= b && v[i] > -INFINITY) || i >= nv) continue;
-        const Item64 e = score_item(v[i], c0 + i);
-        if (e.v < from) continue;
-        const int at = atomicAdd(&s_count, 1);
-        if (at < TOP_LIST) s_list[at] = e.v;
-      }
-    });
-  };
-  list(0.0);
-  __syncthreads();
-  int cnt = s_count;
-  if (cnt > TOP_LIST) {
-    // items from `from` on are K at least and, at the end, TOP_LIST at most
-    uint64_t lo = (uint64_t)__double_as_longlong(score_item(b > -INFINITY ? b : -3.402823466e38f, 0x3fffffff).v);
-    uint64_t hi = (uint64_t)__double_as_longlong(item64(0xffffffffu, 0).v);
-    if (b == -INFINITY) lo = 0;
-    while (cnt > TOP_LIST) {
-      const uint64_t mid = lo + (hi - lo) / 2 + 1;
-      const double m = __longlong_as_double((long long)mid);
-      int n = 0;
-      r.each([&](uint4 raw, int c0, int nv) {
-        float v[VE];
-        unpack<T>(raw, v);
-#pragma unroll
-        for (int i = 0; i < VE; ++i)
-          if (i < nv && v[i] >= b && v[i] > -INFINITY) n += score_item(v[i], c0 + i).v >= m ? 1 : 0;
-      });
-      n = block_reduce<NW>(n, sh_n, AddF());
-      if (n >= K) { lo = mid; cnt = n; }
-      else hi = mid - 1;
-    }
-    if (t == 0) s_count = 0;
-    __syncthreads();
-    list(__longlong_as_double((long long)lo));
-    __syncthreads();
-    cnt = s_count;
-  }
-  // places: several threads count for one item where the list is short
-  int per = 1;
-  while (per < 64 && 2 * per * cnt <= NT) per *= 2;
-  const int sub = t % per;
-  for (int i = t / per; i < cnt; i += NT / per) {
-    const double e = s_list[i];
-    int above = 0;
-    for (int j = sub; j < cnt; j += per) above += s_list[j] > e ? 1 : 0;
-    for (int m = 1; m < per; m <<= 1) above += __shfl_xor(above, m);
-    if (sub == 0 && above < K) put_entry<T>(p, row, above, Item64{e});
-  }
-  for (int j = cnt + t; j < K; j += NT) put_entry<T>(p, row, j, Item64{0.0});
+  float mx;
+  bool bad;
+  const int cnt = list_top(r, K, sh, mx, bad);
+  if (bad) raise_flag(p.flag);
+  rank_list<NT>(sh, cnt, K, [&](int place, double e) { put_entry<T>(p, row, place, Item64{e}); });
+  for (int j = cnt + (int)threadIdx.x; j < K; j += NT) put_entry<T>(p, row, j, Item64{0.0});
 }
 
 // ------------------------------------------------------------- launches ----
@@ -302,10 +162,9 @@ hipError_t launch_rows(const TopParams& p, hipStream_t s) {
   const int64_t nvec = (p.C + Vec<T>::N - 1) / Vec<T>::N;
   const dim3 grid((unsigned)p.n);
   // the bound of step 2 is close where K is small against the threads
-  if (nvec <= 8 * 256 && p.K <= 32) hipLaunchKernelGGL((top_row_kernel<T, 256, 8>), grid, dim3(256), 0, s, p);
-  else if (nvec <= 8 * 512 && p.K <= 64) hipLaunchKernelGGL((top_row_kernel<T, 512, 8>), grid, dim3(512), 0, s, p);
-  else if (nvec <= 8 * 1024) hipLaunchKernelGGL((top_row_kernel<T, 1024, 8>), grid, dim3(1024), 0, s, p);
-  else hipLaunchKernelGGL((top_row_kernel<T, 1024, 0>), grid, dim3(1024), 0, s, p);
+  if (nvec <= 8 * 256 && p.K <= 32) hipLaunchKernelGGL((top_row_kernel<T, 256>), grid, dim3(256), 0, s, p);
+  else if (nvec <= 8 * 512 && p.K <= 64) hipLaunchKernelGGL((top_row_kernel<T, 512>), grid, dim3(512), 0, s, p);
+  else hipLaunchKernelGGL((top_row_kernel<T, 1024>), grid, dim3(1024), 0, s, p);
   return hipGetLastError();
 }
 template <typename T>
