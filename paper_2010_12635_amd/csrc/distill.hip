@@ -226,86 +226,318 @@ __global__ __launch_bounds__(256) void distill_group_kernel(DistillParams p) {
   }
 }
 
-// A workgroup owns a row; entry j belongs to thread j.
+// ---------------------------------------------------------- longer rows ----
+//
+// distill_row_kernel: a workgroup owns a row and holds it in its registers (NV
+// vectors a thread): one read, one write.  The teacher's side is done by every
+// wave for itself while the row is on its way, lane l holding the entries l, l
+// + 64, ...; thread j then owns entry j, whose class it writes after the row.
+//
+// distill_part_kernel and distill_segment_kernel: rows that do not fit, and
+// rows too few to fill the chip, are cut into segments of `seg` vectors, a
+// workgroup each: first every segment's maximum and sum of exponentials, then,
+// from those of the whole row, its part of the gradient.
+
+// A maximum and a sum of exponentials relative to it (0 where it is -inf).
+struct MaxSum { float m, s; };
+__device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b, float k) {
+  const float m = fmaxf(a.m, b.m);
+  const float fa = a.m > -INFINITY ? __builtin_amdgcn_exp2f((a.m - m) * k) : 0.f;
+  const float fb = b.m > -INFINITY ? __builtin_amdgcn_exp2f((b.m - m) * k) : 0.f;
+  return {m, a.s * fa + b.s * fb};                   // a NaN stays in s
+}
+__device__ __forceinline__ MaxSum wave_join(MaxSum v, float k) {
+  const float m = group_max<64>(v.m);
+  v.s *= v.m > -INFINITY ? __builtin_amdgcn_exp2f((v.m - m) * k) : 0.f;
+  return {m, group_sum<64>(v.s)};
+}
 template <typename T>
-__global__ __launch_bounds__(256) void distill_row_kernel(DistillParams p) {
-  __shared__ float shf[4];
-  __shared__ int32_t s_cls[GCN_MAX_TOP];
-  __shared__ float s_q[GCN_MAX_TOP];
+__device__ __forceinline__ float vector_max(const float (&v)[Vec<T>::N], int nv) {
+  float m = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < Vec<T>::N; ++i) m = fmaxf(m, i < nv ? v[i] : -INFINITY);
+  return m;
+}
+template <typename T>
+__device__ __forceinline__ float vector_sum(const float (&v)[Vec<T>::N], int nv, float m, float k) {
+  const float mm = m > -INFINITY ? m : 0.f;          // a row of -inf alone: 0 each
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < Vec<T>::N; ++i) s += i < nv ? __builtin_amdgcn_exp2f((v[i] - mm) * k) : 0.f;
+  return s;
+}
+
+// The teacher's entries of a row, of which a wave holds all: entry q 64 + lane
+// in element q.
+constexpr int TQ = GCN_MAX_TOP / 64;
+template <typename T>
+struct Entries {
+  int32_t c[TQ];
+  float t[TQ], z[TQ];      // the teacher's score, and the student's for the class
+  float q[TQ], y[TQ];      // weight, and (t - max t) / T
+  float ln_r;
+  bool counts, bad;
+
+  __device__ __forceinline__ void load(const DistillParams& p, int64_t row, const T* __restrict__ zrow) {
+    const int lane = threadIdx.x & 63;
+    const bool in = !p.mask || p.mask[row] != 0;
+    bad = false;
+    bool some = false;
+#pragma unroll
+    for (int i = 0; i < TQ; ++i) {
+      const int j = i * 64 + lane;
+      c[i] = -1;
+      t[i] = -INFINITY;
+      z[i] = 0.f;
+      if (in && j < p.K) {
+        c[i] = p.top_classes[row * p.ld_top + j];
+        t[i] = load_as_f32(p.top_prec, p.top_values, row * p.ld_top + j);
+        if (c[i] >= p.C) bad = true;
+        if (c[i] < 0 || c[i] >= p.C || t[i] == -INFINITY) { c[i] = -1; t[i] = -INFINITY; }
+        if (c[i] >= 0) z[i] = to_f32<T>(zrow[c[i]]);
+      }
+      some |= c[i] >= 0;
+    }
+    counts = __ballot(some) != 0;
+  }
+  __device__ __forceinline__ void weigh(const DistillParams& p, float k) {
+    float m = t[0];
+#pragma unroll
+    for (int i = 1; i < TQ; ++i) m = fmaxf(m, t[i]);
+    m = group_max<64>(m);
+    float r = 0.f;
+#pragma unroll
+    for (int i = 0; i < TQ; ++i) {
+      y[i] = c[i] >= 0 ? (t[i] - m) * p.inv_T : 0.f;
+      q[i] = c[i] >= 0 ? __builtin_amdgcn_exp2f((t[i] - m) * k) : 0.f;
+      r += q[i];
+    }
+    r = group_sum<64>(r);
+    const float inv = 1.f / r;
+#pragma unroll
+    for (int i = 0; i < TQ; ++i) q[i] *= inv;
+    ln_r = logf(r);
+  }
+  // sum of q (y - x): an entry of weight 0 adds nothing
+  __device__ __forceinline__ float loss(const DistillParams& p, MaxSum row) const {
+    float a = 0.f;
+#pragma unroll
+    for (int i = 0; i < TQ; ++i)
+      a += q[i] > 0.f || q[i] != q[i] ? q[i] * (y[i] - (z[i] - row.m) * p.inv_T) : 0.f;
+    return group_sum<64>(a) - ln_r + logf(row.s);
+  }
+};
+
+// Shared by the kernels that write gradients: the row's entries by number.
+struct EntryTable {
+  int32_t c[GCN_MAX_TOP];
+  float q[GCN_MAX_TOP];
+};
+
+template <typename T>
+__device__ __forceinline__ bool store_gradient(const DistillParams& p, T* d, const T* base, int c0, int nv,
+                                               const float (&v)[Vec<T>::N], float m, float k, float f) {
+  constexpr int VE = Vec<T>::N;
+  float g[VE], bv[VE];
+  if (base) unpack<T>(ldg16(base + c0), bv);
+#pragma unroll
+  for (int i = 0; i < VE; ++i) {
+    g[i] = f != 0.f || f != f ? __builtin_amdgcn_exp2f((v[i] - m) * k) * f : 0.f;   // f = 0: not a counted row
+    if (base) g[i] += bv[i];
+    g[i] = i < nv ? g[i] : 0.f;
+  }
+  const uint4 o = pack<T>(g);
+  stg16(d + c0, o);
+  return packed_nonfinite<T>(o);
+}
+
+// Thread t's entry, if its class lies in [lo, hi): what its class gets, to be
+// written after the row.
+template <typename T>
+struct OwnEntry {
+  int c;
+  float z, base;
+  __device__ __forceinline__ void take(const Entries<T>& e, const T* base_row, int lo, int hi) {
+    const int wave = threadIdx.x >> 6;
+    c = -1;
+    z = 0.f;
+    base = 0.f;
+#pragma unroll
+    for (int i = 0; i < TQ; ++i)
+      if (i == wave) { c = e.c[i]; z = e.z[i]; }
+    if (c < lo || c >= hi) c = -1;
+    if (c >= 0 && base_row) base = to_f32<T>(base_row[c]);
+  }
+  __device__ __forceinline__ bool store(const DistillParams& p, const EntryTable& tab, T* d, float m, float k, float inv_s,
+                                        float sc) const {
+    if (c < 0) return false;
+    float qs = 0.f;
+    for (int j = 0; j < p.K; ++j) qs += tab.c[j] == c ? tab.q[j] : 0.f;
+    const T o = from_f32<T>((__builtin_amdgcn_exp2f((z - m) * k) * inv_s - qs) * sc + base);
+    d[c] = o;
+    return !finite_f32(to_f32<T>(o));
+  }
+};
+
+template <typename T, int NT, int NV>
+__global__ __launch_bounds__(NT) void distill_row_kernel(DistillParams p) {
+  constexpr int VE = Vec<T>::N;
+  constexpr int NW = NT / 64;
+  __shared__ MaxSum s_part[NW];
+  __shared__ EntryTable s_tab;
   const int64_t row = blockIdx.x;
-  const int t = threadIdx.x;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int C = (int)p.C;
   const T* __restrict__ z = reinterpret_cast<const T*>(p.logits) + row * p.ld;
   const T* base = p.base ? reinterpret_cast<const T*>(p.base) + row * p.ld : nullptr;
   T* d = p.dlogits ? reinterpret_cast<T*>(p.dlogits) + row * p.ld : nullptr;
   const float k = LOG2E * p.inv_T;
-  // the teacher's entries: one a thread
-  int32_t cls = -1;
-  float tv = -INFINITY;
-  const bool in_mask = !p.mask || p.mask[row] != 0;
-  bool bad = false;
-  if (in_mask && t < p.K) {
-    cls = p.top_classes[row * p.ld_top + t];
-    if (cls >= p.C) { cls = -1; bad = true; }
-    if (cls >= 0) tv = load_as_f32(p.top_prec, p.top_values, row * p.ld_top + t);
-    if (tv == -INFINITY) cls = -1;
+  uint4 raw[NV];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int c0 = (v * NT + t) * VE;
+    raw[v] = ldg16(z + (c0 < C ? c0 : 0));
   }
-  const float tmax = block_reduce<4>(cls >= 0 ? tv : -INFINITY, shf, MaxF());
-  const int any = __syncthreads_or(cls >= 0);
-  if (!any) {                                        // nothing to learn from: the gradient is the base
-    if (d)
-      for (int64_t c = t; c < p.C; c += 256) d[c] = base ? base[c] : from_f32<T>(0.f);
-    if (t == 0) p.part_loss[row] = 0.f;
-    if (bad) raise_flag(p.flag);
-    return;
+  Entries<T> e;
+  e.load(p, row, z);
+  e.weigh(p, k);
+  if (wave < TQ) {
+#pragma unroll
+    for (int i = 0; i < TQ; ++i)
+      if (i == wave) { s_tab.c[t] = e.c[i]; s_tab.q[t] = e.q[i]; }
   }
-  const float y = cls >= 0 ? (tv - tmax) * p.inv_T : 0.f;
-  const float ey = cls >= 0 ? __builtin_amdgcn_exp2f((tv - tmax) * k) : 0.f;
-  const float r = block_reduce<4>(ey, shf, AddF());
-  const float q = ey / r;
-  if (t < p.K) { s_cls[t] = cls; s_q[t] = q; }
-  float mx = -INFINITY;
-  for (int64_t c = t; c < p.C; c += 256) {
-    const float v = to_f32<T>(z[c]);
-    mx = v > mx || v != v ? v : mx;
+  OwnEntry<T> own;
+  own.take(e, base, 0, C);
+  MaxSum mine{-INFINITY, 0.f};
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int c0 = (v * NT + t) * VE;
+    float x[VE];
+    unpack<T>(raw[v], x);
+    mine.m = fmaxf(mine.m, vector_max<T>(x, C - c0));
   }
-  if (__syncthreads_or(mx != mx)) mx = NAN;
-  mx = block_reduce<4>(mx, shf, MaxF());
-  float se = 0.f;
-  for (int64_t c = t; c < p.C; c += 256) se += __builtin_amdgcn_exp2f((to_f32<T>(z[c]) - mx) * k);
-  se = block_reduce<4>(se, shf, AddF());
-  // q (y - x) of this thread's entry; an entry of weight 0 adds nothing
-  float zc = cls >= 0 ? to_f32<T>(z[cls]) : 0.f;
-  const float kl_j = q > 0.f || q != q ? q * (y - (zc - mx) * p.inv_T) : 0.f;
-  const float kl = block_reduce<4>(kl_j, shf, AddF()) - logf(r) + logf(se);
-  if (t == 0) p.part_loss[row] = kl;
-  if (!d) {
-    if (bad) raise_flag(p.flag);
-    return;
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int c0 = (v * NT + t) * VE;
+    float x[VE];
+    unpack<T>(raw[v], x);
+    mine.s += vector_sum<T>(x, C - c0, mine.m, k);
   }
-  const float sc = p.scale * (p.loss_scale ? *p.loss_scale : 1.f);
-  const float inv_se = 1.f / se;
-  // the entry's own element, read before the row is written over (the base
-  // may be the gradient's buffer)
-  float own = 0.f;
-  if (cls >= 0) {
-    float qs = 0.f;
-    for (int j = 0; j < p.K; ++j) qs += s_cls[j] == cls ? s_q[j] : 0.f;
-    own = (__builtin_amdgcn_exp2f((zc - mx) * k) * inv_se - qs) * sc;
-    if (base) own += to_f32<T>(base[cls]);
-  }
+  mine = wave_join(mine, k);
+  if (lane == 0) s_part[wave] = mine;
   __syncthreads();
-  for (int64_t c = t; c < p.C; c += 256) {
-    float g = __builtin_amdgcn_exp2f((to_f32<T>(z[c]) - mx) * k) * inv_se * sc;
-    if (base) g += to_f32<T>(base[c]);
-    const T o = from_f32<T>(g);
-    d[c] = o;
-    bad |= !finite_f32(to_f32<T>(o));
+  MaxSum all = s_part[0];
+#pragma unroll
+  for (int i = 1; i < NW; ++i) all = join(all, s_part[i], k);
+  if (wave == 0) {
+    const float kl = e.loss(p, all);
+    if (t == 0) p.part_loss[row] = e.counts ? kl : 0.f;
   }
+  bool bad = e.bad;
+  if (d) {
+    const float sc = e.counts ? p.scale * (p.loss_scale ? *p.loss_scale : 1.f) : 0.f;
+    const float inv_s = 1.f / all.s;
+    const float f = e.counts ? inv_s * sc : 0.f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int c0 = (v * NT + t) * VE;
+      float x[VE];
+      unpack<T>(raw[v], x);
+      if (c0 < C) bad |= store_gradient<T>(p, d, base, c0, C - c0, x, all.m, k, f);
+    }
+    __syncthreads();                                 // the row is written
+    bad |= own.store(p, s_tab, d, all.m, k, inv_s, sc);
+  }
+  if (bad) raise_flag(p.flag);
+}
+
+// Segments: workgroup (row, s) = (blockIdx.x / segs, blockIdx.x % segs).
+template <typename T>
+__global__ __launch_bounds__(256) void distill_part_kernel(DistillParams p) {
+  constexpr int VE = Vec<T>::N;
+  __shared__ MaxSum s_part[4];
+  const int64_t row = blockIdx.x / p.segs;
+  const int t = threadIdx.x;
+  const int C = (int)p.C;
+  const int lo = (int)(blockIdx.x % p.segs) * p.seg, hi = lo + p.seg < (C + VE - 1) / VE ? lo + p.seg : (C + VE - 1) / VE;
+  const T* __restrict__ z = reinterpret_cast<const T*>(p.logits) + row * p.ld;
+  const float k = LOG2E * p.inv_T;
+  MaxSum mine{-INFINITY, 0.f};
+  for (int b = lo + t; b < hi; b += 4 * 256) {
+    uint4 raw[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) raw[q] = ldg16(z + (int64_t)(b + q * 256 < hi ? b + q * 256 : lo) * VE);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int nv = b + q * 256 < hi ? C - (b + q * 256) * VE : 0;
+      float x[VE];
+      unpack<T>(raw[q], x);
+      const float m = fmaxf(mine.m, vector_max<T>(x, nv));
+      mine.s *= mine.m > -INFINITY ? __builtin_amdgcn_exp2f((mine.m - m) * k) : 0.f;
+      mine.m = m;
+      mine.s += vector_sum<T>(x, nv, m, k);
+    }
+  }
+  mine = wave_join(mine, k);
+  if ((t & 63) == 0) s_part[t >> 6] = mine;
   __syncthreads();
-  if (cls >= 0) {
-    const T o = from_f32<T>(own);
-    d[cls] = o;
-    bad |= !finite_f32(to_f32<T>(o));
+  if (t == 0) {
+    MaxSum a = s_part[0];
+    for (int i = 1; i < 4; ++i) a = join(a, s_part[i], k);
+    reinterpret_cast<MaxSum*>(p.part_ms)[blockIdx.x] = a;
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void distill_segment_kernel(DistillParams p) {
+  constexpr int VE = Vec<T>::N;
+  __shared__ EntryTable s_tab;
+  const int64_t row = blockIdx.x / p.segs;
+  const int s = (int)(blockIdx.x % p.segs);
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int C = (int)p.C;
+  const int lo = s * p.seg, hi = lo + p.seg < (C + VE - 1) / VE ? lo + p.seg : (C + VE - 1) / VE;
+  const T* __restrict__ z = reinterpret_cast<const T*>(p.logits) + row * p.ld;
+  const T* base = p.base ? reinterpret_cast<const T*>(p.base) + row * p.ld : nullptr;
+  T* d = p.dlogits ? reinterpret_cast<T*>(p.dlogits) + row * p.ld : nullptr;
+  const float k = LOG2E * p.inv_T;
+  Entries<T> e;
+  e.load(p, row, z);
+  // the row's maximum and sum, by every wave: its segments a lane each, in turn
+  const MaxSum* part = reinterpret_cast<const MaxSum*>(p.part_ms) + row * p.segs;
+  MaxSum all{-INFINITY, 0.f};
+  for (int i = lane; i < p.segs; i += 64) all = join(all, part[i], k);
+  all = wave_join(all, k);
+  e.weigh(p, k);
+  if (s == 0 && wave == 0) {
+    const float kl = e.loss(p, all);
+    if (t == 0) p.part_loss[row] = e.counts ? kl : 0.f;
+  }
+  bool bad = e.bad;
+  if (d) {
+#pragma unroll
+    for (int i = 0; i < TQ; ++i)
+      if (i == wave) { s_tab.c[t] = e.c[i]; s_tab.q[t] = e.q[i]; }
+    OwnEntry<T> own;
+    own.take(e, base, lo * VE, hi * VE);
+    __syncthreads();                                 // the base's entries are read
+    const float sc = e.counts ? p.scale * (p.loss_scale ? *p.loss_scale : 1.f) : 0.f;
+    const float inv_s = 1.f / all.s;
+    const float f = e.counts ? inv_s * sc : 0.f;
+    for (int b = lo + t; b < hi; b += 4 * 256) {
+      uint4 raw[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) raw[q] = ldg16(z + (int64_t)(b + q * 256 < hi ? b + q * 256 : lo) * VE);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int c0 = (b + q * 256) * VE;
+        float x[VE];
+        unpack<T>(raw[q], x);
+        if (b + q * 256 < hi) bad |= store_gradient<T>(p, d, base, c0, C - c0, x, all.m, k, f);
+      }
+    }
+    __syncthreads();                                 // the segment is written
+    bad |= own.store(p, s_tab, d, all.m, k, inv_s, sc);
   }
   if (bad) raise_flag(p.flag);
 }
@@ -372,6 +604,41 @@ hipError_t launch_group(int lpr, const DistillParams& p, int64_t nb, hipStream_t
   }
 }
 
+// Long rows: a workgroup each where a row fits its registers (1024 threads, 8
+// vectors) and there are rows for most compute units; else segments of at
+// least 1024 vectors (4 a thread), SEGMENT_GROUPS workgroups in all if the rows
+// allow, and at most 8192 vectors each.
+constexpr int64_t ROW_VECS = 8192, SEG_VECS = 1024, ROW_WORKGROUPS = 192, SEGMENT_GROUPS = 512;
+struct LongPlan { int segs, seg; };                  // segs = 0: a workgroup a row
+LongPlan long_plan(int prec, int64_t n, int64_t C) {
+  const int64_t nvec = (C + vec_elems(prec) - 1) / vec_elems(prec);
+  if (nvec <= ROW_VECS && (n >= ROW_WORKGROUPS || nvec <= SEG_VECS)) return {0, 0};
+  const int64_t want = (SEGMENT_GROUPS + n - 1) / n;
+  const int64_t most = (nvec + SEG_VECS - 1) / SEG_VECS, least = (nvec + ROW_VECS - 1) / ROW_VECS;
+  const int64_t segs = want > most ? most : want < least ? least : want;
+  const int64_t seg = (nvec + segs - 1) / segs;
+  return {(int)((nvec + seg - 1) / seg), (int)seg};
+}
+
+template <typename T>
+hipError_t launch_rows(const DistillParams& p, hipStream_t s) {
+  const int64_t nvec = (p.C + Vec<T>::N - 1) / Vec<T>::N;
+  if (p.segs == 0) {
+    const dim3 grid((unsigned)p.n);
+    if (nvec <= 4 * 256) hipLaunchKernelGGL((distill_row_kernel<T, 256, 4>), grid, dim3(256), 0, s, p);
+    else if (nvec <= 8 * 256) hipLaunchKernelGGL((distill_row_kernel<T, 256, 8>), grid, dim3(256), 0, s, p);
+    else if (nvec <= 8 * 512) hipLaunchKernelGGL((distill_row_kernel<T, 512, 8>), grid, dim3(512), 0, s, p);
+    else hipLaunchKernelGGL((distill_row_kernel<T, 1024, 8>), grid, dim3(1024), 0, s, p);
+    return hipGetLastError();
+  }
+  const dim3 grid((unsigned)(p.n * p.segs));
+  hipLaunchKernelGGL((distill_part_kernel<T>), grid, dim3(256), 0, s, p);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((distill_segment_kernel<T>), grid, dim3(256), 0, s, p);
+  return hipGetLastError();
+}
+
 size_t up256(size_t b) { return (b + 255) & ~size_t(255); }
 int64_t cs_ld(int64_t C) { return (C + 7) / 8 * 8; }
 
@@ -380,9 +647,11 @@ int64_t cs_ld(int64_t C) { return (C + 7) / 8 * 8; }
 bool distill_colsum_supported(int prec, int64_t C) { return in_group(prec, C); }
 
 // Lane groups: [loss partials][column-sum partials (blocks x cs_ld)][their
-// block sums].  Workgroup rows: a loss a row.
+// block sums].  Longer rows: [a loss a row][a maximum and sum a
+// segment].
 size_t distill_workspace_bytes(int prec, int64_t n, int64_t C, int64_t K) {
-  if (!in_group(prec, C)) return up256((size_t)n * sizeof(float));
+  if (!in_group(prec, C))
+    return up256((size_t)n * sizeof(float)) + up256((size_t)n * long_plan(prec, n, C).segs * sizeof(MaxSum));
   const int64_t nb = group_blocks(prec, n, C);
   return up256((size_t)nb * sizeof(float)) + up256((size_t)nb * (size_t)cs_ld(C) * sizeof(float)) +
          up256((size_t)colsum_partials_floats(nb, cs_ld(C)) * sizeof(float));
@@ -410,11 +679,11 @@ hipError_t distill_launch(int prec, DistillParams p, float* loss, float* colsum,
     e = prec == 0 ? launch_group<float>(lpr, p, nb, s)
                   : prec == 1 ? launch_group<f16>(lpr, p, nb, s) : launch_group<bf16>(lpr, p, nb, s);
   } else {
-    const dim3 grid((unsigned)p.n);
-    if (prec == 0) hipLaunchKernelGGL((distill_row_kernel<float>), grid, dim3(256), 0, s, p);
-    else if (prec == 1) hipLaunchKernelGGL((distill_row_kernel<f16>), grid, dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((distill_row_kernel<bf16>), grid, dim3(256), 0, s, p);
-    e = hipGetLastError();
+    const LongPlan lp = long_plan(prec, p.n, p.C);
+    p.segs = lp.segs;
+    p.seg = lp.seg;
+    p.part_ms = w + up256((size_t)p.n * sizeof(float));
+    e = prec == 0 ? launch_rows<float>(p, s) : prec == 1 ? launch_rows<f16>(p, s) : launch_rows<bf16>(p, s);
   }
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(distill_final_kernel, dim3(1), dim3(256), 0, s, p.part_loss, nb, p.loss_factor, loss, p.flag);

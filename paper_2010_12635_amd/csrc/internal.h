@@ -201,6 +201,8 @@ struct DistillParams {
   float* part_loss;     // set by distill_launch: loss partials,
   float* part_cs;       // column-sum partials of the workgroups, or NULL,
   int64_t ldcs;         // and their row stride
+  void* part_ms;        // maximum and sum of the segments of long rows,
+  int segs, seg;        // how many a row has, and their vectors
   int32_t* flag;
 };
 bool distill_colsum_supported(int prec, int64_t C);
