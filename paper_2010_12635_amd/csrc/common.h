@@ -40,6 +40,12 @@ __device__ __forceinline__ void stg16(void* p, uint4 v) {
   *reinterpret_cast<uint4*>(p) = v;
 }
 
+__device__ __forceinline__ void stg16_nt(void* p, uint4 v) {
+  u32x4_t x;
+  x.x = v.x; x.y = v.y; x.z = v.z; x.w = v.w;
+  __builtin_nontemporal_store(x, reinterpret_cast<u32x4_t*>(p));
+}
+
 // Unpack a 16-byte vector of storage elements into fp32.
 template <typename T>
 __device__ __forceinline__ void unpack(uint4 raw, float* out) {

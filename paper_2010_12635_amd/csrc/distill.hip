@@ -29,9 +29,10 @@ __device__ __forceinline__ float load_as_f32(int prec, const void* p, int64_t i)
 // marks its class with its number; where an entry finds another's number the
 // same class occurs twice, and one lane adds the row's weights in the order
 // of the entries, so that the sum does not depend on timing.
-// ONE: K <= LPR, an entry a lane at most, loaded with the row; else entries
-// li, li + LPR, ... are read (from the caches) whenever they are needed.
-template <typename T, int LPR, int R, bool ONE>
+// KPL > 0: K <= KPL LPR, entries li, li + LPR, ... of the row are held by lane
+// li, loaded with the row; KPL = 0: they are read (from the caches) whenever
+// they are needed.
+template <typename T, int LPR, int R, int KPL>
 __global__ __launch_bounds__(256) void distill_group_kernel(DistillParams p) {
   constexpr int VE = Vec<T>::N;
   constexpr int G = 64 / LPR;
@@ -64,8 +65,9 @@ __global__ __launch_bounds__(256) void distill_group_kernel(DistillParams p) {
   };
   for (int64_t first = (int64_t)blockIdx.x * (R * RG); first < p.n; first += (int64_t)gridDim.x * (R * RG)) {
     uint4 raw[R], braw[R];
-    int32_t cls[R];
-    float tvs[R];
+    constexpr int KE = KPL > 0 ? KPL : 1;
+    int32_t cls[R][KE];
+    float tvs[R][KE];
     bool on[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -74,7 +76,8 @@ __global__ __launch_bounds__(256) void distill_group_kernel(DistillParams p) {
       raw[r] = ldg16(logits + row * p.ld + (col_ok ? col0 : 0));
       if (p.base) braw[r] = ldg16(reinterpret_cast<const T*>(p.base) + row * p.ld + (col_ok ? col0 : 0));
       on[r] = !p.mask || p.mask[row] != 0;
-      if (ONE) entry(row, li < p.K ? li : 0, cls[r], tvs[r]);
+#pragma unroll
+      for (int i = 0; i < KPL; ++i) entry(row, li + i * LPR < p.K ? li + i * LPR : 0, cls[r][i], tvs[r][i]);
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -82,15 +85,16 @@ __global__ __launch_bounds__(256) void distill_group_kernel(DistillParams p) {
       const bool row_ok = row < p.n;
       const bool in = row_ok && on[r];
       // the teacher's side
-      int32_t c1 = -1;
-      float t1 = -INFINITY;
       float tmax = -INFINITY;
       bool some = false;
-      if (ONE) {
-        if (in && li < p.K) { c1 = cls[r]; t1 = tvs[r]; accept(c1, t1); }
-        some = c1 >= 0;
-        tmax = t1;
-      } else if (in) {
+#pragma unroll
+      for (int i = 0; i < KPL; ++i) {
+        if (in && li + i * LPR < p.K) accept(cls[r][i], tvs[r][i]);
+        else { cls[r][i] = -1; tvs[r][i] = -INFINITY; }
+        some |= cls[r][i] >= 0;
+        tmax = tvs[r][i] > tmax || tvs[r][i] != tvs[r][i] ? tvs[r][i] : tmax;
+      }
+      if (KPL == 0 && in) {
         for (int j = li; j < p.K; j += LPR) {
           int32_t c; float tv;
           entry(row, j, c, tv);
@@ -103,13 +107,17 @@ __global__ __launch_bounds__(256) void distill_group_kernel(DistillParams p) {
       const bool counts = group_any<LPR>(some);
       float er = 0.f, a = 0.f;                       // sum of exponentials, and of exponentials times y T
       const float tm = counts ? tmax : 0.f;
-      float e1 = 0.f;
-      if (ONE) {
-        e1 = c1 >= 0 ? __builtin_amdgcn_exp2f((t1 - tm) * k) : 0.f;
-        er = e1;
-        a = e1 > 0.f || e1 != e1 ? e1 * (t1 - tm) : 0.f;
-        if (c1 >= 0) mine[c1] = __int_as_float(li + 1);
-      } else if (counts) {
+      float ej[KE];
+#pragma unroll
+      for (int i = 0; i < KPL; ++i) {
+        const int32_t c = cls[r][i];
+        const float y = tvs[r][i] - tm;
+        ej[i] = c >= 0 ? __builtin_amdgcn_exp2f(y * k) : 0.f;
+        er += ej[i];
+        a += ej[i] > 0.f || ej[i] != ej[i] ? ej[i] * y : 0.f;
+        if (c >= 0) mine[c] = __int_as_float(li + i * LPR + 1);
+      }
+      if (KPL == 0 && counts) {
         for (int j = li; j < p.K; j += LPR) {
           int32_t c; float tv;
           entry(row, j, c, tv);
@@ -123,9 +131,12 @@ __global__ __launch_bounds__(256) void distill_group_kernel(DistillParams p) {
       }
       wave_sync();
       bool twice = false;
-      if (ONE) {
-        twice = c1 >= 0 && __float_as_int(mine[c1 >= 0 ? c1 : 0]) != li + 1;
-      } else if (counts) {
+#pragma unroll
+      for (int i = 0; i < KPL; ++i) {
+        const int32_t c = cls[r][i];
+        twice |= c >= 0 && __float_as_int(mine[c >= 0 ? c : 0]) != li + i * LPR + 1;
+      }
+      if (KPL == 0 && counts) {
         for (int j = li; j < p.K; j += LPR) {
           int32_t c; float tv;
           entry(row, j, c, tv);
@@ -138,9 +149,10 @@ __global__ __launch_bounds__(256) void distill_group_kernel(DistillParams p) {
       const float inv_er = counts ? 1.f / er : 0.f;
       wave_sync();
       if (!twice) {
-        if (ONE) {
-          if (c1 >= 0) mine[c1] = e1 * inv_er;
-        } else if (counts) {
+#pragma unroll
+        for (int i = 0; i < KPL; ++i)
+          if (cls[r][i] >= 0) mine[cls[r][i]] = ej[i] * inv_er;
+        if (KPL == 0 && counts) {
           for (int j = li; j < p.K; j += LPR) {
             int32_t c; float tv;
             entry(row, j, c, tv);
@@ -199,7 +211,7 @@ __global__ __launch_bounds__(256) void distill_group_kernel(DistillParams p) {
 #pragma unroll
         for (int i = 0; i < VE; ++i) acc_cs[i] += d[i];
         const uint4 o = pack<T>(d);
-        stg16(reinterpret_cast<T*>(p.dlogits) + row * p.ld + col0, o);
+        stg16_nt(reinterpret_cast<T*>(p.dlogits) + row * p.ld + col0, o);
         bad |= packed_nonfinite<T>(o);
       }
     }
@@ -229,158 +241,185 @@ __global__ __launch_bounds__(256) void distill_group_kernel(DistillParams p) {
 // ---------------------------------------------------------- longer rows ----
 //
 // distill_row_kernel: a workgroup owns a row and holds it in its registers (NV
-// vectors a thread): one read, one write.  The teacher's side is done by every
-// wave for itself while the row is on its way, lane l holding the entries l, l
-// + 64, ...; thread j then owns entry j, whose class it writes after the row.
+// vectors a thread): one read, one write.  Thread j has the teacher's entry j
+// and writes its class after the row.
 //
 // distill_part_kernel and distill_segment_kernel: rows that do not fit, and
 // rows too few to fill the chip, are cut into segments of `seg` vectors, a
 // workgroup each: first every segment's maximum and sum of exponentials, then,
 // from those of the whole row, its part of the gradient.
 
-// A maximum and a sum of exponentials relative to it (0 where it is -inf).
+// With k = log2(e) / T everything is in powers of 2: M = k max z as rounded, X_c
+// = z_c k - M (one rounding), p_c = 2^X_c / S, S = sum of the 2^X_c.
+
+// z k rounded on its own: a product that the compiler joins with a later
+// subtraction would make M - M what the rounding left.
+__device__ __forceinline__ float scaled(float z, float k) {
+#pragma clang fp contract(off)
+  return z * k;
+}
+
+// A reference M and a sum of powers relative to it (0 where M is -inf).
 struct MaxSum { float m, s; };
-__device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b, float k) {
+__device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b) {
   const float m = fmaxf(a.m, b.m);
-  const float fa = a.m > -INFINITY ? __builtin_amdgcn_exp2f((a.m - m) * k) : 0.f;
-  const float fb = b.m > -INFINITY ? __builtin_amdgcn_exp2f((b.m - m) * k) : 0.f;
+  const float fa = a.m > -INFINITY ? __builtin_amdgcn_exp2f(a.m - m) : 0.f;
+  const float fb = b.m > -INFINITY ? __builtin_amdgcn_exp2f(b.m - m) : 0.f;
   return {m, a.s * fa + b.s * fb};                   // a NaN stays in s
 }
-__device__ __forceinline__ MaxSum wave_join(MaxSum v, float k) {
+__device__ __forceinline__ MaxSum wave_join(MaxSum v) {
   const float m = group_max<64>(v.m);
-  v.s *= v.m > -INFINITY ? __builtin_amdgcn_exp2f((v.m - m) * k) : 0.f;
+  v.s *= v.m > -INFINITY ? __builtin_amdgcn_exp2f(v.m - m) : 0.f;
   return {m, group_sum<64>(v.s)};
 }
+
+// The vector with the elements from nv < VE on replaced by `fill`: what lies
+// behind a row's end takes no part and needs no test later.
 template <typename T>
-__device__ __forceinline__ float vector_max(const float (&v)[Vec<T>::N], int nv) {
-  float m = -INFINITY;
+__device__ __forceinline__ uint4 fill_tail(uint4 raw, int nv, float fill) {
+  float v[Vec<T>::N];
+  unpack<T>(raw, v);
 #pragma unroll
-  for (int i = 0; i < Vec<T>::N; ++i) m = fmaxf(m, i < nv ? v[i] : -INFINITY);
+  for (int i = 0; i < Vec<T>::N; ++i) v[i] = i < nv ? v[i] : fill;
+  return pack<T>(v);                                 // the others as they were: exact
+}
+template <typename T>
+__device__ __forceinline__ uint4 load_row(const T* row, int c0, int C, float fill) {
+  uint4 raw = ldg16(row + (c0 < C ? c0 : 0));
+  if (C - c0 < Vec<T>::N) raw = fill_tail<T>(raw, C - c0, fill);
+  return raw;
+}
+template <typename T>
+__device__ __forceinline__ float vector_max(uint4 raw) {
+  float v[Vec<T>::N];
+  unpack<T>(raw, v);
+  float m = v[0];
+#pragma unroll
+  for (int i = 1; i < Vec<T>::N; ++i) m = fmaxf(m, v[i]);
   return m;
 }
+// Sum of 2^(z k - M); a lane that has seen only -inf takes M = 0.
 template <typename T>
-__device__ __forceinline__ float vector_sum(const float (&v)[Vec<T>::N], int nv, float m, float k) {
-  const float mm = m > -INFINITY ? m : 0.f;          // a row of -inf alone: 0 each
+__device__ __forceinline__ float vector_sum(uint4 raw, float M, float k) {
+  float v[Vec<T>::N];
+  unpack<T>(raw, v);
   float s = 0.f;
 #pragma unroll
-  for (int i = 0; i < Vec<T>::N; ++i) s += i < nv ? __builtin_amdgcn_exp2f((v[i] - mm) * k) : 0.f;
+  for (int i = 0; i < Vec<T>::N; ++i) s += __builtin_amdgcn_exp2f(fmaf(v[i], k, -M));
   return s;
 }
+// Keeps the compiler from holding unpacked scores between two passes.
+__device__ __forceinline__ void forget(uint4& r) {
+  asm volatile("" : "+v"(r.x), "+v"(r.y), "+v"(r.z), "+v"(r.w));
+}
 
-// The teacher's entries of a row, of which a wave holds all: entry q 64 + lane
-// in element q.
-constexpr int TQ = GCN_MAX_TOP / 64;
-template <typename T>
-struct Entries {
-  int32_t c[TQ];
-  float t[TQ], z[TQ];      // the teacher's score, and the student's for the class
-  float q[TQ], y[TQ];      // weight, and (t - max t) / T
-  float ln_r;
-  bool counts, bad;
-
-  __device__ __forceinline__ void load(const DistillParams& p, int64_t row, const T* __restrict__ zrow) {
-    const int lane = threadIdx.x & 63;
-    const bool in = !p.mask || p.mask[row] != 0;
-    bad = false;
-    bool some = false;
-#pragma unroll
-    for (int i = 0; i < TQ; ++i) {
-      const int j = i * 64 + lane;
-      c[i] = -1;
-      t[i] = -INFINITY;
-      z[i] = 0.f;
-      if (in && j < p.K) {
-        c[i] = p.top_classes[row * p.ld_top + j];
-        t[i] = load_as_f32(p.top_prec, p.top_values, row * p.ld_top + j);
-        if (c[i] >= p.C) bad = true;
-        if (c[i] < 0 || c[i] >= p.C || t[i] == -INFINITY) { c[i] = -1; t[i] = -INFINITY; }
-        if (c[i] >= 0) z[i] = to_f32<T>(zrow[c[i]]);
-      }
-      some |= c[i] >= 0;
-    }
-    counts = __ballot(some) != 0;
-  }
-  __device__ __forceinline__ void weigh(const DistillParams& p, float k) {
-    float m = t[0];
-#pragma unroll
-    for (int i = 1; i < TQ; ++i) m = fmaxf(m, t[i]);
-    m = group_max<64>(m);
-    float r = 0.f;
-#pragma unroll
-    for (int i = 0; i < TQ; ++i) {
-      y[i] = c[i] >= 0 ? (t[i] - m) * p.inv_T : 0.f;
-      q[i] = c[i] >= 0 ? __builtin_amdgcn_exp2f((t[i] - m) * k) : 0.f;
-      r += q[i];
-    }
-    r = group_sum<64>(r);
-    const float inv = 1.f / r;
-#pragma unroll
-    for (int i = 0; i < TQ; ++i) q[i] *= inv;
-    ln_r = logf(r);
-  }
-  // sum of q (y - x): an entry of weight 0 adds nothing
-  __device__ __forceinline__ float loss(const DistillParams& p, MaxSum row) const {
-    float a = 0.f;
-#pragma unroll
-    for (int i = 0; i < TQ; ++i)
-      a += q[i] > 0.f || q[i] != q[i] ? q[i] * (y[i] - (z[i] - row.m) * p.inv_T) : 0.f;
-    return group_sum<64>(a) - ln_r + logf(row.s);
-  }
-};
-
-// Shared by the kernels that write gradients: the row's entries by number.
+// The teacher's entries of a workgroup's row: thread j has entry j, the first
+// waves join their references and sums through shared memory, as the row's.
+constexpr int TW = GCN_MAX_TOP / 64;
 struct EntryTable {
   int32_t c[GCN_MAX_TOP];
   float q[GCN_MAX_TOP];
+  MaxSum part[TW];
+  float loss[TW];
+  int some[TW];
 };
-
 template <typename T>
-__device__ __forceinline__ bool store_gradient(const DistillParams& p, T* d, const T* base, int c0, int nv,
-                                               const float (&v)[Vec<T>::N], float m, float k, float f) {
-  constexpr int VE = Vec<T>::N;
-  float g[VE], bv[VE];
-  if (base) unpack<T>(ldg16(base + c0), bv);
-#pragma unroll
-  for (int i = 0; i < VE; ++i) {
-    g[i] = f != 0.f || f != f ? __builtin_amdgcn_exp2f((v[i] - m) * k) * f : 0.f;   // f = 0: not a counted row
-    if (base) g[i] += bv[i];
-    g[i] = i < nv ? g[i] : 0.f;
-  }
-  const uint4 o = pack<T>(g);
-  stg16(d + c0, o);
-  return packed_nonfinite<T>(o);
-}
+struct Entry {
+  int32_t c;               // class, -1: none
+  float t, z;              // the teacher's score, and the student's for the class
 
-// Thread t's entry, if its class lies in [lo, hi): what its class gets, to be
-// written after the row.
-template <typename T>
-struct OwnEntry {
-  int c;
-  float z, base;
-  __device__ __forceinline__ void take(const Entries<T>& e, const T* base_row, int lo, int hi) {
-    const int wave = threadIdx.x >> 6;
+  // Returns whether the entry is refused.
+  __device__ __forceinline__ bool load(const DistillParams& p, int64_t row, const T* __restrict__ zrow) {
+    const int j = threadIdx.x;
+    const bool in = j < p.K && (!p.mask || p.mask[row] != 0);
     c = -1;
+    t = -INFINITY;
     z = 0.f;
-    base = 0.f;
-#pragma unroll
-    for (int i = 0; i < TQ; ++i)
-      if (i == wave) { c = e.c[i]; z = e.z[i]; }
-    if (c < lo || c >= hi) c = -1;
-    if (c >= 0 && base_row) base = to_f32<T>(base_row[c]);
+    bool bad = false;
+    if (in) {
+      c = p.top_classes[row * p.ld_top + j];
+      t = load_as_f32(p.top_prec, p.top_values, row * p.ld_top + j);
+      bad = c >= p.C;
+      if (c < 0 || bad || t == -INFINITY) { c = -1; t = -INFINITY; }
+      if (c >= 0) z = to_f32<T>(zrow[c]);
+    }
+    return bad;
   }
-  __device__ __forceinline__ bool store(const DistillParams& p, const EntryTable& tab, T* d, float m, float k, float inv_s,
-                                        float sc) const {
-    if (c < 0) return false;
+  // To shared memory; a barrier later every thread may ask counts().
+  __device__ __forceinline__ void share(EntryTable& tab, float k) const {
+    const int w = threadIdx.x >> 6;
+    if (w >= TW) return;
+    const float m = scaled(t, k);
+    const bool some = __ballot(c >= 0) != 0;
+    const MaxSum a = wave_join(MaxSum{c >= 0 ? m : -INFINITY, c < 0 ? 0.f : m == m ? 1.f : m});
+    if ((threadIdx.x & 63) == 0) { tab.part[w] = a; tab.some[w] = some ? 1 : 0; }
+    tab.c[threadIdx.x] = c;
+  }
+  static __device__ __forceinline__ bool counts(const EntryTable& tab) {
+    return (tab.some[0] | tab.some[1] | tab.some[2] | tab.some[3]) != 0;
+  }
+  // The weights, and the waves' parts of the row's loss, to shared memory.
+  __device__ __forceinline__ void weigh(EntryTable& tab, MaxSum row, float k) const {
+    const int w = threadIdx.x >> 6;
+    if (w >= TW) return;
+    MaxSum r = tab.part[0];
+#pragma unroll
+    for (int i = 1; i < TW; ++i) r = join(r, tab.part[i]);
+    const float y = fmaf(t, k, -r.m);                  // log2 of q r
+    const float q = c >= 0 ? __builtin_amdgcn_exp2f(y) / r.s : 0.f;
+    tab.q[threadIdx.x] = q;
+    // sum of q (log2 q - log2 p): an entry of weight 0 adds nothing
+    const float a = q > 0.f || q != q ? q * (y - fmaf(z, k, -row.m)) : 0.f;
+    const float sum = group_sum<64>(a);
+    if ((threadIdx.x & 63) == 0) tab.loss[w] = w == 0 ? sum - log2f(r.s) + log2f(row.s) : sum;
+  }
+  // After a barrier: the row's loss.
+  static __device__ __forceinline__ float loss(const EntryTable& tab) {
+    return ((tab.loss[0] + tab.loss[1]) + (tab.loss[2] + tab.loss[3])) * 0.693147180559945309f;
+  }
+  // After the row is written: what the entry's class gets.
+  __device__ __forceinline__ bool store(const DistillParams& p, const EntryTable& tab, T* d, float base, float M, float k,
+                                        float inv_s, float sc) const {
     float qs = 0.f;
     for (int j = 0; j < p.K; ++j) qs += tab.c[j] == c ? tab.q[j] : 0.f;
-    const T o = from_f32<T>((__builtin_amdgcn_exp2f((z - m) * k) * inv_s - qs) * sc + base);
+    const T o = from_f32<T>((__builtin_amdgcn_exp2f(fmaf(z, k, -M)) * inv_s - qs) * sc + base);
     d[c] = o;
     return !finite_f32(to_f32<T>(o));
   }
 };
+static_assert(TW == 4, "the waves' parts are joined by hand");
 
+// 2^(z k - M) f, added to the base, of a vector from class c0 on.  Returns
+// whether an element is not finite.
+template <typename T>
+__device__ __forceinline__ bool store_gradient(T* d, const T* base, int c0, int C, uint4 raw, float M, float k, float f) {
+  constexpr int VE = Vec<T>::N;
+  float g[VE], v[VE];
+  unpack<T>(raw, v);
+#pragma unroll
+  for (int i = 0; i < VE; ++i) g[i] = __builtin_amdgcn_exp2f(fmaf(v[i], k, -M)) * f;
+  if (base) {
+    float bv[VE];
+    unpack<T>(load_row(base, c0, C, 0.f), bv);
+#pragma unroll
+    for (int i = 0; i < VE; ++i) g[i] += bv[i];
+  }
+  const uint4 o = pack<T>(g);
+  stg16_nt(d + c0, o);
+  return packed_nonfinite<T>(o);
+}
+// The gradient of a row that is not counted.
+template <typename T>
+__device__ __forceinline__ bool store_base(T* d, const T* base, int c0, int C) {
+  const uint4 o = base ? load_row(base, c0, C, 0.f) : make_uint4(0, 0, 0, 0);
+  stg16(d + c0, o);
+  return packed_nonfinite<T>(o);
+}
+
+// Two workgroups of 1024 threads a compute unit, or as many waves of smaller
+// ones: one row's loads and stores under another's arithmetic.
 template <typename T, int NT, int NV>
-__global__ __launch_bounds__(NT) void distill_row_kernel(DistillParams p) {
+__global__ __launch_bounds__(NT, 4) void distill_row_kernel(DistillParams p) {
   constexpr int VE = Vec<T>::N;
   constexpr int NW = NT / 64;
   __shared__ MaxSum s_part[NW];
@@ -394,96 +433,88 @@ __global__ __launch_bounds__(NT) void distill_row_kernel(DistillParams p) {
   const float k = LOG2E * p.inv_T;
   uint4 raw[NV];
 #pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    const int c0 = (v * NT + t) * VE;
-    raw[v] = ldg16(z + (c0 < C ? c0 : 0));
-  }
-  Entries<T> e;
-  e.load(p, row, z);
-  e.weigh(p, k);
-  if (wave < TQ) {
-#pragma unroll
-    for (int i = 0; i < TQ; ++i)
-      if (i == wave) { s_tab.c[t] = e.c[i]; s_tab.q[t] = e.q[i]; }
-  }
-  OwnEntry<T> own;
-  own.take(e, base, 0, C);
+  for (int v = 0; v < NV; ++v) raw[v] = load_row(z, (v * NT + t) * VE, C, -INFINITY);
+  Entry<T> e;
+  bool bad = e.load(p, row, z);
+  // read before the row is written over (the base may be the gradient's buffer)
+  const float base_c = base && e.c >= 0 ? to_f32<T>(base[e.c]) : 0.f;
+  e.share(s_tab, k);
   MaxSum mine{-INFINITY, 0.f};
 #pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    const int c0 = (v * NT + t) * VE;
-    float x[VE];
-    unpack<T>(raw[v], x);
-    mine.m = fmaxf(mine.m, vector_max<T>(x, C - c0));
-  }
+  for (int v = 0; v < NV; ++v) mine.m = fmaxf(mine.m, vector_max<T>(raw[v]));
+  mine.m = scaled(mine.m, k);
+  const float M = mine.m > -INFINITY ? mine.m : 0.f;
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
-    const int c0 = (v * NT + t) * VE;
-    float x[VE];
-    unpack<T>(raw[v], x);
-    mine.s += vector_sum<T>(x, C - c0, mine.m, k);
+    forget(raw[v]);
+    mine.s += vector_sum<T>(raw[v], M, k);
+    forget(raw[v]);
   }
-  mine = wave_join(mine, k);
+  mine = wave_join(mine);
   if (lane == 0) s_part[wave] = mine;
   __syncthreads();
   MaxSum all = s_part[0];
 #pragma unroll
-  for (int i = 1; i < NW; ++i) all = join(all, s_part[i], k);
-  if (wave == 0) {
-    const float kl = e.loss(p, all);
-    if (t == 0) p.part_loss[row] = e.counts ? kl : 0.f;
-  }
-  bool bad = e.bad;
+  for (int i = 1; i < NW; ++i) all = join(all, s_part[i]);
+  const bool counts = e.counts(s_tab);
+  e.weigh(s_tab, all, k);
+  const float sc = p.scale * (p.loss_scale ? *p.loss_scale : 1.f);
+  const float inv_s = 1.f / all.s;
   if (d) {
-    const float sc = e.counts ? p.scale * (p.loss_scale ? *p.loss_scale : 1.f) : 0.f;
-    const float inv_s = 1.f / all.s;
-    const float f = e.counts ? inv_s * sc : 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int c0 = (v * NT + t) * VE;
-      float x[VE];
-      unpack<T>(raw[v], x);
-      if (c0 < C) bad |= store_gradient<T>(p, d, base, c0, C - c0, x, all.m, k, f);
+      if (c0 >= C) break;
+      bad |= counts ? store_gradient(d, base, c0, C, raw[v], all.m, k, inv_s * sc) : store_base(d, base, c0, C);
     }
-    __syncthreads();                                 // the row is written
-    bad |= own.store(p, s_tab, d, all.m, k, inv_s, sc);
   }
+  __syncthreads();                                   // the row is written, the weights known
+  if (t == 0) p.part_loss[row] = counts ? e.loss(s_tab) : 0.f;
+  if (d && e.c >= 0) bad |= e.store(p, s_tab, d, base_c, all.m, k, inv_s, sc);
   if (bad) raise_flag(p.flag);
 }
 
 // Segments: workgroup (row, s) = (blockIdx.x / segs, blockIdx.x % segs).
+struct Segment {
+  int64_t row;
+  int s, lo, hi;                                     // vectors [lo, hi)
+  __device__ __forceinline__ Segment(const DistillParams& p, int VE)
+      : row(blockIdx.x / p.segs), s((int)(blockIdx.x % p.segs)), lo(s * p.seg) {
+    const int nvec = (int)((p.C + VE - 1) / VE);
+    hi = lo + p.seg < nvec ? lo + p.seg : nvec;
+  }
+};
+
 template <typename T>
 __global__ __launch_bounds__(256) void distill_part_kernel(DistillParams p) {
   constexpr int VE = Vec<T>::N;
   __shared__ MaxSum s_part[4];
-  const int64_t row = blockIdx.x / p.segs;
+  const Segment g(p, VE);
   const int t = threadIdx.x;
   const int C = (int)p.C;
-  const int lo = (int)(blockIdx.x % p.segs) * p.seg, hi = lo + p.seg < (C + VE - 1) / VE ? lo + p.seg : (C + VE - 1) / VE;
-  const T* __restrict__ z = reinterpret_cast<const T*>(p.logits) + row * p.ld;
+  const T* __restrict__ z = reinterpret_cast<const T*>(p.logits) + g.row * p.ld;
   const float k = LOG2E * p.inv_T;
   MaxSum mine{-INFINITY, 0.f};
-  for (int b = lo + t; b < hi; b += 4 * 256) {
+  for (int b = g.lo + t; b < g.hi; b += 4 * 256) {
     uint4 raw[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) raw[q] = ldg16(z + (int64_t)(b + q * 256 < hi ? b + q * 256 : lo) * VE);
+    for (int q = 0; q < 4; ++q) raw[q] = load_row(z, b + q * 256 < g.hi ? (b + q * 256) * VE : C, C, -INFINITY);
+    float m = vector_max<T>(raw[0]);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int nv = b + q * 256 < hi ? C - (b + q * 256) * VE : 0;
-      float x[VE];
-      unpack<T>(raw[q], x);
-      const float m = fmaxf(mine.m, vector_max<T>(x, nv));
-      mine.s *= mine.m > -INFINITY ? __builtin_amdgcn_exp2f((mine.m - m) * k) : 0.f;
-      mine.m = m;
-      mine.s += vector_sum<T>(x, nv, m, k);
-    }
+    for (int q = 1; q < 4; ++q) m = fmaxf(m, vector_max<T>(raw[q]));
+    m = fmaxf(mine.m, scaled(m, k));
+    const float M = m > -INFINITY ? m : 0.f;
+    mine.s *= mine.m > -INFINITY ? __builtin_amdgcn_exp2f(mine.m - m) : 1.f;
+    mine.m = m;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) mine.s += vector_sum<T>(raw[q], M, k);
   }
-  mine = wave_join(mine, k);
+  mine = wave_join(mine);
   if ((t & 63) == 0) s_part[t >> 6] = mine;
   __syncthreads();
   if (t == 0) {
     MaxSum a = s_part[0];
-    for (int i = 1; i < 4; ++i) a = join(a, s_part[i], k);
+    for (int i = 1; i < 4; ++i) a = join(a, s_part[i]);
     reinterpret_cast<MaxSum*>(p.part_ms)[blockIdx.x] = a;
   }
 }
@@ -492,62 +523,61 @@ template <typename T>
 __global__ __launch_bounds__(256) void distill_segment_kernel(DistillParams p) {
   constexpr int VE = Vec<T>::N;
   __shared__ EntryTable s_tab;
-  const int64_t row = blockIdx.x / p.segs;
-  const int s = (int)(blockIdx.x % p.segs);
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const Segment g(p, VE);
+  const int t = threadIdx.x;
   const int C = (int)p.C;
-  const int lo = s * p.seg, hi = lo + p.seg < (C + VE - 1) / VE ? lo + p.seg : (C + VE - 1) / VE;
-  const T* __restrict__ z = reinterpret_cast<const T*>(p.logits) + row * p.ld;
-  const T* base = p.base ? reinterpret_cast<const T*>(p.base) + row * p.ld : nullptr;
-  T* d = p.dlogits ? reinterpret_cast<T*>(p.dlogits) + row * p.ld : nullptr;
+  const T* __restrict__ z = reinterpret_cast<const T*>(p.logits) + g.row * p.ld;
+  const T* base = p.base ? reinterpret_cast<const T*>(p.base) + g.row * p.ld : nullptr;
+  T* d = p.dlogits ? reinterpret_cast<T*>(p.dlogits) + g.row * p.ld : nullptr;
   const float k = LOG2E * p.inv_T;
-  Entries<T> e;
-  e.load(p, row, z);
-  // the row's maximum and sum, by every wave: its segments a lane each, in turn
-  const MaxSum* part = reinterpret_cast<const MaxSum*>(p.part_ms) + row * p.segs;
+  Entry<T> e;
+  bool bad = e.load(p, g.row, z);
+  const bool mine = e.c >= g.lo * VE && e.c < g.hi * VE;
+  const float base_c = base && mine ? to_f32<T>(base[e.c]) : 0.f;
+  e.share(s_tab, k);
+  // the row's reference and sum, by every wave: its segments a lane each, in turn
+  const MaxSum* part = reinterpret_cast<const MaxSum*>(p.part_ms) + g.row * p.segs;
   MaxSum all{-INFINITY, 0.f};
-  for (int i = lane; i < p.segs; i += 64) all = join(all, part[i], k);
-  all = wave_join(all, k);
-  e.weigh(p, k);
-  if (s == 0 && wave == 0) {
-    const float kl = e.loss(p, all);
-    if (t == 0) p.part_loss[row] = e.counts ? kl : 0.f;
-  }
-  bool bad = e.bad;
+  for (int i = t & 63; i < p.segs; i += 64) all = join(all, part[i]);
+  all = wave_join(all);
+  __syncthreads();                                   // the table is there, the base's entries are read
+  const bool counts = e.counts(s_tab);
+  e.weigh(s_tab, all, k);
+  const float sc = p.scale * (p.loss_scale ? *p.loss_scale : 1.f);
+  const float inv_s = 1.f / all.s;
   if (d) {
-#pragma unroll
-    for (int i = 0; i < TQ; ++i)
-      if (i == wave) { s_tab.c[t] = e.c[i]; s_tab.q[t] = e.q[i]; }
-    OwnEntry<T> own;
-    own.take(e, base, lo * VE, hi * VE);
-    __syncthreads();                                 // the base's entries are read
-    const float sc = e.counts ? p.scale * (p.loss_scale ? *p.loss_scale : 1.f) : 0.f;
-    const float inv_s = 1.f / all.s;
-    const float f = e.counts ? inv_s * sc : 0.f;
-    for (int b = lo + t; b < hi; b += 4 * 256) {
+    for (int b = g.lo + t; b < g.hi; b += 4 * 256) {
       uint4 raw[4];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) raw[q] = ldg16(z + (int64_t)(b + q * 256 < hi ? b + q * 256 : lo) * VE);
+      for (int q = 0; q < 4; ++q) raw[q] = load_row(z, b + q * 256 < g.hi ? (b + q * 256) * VE : C, C, -INFINITY);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int c0 = (b + q * 256) * VE;
-        float x[VE];
-        unpack<T>(raw[q], x);
-        if (b + q * 256 < hi) bad |= store_gradient<T>(p, d, base, c0, C - c0, x, all.m, k, f);
+        if (b + q * 256 >= g.hi) continue;
+        bad |= counts ? store_gradient(d, base, c0, C, raw[q], all.m, k, inv_s * sc) : store_base(d, base, c0, C);
       }
     }
-    __syncthreads();                                 // the segment is written
-    bad |= own.store(p, s_tab, d, all.m, k, inv_s, sc);
   }
+  __syncthreads();                                   // the segment is written, the weights known
+  if (g.s == 0 && t == 0) p.part_loss[g.row] = counts ? e.loss(s_tab) : 0.f;
+  if (d && mine) bad |= e.store(p, s_tab, d, base_c, all.m, k, inv_s, sc);
   if (bad) raise_flag(p.flag);
 }
 
-__global__ __launch_bounds__(256) void distill_final_kernel(const float* __restrict__ part, int64_t nb, float scale,
-                                                            float* loss, int32_t* flag) {
-  __shared__ float sh[4];
+// Thread t adds partials t, t + 1024, ... in that order (eight loads in
+// flight), then the threads' sums are added in a fixed order.
+__global__ __launch_bounds__(1024) void distill_final_kernel(const float* __restrict__ part, int64_t nb, float scale,
+                                                             float* loss, int32_t* flag) {
+  __shared__ float sh[16];
   float a = 0.f;
-  for (int64_t i = threadIdx.x; i < nb; i += 256) a += part[i];
-  a = block_reduce<4>(a, sh, AddF());
+  for (int64_t i = threadIdx.x; i < nb; i += 8 * 1024) {
+    float v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = i + u * 1024 < nb ? part[i + u * 1024] : 0.f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) a += v[u];
+  }
+  a = block_reduce<16>(a, sh, AddF());
   if (threadIdx.x == 0) {
     const float l = a * scale;
     *loss = l;
@@ -578,18 +608,21 @@ int64_t group_blocks(int prec, int64_t n, int64_t C) {
   return blocks_of(n, rows_per_group(n, rg) * rg);
 }
 
-template <typename T, int LPR, bool ONE>
+template <typename T, int LPR, int KPL>
 hipError_t launch_one(const DistillParams& p, int64_t nb, hipStream_t s) {
   constexpr int64_t RG = 4 * (64 / LPR);
   if (rows_per_group(p.n, RG) == 4)
-    hipLaunchKernelGGL((distill_group_kernel<T, LPR, 4, ONE>), dim3((unsigned)nb), dim3(256), 0, s, p);
+    hipLaunchKernelGGL((distill_group_kernel<T, LPR, 4, KPL>), dim3((unsigned)nb), dim3(256), 0, s, p);
   else
-    hipLaunchKernelGGL((distill_group_kernel<T, LPR, 1, ONE>), dim3((unsigned)nb), dim3(256), 0, s, p);
+    hipLaunchKernelGGL((distill_group_kernel<T, LPR, 1, KPL>), dim3((unsigned)nb), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 template <typename T, int LPR>
 hipError_t launch_lpr(const DistillParams& p, int64_t nb, hipStream_t s) {
-  return p.K <= LPR ? launch_one<T, LPR, true>(p, nb, s) : launch_one<T, LPR, false>(p, nb, s);
+  if (p.K <= LPR) return launch_one<T, LPR, 1>(p, nb, s);
+  if (p.K <= 2 * LPR) return launch_one<T, LPR, 2>(p, nb, s);
+  if (p.K <= 4 * LPR) return launch_one<T, LPR, 4>(p, nb, s);
+  return launch_one<T, LPR, 0>(p, nb, s);
 }
 template <typename T>
 hipError_t launch_group(int lpr, const DistillParams& p, int64_t nb, hipStream_t s) {
@@ -628,7 +661,7 @@ hipError_t launch_rows(const DistillParams& p, hipStream_t s) {
     if (nvec <= 4 * 256) hipLaunchKernelGGL((distill_row_kernel<T, 256, 4>), grid, dim3(256), 0, s, p);
     else if (nvec <= 8 * 256) hipLaunchKernelGGL((distill_row_kernel<T, 256, 8>), grid, dim3(256), 0, s, p);
     else if (nvec <= 8 * 512) hipLaunchKernelGGL((distill_row_kernel<T, 512, 8>), grid, dim3(512), 0, s, p);
-    else hipLaunchKernelGGL((distill_row_kernel<T, 1024, 8>), grid, dim3(1024), 0, s, p);
+    else hipLaunchKernelGGL((distill_row_kernel<T, 512, 16>), grid, dim3(512), 0, s, p);
     return hipGetLastError();
   }
   const dim3 grid((unsigned)(p.n * p.segs));
@@ -686,7 +719,7 @@ hipError_t distill_launch(int prec, DistillParams p, float* loss, float* colsum,
     e = prec == 0 ? launch_rows<float>(p, s) : prec == 1 ? launch_rows<f16>(p, s) : launch_rows<bf16>(p, s);
   }
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(distill_final_kernel, dim3(1), dim3(256), 0, s, p.part_loss, nb, p.loss_factor, loss, p.flag);
+  hipLaunchKernelGGL(distill_final_kernel, dim3(1), dim3(1024), 0, s, p.part_loss, nb, p.loss_factor, loss, p.flag);
   e = hipGetLastError();
   if (e != hipSuccess || !colsum) return e;
   Epilogue eb{};

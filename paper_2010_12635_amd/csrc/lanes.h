@@ -136,17 +136,19 @@ template <> __device__ __forceinline__ bool packed_nonfinite<float>(uint4 o) {
   const uint32_t e = 0x7f800000u;
   return (o.x & e) == e || (o.y & e) == e || (o.z & e) == e || (o.w & e) == e;
 }
-template <uint32_t E>
-__device__ __forceinline__ bool half_pair_nonfinite(uint32_t w) {
-  return (w & E) == E || (w & (E << 16)) == (E << 16);
+// Both halves of a word at once: one is not finite if adding a one at its
+// exponent's lowest bit carries into its (cleared) sign bit.
+template <uint32_t E, uint32_t ONE>
+__device__ __forceinline__ bool half_words_nonfinite(uint4 o) {
+  constexpr uint32_t EE = E | E << 16, ONES = ONE | ONE << 16;
+  const uint32_t c = (((o.x & EE) + ONES) | ((o.y & EE) + ONES)) | (((o.z & EE) + ONES) | ((o.w & EE) + ONES));
+  return (c & 0x80008000u) != 0;
 }
 template <> __device__ __forceinline__ bool packed_nonfinite<f16>(uint4 o) {
-  return half_pair_nonfinite<0x7c00u>(o.x) || half_pair_nonfinite<0x7c00u>(o.y) ||
-         half_pair_nonfinite<0x7c00u>(o.z) || half_pair_nonfinite<0x7c00u>(o.w);
+  return half_words_nonfinite<0x7c00u, 0x0400u>(o);
 }
 template <> __device__ __forceinline__ bool packed_nonfinite<bf16>(uint4 o) {
-  return half_pair_nonfinite<0x7f80u>(o.x) || half_pair_nonfinite<0x7f80u>(o.y) ||
-         half_pair_nonfinite<0x7f80u>(o.z) || half_pair_nonfinite<0x7f80u>(o.w);
+  return half_words_nonfinite<0x7f80u, 0x0080u>(o);
 }
 
 }  // namespace gcn
