@@ -273,22 +273,6 @@ __device__ __forceinline__ MaxSum wave_join(MaxSum v) {
   return {m, group_sum<64>(v.s)};
 }
 
-// The vector with the elements from nv < VE on replaced by `fill`: what lies
-// behind a row's end takes no part and needs no test later.
-template <typename T>
-__device__ __forceinline__ uint4 fill_tail(uint4 raw, int nv, float fill) {
-  float v[Vec<T>::N];
-  unpack<T>(raw, v);
-#pragma unroll
-  for (int i = 0; i < Vec<T>::N; ++i) v[i] = i < nv ? v[i] : fill;
-  return pack<T>(v);                                 // the others as they were: exact
-}
-template <typename T>
-__device__ __forceinline__ uint4 load_row(const T* row, int c0, int C, float fill) {
-  uint4 raw = ldg16(row + (c0 < C ? c0 : 0));
-  if (C - c0 < Vec<T>::N) raw = fill_tail<T>(raw, C - c0, fill);
-  return raw;
-}
 template <typename T>
 __device__ __forceinline__ float vector_max(uint4 raw) {
   float v[Vec<T>::N];

@@ -151,4 +151,20 @@ template <> __device__ __forceinline__ bool packed_nonfinite<bf16>(uint4 o) {
   return half_words_nonfinite<0x7f80u, 0x0080u>(o);
 }
 
+// The vector with the elements from nv < VE on replaced by `fill`: what lies
+// behind a row's end takes no part and needs no test later.
+template <typename T>
+__device__ __forceinline__ uint4 fill_tail(uint4 raw, int nv, float fill) {
+  float v[Vec<T>::N];
+  unpack<T>(raw, v);
+#pragma unroll
+  for (int i = 0; i < Vec<T>::N; ++i) v[i] = i < nv ? v[i] : fill;
+  return pack<T>(v);                                 // the others as they were: exact
+}
+template <typename T>
+__device__ __forceinline__ uint4 load_row(const T* row, int c0, int C, float fill) {
+  uint4 raw = ldg16(row + (c0 < C ? c0 : 0));
+  if (C - c0 < Vec<T>::N) raw = fill_tail<T>(raw, C - c0, fill);
+  return raw;
+}
 }  // namespace gcn

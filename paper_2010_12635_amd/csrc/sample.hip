@@ -19,19 +19,21 @@ namespace {
 
 // ------------------------------------------------ rows in lane groups ----
 //
-// A group of LPR lanes holds a row, VE classes a lane.  With top-k or top-p the
-// row's items are sorted over the group (sorted.h): the weights in that order
-// and their running sum give the number of classes kept, and the last kept
-// item the border.  The draw then runs over the classes in their own order.
+// A group of LPR lanes holds a row, N classes a lane (two vectors: half the
+// exchanges between lanes and half the work a group does once, against one).
+// With top-k or top-p the row's items are sorted over the group (sorted.h): the
+// weights in that order and their running sum give the number of classes kept,
+// and the last kept item the border.  The draw then runs over the classes in
+// their own order.
 //
 // Weights and sums are in 32 bits (W = float); a border is believed only where
 // no running sum lies within DRAW_EPS of it.  With e = 2^-24: a weight's
 // exponent x = (z - max) log2(e) / T carries 3 e |x| (difference, constant,
-// product), so a sum S of weights is off by at most S (3 e ln C / ln 2 + 4 e)
-// with the base-2 exponential's 4 e (the mean of |x| under the weights is at
-// most log2 C), its VE + 6 adds by (VE + 6) e, and p S or u S by 2 e: below
-// 2^-18 S for C <= 512.  Where one does, W = double settles it, for the wave:
-// about one wave in a thousand for 64 classes a row.
+// product), so a sum S of weights is off by at most S (3 e ln C + 4 e) with the
+// base-2 exponential's 4 e (the mean of |x| under the weights is at most log2
+// C), its N + 7 adds by (N + 7) e, and p S or u S by 2 e: below 2^-18 S for C
+// <= 1024.  Where one does, W = double settles it, for the wave: about one wave
+// in a thousand for 64 classes a row.
 constexpr float DRAW_EPS = 3.814697265625e-6f;           // 2^-18
 
 template <typename W> struct Draw;
@@ -57,69 +59,66 @@ __device__ __forceinline__ float least_kept(const SampleParams& p, float zmax) {
   return f;
 }
 
-// The draw of a group's row.  a: the row's items in class order, s: sorted
-// (with FILTER).  Returns whether the answer is certain.
-template <typename W, typename T, int LPR, bool FILTER, typename I, int VE>
-__device__ __forceinline__ bool group_draw(const SampleParams& p, const I (&a)[VE], const I (&s)[VE], int li, float zmax,
-                                           float u, int32_t& label, float& prob) {
+// The draw of a group's row.  z, a: the row's scores and items in class order,
+// s: the items sorted (with FILTER); absent classes have z = -inf and so weight
+// 0.  Returns whether the answer is certain.
+template <typename W, typename T, int LPR, bool FILTER, typename I, int N>
+__device__ __forceinline__ bool group_draw(const SampleParams& p, const float (&z)[N], const I (&a)[N], const I (&s)[N],
+                                           int li, float zmax, float u, int32_t& label, float& prob) {
   typedef Draw<W> D;
-  const int col0 = li * VE;
+  const int col0 = li * N;
   bool sure = true;
   I border{0};
   if constexpr (FILTER) {
-    W w[VE], sum = 0;
-    int n = 0;                                           // this lane's classes under top-k
-#pragma unroll
-    for (int i = 0; i < VE; ++i) {
-      const bool in = item_present<T>(s[i]) && col0 + i < p.top_k;
-      w[i] = in ? D::weight(to_f32<T>(item_score<T>(s[i])), zmax, p) : W(0);
-      sum += w[i];
-      n += in ? 1 : 0;
-    }
-    int m;
+    const int64_t limit = p.top_k - col0;                // this lane's items under top-k
+    const int k = limit < N ? (int)limit : N;
+    int m = (int)p.top_k;                                // the items kept; past the last present one: all
     if (p.top_p < 1.0) {
+      W w[N], sum = 0;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        w[i] = D::weight(to_f32<T>(item_score<T>(s[i])), zmax, p);
+        w[i] = i < k ? w[i] : W(0);
+        sum += w[i];
+      }
       const W total = group_sum<LPR>(sum);
       W run = group_sum_before<LPR>(sum, li);
       const W want = (W)p.top_p * total;
       const W lo = want - D::EPS * total, hi = want + D::EPS * total;
-      int n_lo = 0, n_hi = 0;
+      int n_lo = 0, n_hi = 0;                            // past the last weight the sum is the total
 #pragma unroll
-      for (int i = 0; i < VE; ++i) {
-        const bool in = i < n;                           // what is in comes first
-        n_lo += in && run < lo ? 1 : 0;
-        n_hi += in && run < hi ? 1 : 0;
+      for (int i = 0; i < N; ++i) {
+        n_lo += run < lo ? 1 : 0;
+        n_hi += run < hi ? 1 : 0;
         run += w[i];
       }
       const int both = group_sum<LPR>(n_lo | n_hi << 16);
       m = both & 0xffff;
       sure = m == both >> 16 && m > 0;
-    } else {
-      m = group_sum<LPR>(n);
     }
     // the m-th item, from the lane that holds it
     I mine{0};
 #pragma unroll
-    for (int i = 0; i < VE; ++i) mine = item_pick(col0 + i == m - 1, s[i], mine);
+    for (int i = 0; i < N; ++i) mine = item_pick(i == m - 1 - col0, s[i], mine);
     border = group_max_item<LPR>(mine);
   }
   const float zmin = least_kept(p, zmax);
-  W w[VE], sum = 0;
+  W w[N], sum = 0;
 #pragma unroll
-  for (int i = 0; i < VE; ++i) {
-    const float z = to_f32<T>(item_score<T>(a[i]));
-    const bool kept = item_present<T>(a[i]) && !item_above(border, a[i]) && z >= zmin;
-    w[i] = kept ? D::weight(z, zmax, p) : W(0);
+  for (int i = 0; i < N; ++i) {
+    const bool kept = (!FILTER || !item_above(border, a[i])) && z[i] >= zmin;
+    w[i] = kept ? D::weight(z[i], zmax, p) : W(0);
     sum += w[i];
   }
   const W total = group_sum<LPR>(sum);
   const W want = (W)u * total;
-  const W lo = want - D::EPS * total, hi = want + D::EPS * total;
   W run = group_sum_before<LPR>(sum, li);
   int at;
   if constexpr (sizeof(W) == 4) {
+    const W lo = want - D::EPS * total, hi = want + D::EPS * total;
     int n_lo = 0, n_hi = 0;
 #pragma unroll
-    for (int i = 0; i < VE; ++i) {
+    for (int i = 0; i < N; ++i) {
       run += w[i];
       n_lo += run <= lo ? 1 : 0;
       n_hi += run <= hi ? 1 : 0;
@@ -130,13 +129,13 @@ __device__ __forceinline__ bool group_draw(const SampleParams& p, const I (&a)[V
   } else {
     // the first kept class whose sum passes; the last kept one where rounding
     // leaves none
-    int first = LPR * VE, last = -1;
+    int first = LPR * N, last = -1;
 #pragma unroll
-    for (int i = VE - 1; i >= 0; --i) last = w[i] > 0 && last < 0 ? col0 + i : last;
+    for (int i = N - 1; i >= 0; --i) last = w[i] > 0 && last < 0 ? col0 + i : last;
 #pragma unroll
-    for (int i = 0; i < VE; ++i) {
+    for (int i = 0; i < N; ++i) {
       run += w[i];
-      if (w[i] > 0 && run > want && first == LPR * VE) first = col0 + i;
+      if (w[i] > 0 && run > want && first == LPR * N) first = col0 + i;
     }
     first = -group_max_int<LPR>(-first);
     last = group_max_int<LPR>(last);
@@ -144,26 +143,26 @@ __device__ __forceinline__ bool group_draw(const SampleParams& p, const I (&a)[V
   }
   W mine = 0;
 #pragma unroll
-  for (int i = 0; i < VE; ++i) mine = col0 + i == at ? w[i] : mine;
+  for (int i = 0; i < N; ++i) mine = i == at - col0 ? w[i] : mine;
   label = at;
   prob = (float)(group_sum<LPR>(mine) / total);
   return sure;
 }
 
+// R rows a group and iteration, their loads going out together.
 template <typename T, int LPR, int R, bool FILTER>
 __global__ __launch_bounds__(256) void sample_group_kernel(SampleParams p) {
-  constexpr int VE = Vec<T>::N;
+  constexpr int VE = Vec<T>::N, N = 2 * VE;
   constexpr int RG = 4 * (64 / LPR);
   typedef typename ItemOf<T>::type I;
   const int lane = threadIdx.x & 63, li = lane % LPR;
   const int slot = (threadIdx.x >> 6) * (64 / LPR) + lane / LPR;
-  const int col0 = li * VE;
-  const bool col_ok = col0 < p.C;
-  const int nv = (int)(p.C - col0 < VE ? (p.C - col0 > 0 ? p.C - col0 : 0) : VE);
+  const int col0 = li * N;
+  const int C = (int)p.C;
   const T* __restrict__ logits = reinterpret_cast<const T*>(p.logits);
   bool report = false;
   for (int64_t first = (int64_t)blockIdx.x * (R * RG); first < p.n; first += (int64_t)gridDim.x * (R * RG)) {
-    uint4 raw[R];
+    uint4 raw[R][2];
     float us[R];
     bool on[R];
 #pragma unroll
@@ -174,10 +173,11 @@ __global__ __launch_bounds__(256) void sample_group_kernel(SampleParams p) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int64_t row = first + r * RG + slot;
-      raw[r] = make_uint4(0, 0, 0, 0);
+      raw[r][0] = raw[r][1] = make_uint4(0, 0, 0, 0);
       us[r] = 0.f;
       if (on[r]) {                                       // rows left out are not read
-        raw[r] = ldg16(logits + row * p.ld + (col_ok ? col0 : 0));
+        raw[r][0] = load_row(logits + row * p.ld, col0, C, -INFINITY);
+        raw[r][1] = load_row(logits + row * p.ld, col0 + VE, C, -INFINITY);
         if (!p.greedy) us[r] = p.u[row];
       }
     }
@@ -185,22 +185,39 @@ __global__ __launch_bounds__(256) void sample_group_kernel(SampleParams p) {
     for (int r = 0; r < R; ++r) {
       if (!__ballot(on[r])) continue;
       const int64_t row = first + r * RG + slot;
-      I a[VE], s[VE];
-      const bool bad = group_any<LPR>(make_items<T>(raw[r], col0, nv, a)) || !(us[r] >= 0.f && us[r] < 1.f);
-      I top{0};
+      I a[N], s[N];
+      float z[N];
 #pragma unroll
-      for (int i = 0; i < VE; ++i) top = item_max(top, s[i] = a[i]);
-      if constexpr (FILTER) group_sort<LPR, VE>(s, li);
-      top = group_max_item<LPR>(top);
-      const bool none = bad || !item_present<T>(top);
-      const float zmax = none ? 0.f : to_f32<T>(item_score<T>(top));
+      for (int v = 0; v < 2; ++v) {
+        order_items<T>(raw[r][v], col0 + v * VE, a + v * VE);
+        unpack<T>(raw[r][v], z + v * VE);
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[i] = a[i];
+      I most = a[0], least = a[0];
+      if constexpr (FILTER) {
+        group_sort<LPR, N>(s, li);
+        most = s[0];
+        least = s[N - 1];
+      } else {
+#pragma unroll
+        for (int i = 1; i < N; ++i) {
+          most = item_max(most, a[i]);
+          least = item_min(least, a[i]);
+        }
+      }
+      most = group_max_item<LPR>(most);
+      least = group_min_item<LPR>(least);
+      const bool bad = !items_regular<T>(most, least) || !(us[r] >= 0.f && us[r] < 1.f);
+      const bool none = bad || !item_present<T>(most);
+      const float zmax = none ? 0.f : to_f32<T>(item_score<T>(most));
       int32_t label;
       float prob;
-      const bool sure = group_draw<float, T, LPR, FILTER>(p, a, s, li, zmax, us[r], label, prob);
+      const bool sure = group_draw<float, T, LPR, FILTER>(p, z, a, s, li, zmax, us[r], label, prob);
       if (__ballot(on[r] && !none && !sure)) {
         int32_t l2;
         float p2;
-        group_draw<double, T, LPR, FILTER>(p, a, s, li, zmax, us[r], l2, p2);
+        group_draw<double, T, LPR, FILTER>(p, z, a, s, li, zmax, us[r], l2, p2);
         if (!sure) { label = l2; prob = p2; }
       }
       if (on[r] && li == 0) {
@@ -636,15 +653,15 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleParams p) {
 // ------------------------------------------------------------- launches ----
 
 constexpr int64_t MAX_BLOCKS = 65536;
-constexpr int64_t R4_GROUPS = 16384;      // 4 rows a group and iteration from this many workgroups on
+constexpr int64_t R2_GROUPS = 16384;      // 2 rows a group and iteration from this many workgroups on
 
 template <typename T, int LPR, bool FILTER>
 hipError_t launch_filter(const SampleParams& p, hipStream_t s) {
   constexpr int64_t RG = 4 * (64 / LPR);
-  const int r = (p.n + RG - 1) / RG > R4_GROUPS ? 4 : 1;
+  const int r = (p.n + RG - 1) / RG > R2_GROUPS ? 2 : 1;
   const int64_t nb = std::min<int64_t>((p.n + r * RG - 1) / (r * RG), MAX_BLOCKS);
-  if (r == 4)
-    hipLaunchKernelGGL((sample_group_kernel<T, LPR, 4, FILTER>), dim3((unsigned)nb), dim3(256), 0, s, p);
+  if (r == 2)
+    hipLaunchKernelGGL((sample_group_kernel<T, LPR, 2, FILTER>), dim3((unsigned)nb), dim3(256), 0, s, p);
   else
     hipLaunchKernelGGL((sample_group_kernel<T, LPR, 1, FILTER>), dim3((unsigned)nb), dim3(256), 0, s, p);
   return hipGetLastError();
@@ -668,14 +685,14 @@ hipError_t launch_rows(const SampleParams& p, hipStream_t s) {
 }
 template <typename T>
 hipError_t launch_t(const SampleParams& p, hipStream_t s) {
-  const int64_t nvec = (p.C + Vec<T>::N - 1) / Vec<T>::N;
-  if (nvec <= 1) return launch_lpr<T, 1>(p, s);
-  if (nvec <= 2) return launch_lpr<T, 2>(p, s);
-  if (nvec <= 4) return launch_lpr<T, 4>(p, s);
-  if (nvec <= 8) return launch_lpr<T, 8>(p, s);
-  if (nvec <= 16) return launch_lpr<T, 16>(p, s);
-  if (nvec <= 32) return launch_lpr<T, 32>(p, s);
-  if (nvec <= 64) return launch_lpr<T, 64>(p, s);
+  const int64_t pairs = (p.C + 2 * Vec<T>::N - 1) / (2 * Vec<T>::N);
+  if (pairs <= 1) return launch_lpr<T, 1>(p, s);
+  if (pairs <= 2) return launch_lpr<T, 2>(p, s);
+  if (pairs <= 4) return launch_lpr<T, 4>(p, s);
+  if (pairs <= 8) return launch_lpr<T, 8>(p, s);
+  if (pairs <= 16) return launch_lpr<T, 16>(p, s);
+  if (pairs <= 32) return launch_lpr<T, 32>(p, s);
+  if (pairs <= 64) return launch_lpr<T, 64>(p, s);
   return launch_rows<T>(p, s);
 }
 

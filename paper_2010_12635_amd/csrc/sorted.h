@@ -147,6 +147,50 @@ __device__ __forceinline__ bool make_items(uint4 raw, int c0, int nv, Item64 (&a
   return bad;
 }
 
+// The same for scores that may be anything: NaN takes its place by its bits,
+// above +inf or below -inf, where item_regular() sees it.  p: the items of
+// consecutive vectors, one after the other.
+__device__ __forceinline__ uint32_t plus_zero(f16, uint32_t w) {   // -0 as +0, both halves
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+  f16x2 h;
+  __builtin_memcpy(&h, &w, 4);
+  h += (f16x2)(_Float16)0;
+  __builtin_memcpy(&w, &h, 4);
+  return w;
+}
+__device__ __forceinline__ uint32_t plus_zero(bf16, uint32_t w) {
+  w = (w & 0xffffu) == 0x8000u ? w & 0xffff0000u : w;
+  return w >> 16 == 0x8000u ? w & 0xffffu : w;
+}
+template <typename T>
+__device__ __forceinline__ void order_items(uint4 raw, int c0, Item32* p) {
+  const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+    const uint32_t x = plus_zero(T(), w[h]);
+    const uint32_t s = (x >> 15) & 0x00010001u;
+    const uint32_t k = x ^ (((s << 15) - s) | 0x80008000u);
+    p[2 * h].v = k << 16 | (0xffffu - (uint32_t)(c0 + 2 * h));
+    p[2 * h + 1].v = (k & 0xffff0000u) | (0xffffu - (uint32_t)(c0 + 2 * h + 1));
+  }
+}
+template <typename T>
+__device__ __forceinline__ void order_items(uint4 raw, int c0, Item64* p) {
+  float z[4];
+  unpack<float>(raw, z);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) p[i] = item64(score_key(z[i]), (uint32_t)(c0 + i));
+}
+// Whether the row with these largest and smallest items holds neither NaN nor
+// +inf.
+template <typename T> __device__ __forceinline__ bool items_regular(Item32 most, Item32 least) {
+  const uint32_t inf = 0xffffu - key16_neg_inf<T>();
+  return most.v >> 16 < inf && least.v >> 16 >= key16_neg_inf<T>();
+}
+template <typename T> __device__ __forceinline__ bool items_regular(Item64 most, Item64 least) {
+  return item_key(most) < 0xff800000u && item_key(least) >= KEY_NEG_INF;
+}
+
 // Sorting networks on registers, largest first.
 template <typename I>
 __device__ __forceinline__ void order2(I& a, I& b) {
@@ -193,6 +237,24 @@ __device__ __forceinline__ int group_max_int(int a) {
   }
 }
 
+template <int LPR, int M = 1, typename I>
+__device__ __forceinline__ I group_min_item(I a) {
+  if constexpr (M < LPR) return group_min_item<LPR, 2 * M>(item_min(a, lane_xor<M>(a)));
+  else return a;
+}
+
+// The larger of two items in the front lane, the smaller in the other: for 32
+// bits the median of both and the largest or smallest number.
+__device__ __forceinline__ Item32 item_side(bool front, Item32 a, Item32 o) {
+  const uint32_t end = front ? 0xffffffffu : 0u;
+  uint32_t r;
+  asm("v_med3_u32 %0, %1, %2, %3" : "=v"(r) : "v"(a.v), "v"(o.v), "v"(end));
+  return {r};
+}
+__device__ __forceinline__ Item64 item_side(bool front, Item64 a, Item64 o) {
+  return item_pick(front, item_max(a, o), item_min(a, o));
+}
+
 // The LPR * N items of a lane group, N a lane, into order over the whole
 // group: lane li then holds items li N .. li N + N - 1 of the order.  Merge
 // sort whose first step of each merge pairs an item with its mirror image, so
@@ -204,7 +266,7 @@ __device__ __forceinline__ void group_merge_steps(I (&a)[N], int li) {
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const I o = lane_xor<W>(a[i]);
-    a[i] = item_pick(front, item_max(a[i], o), item_min(a[i], o));
+    a[i] = item_side(front, a[i], o);
   }
   if constexpr (W > 1) group_merge_steps<LPR, N, W / 2>(a, li);
 }
@@ -216,7 +278,7 @@ __device__ __forceinline__ void group_merge_levels(I (&a)[N], int li) {
 #pragma unroll
     for (int i = 0; i < N; ++i) o[i] = lane_xor<W - 1>(a[N - 1 - i]);
 #pragma unroll
-    for (int i = 0; i < N; ++i) a[i] = item_pick(front, item_max(a[i], o[i]), item_min(a[i], o[i]));
+    for (int i = 0; i < N; ++i) a[i] = item_side(front, a[i], o[i]);
     if constexpr (W > 2) group_merge_steps<LPR, N, W / 4>(a, li);
     merge_bitonic<N>(a);
     group_merge_levels<LPR, N, 2 * W>(a, li);
