@@ -24,27 +24,21 @@ struct LongRow {
     if constexpr (RANGES) return (((int)(threadIdx.x >> 6) * span + v) * 64 + (int)(threadIdx.x & 63)) * VE;
     else return (v * NT + (int)threadIdx.x) * VE;
   }
-  // f(scores of a vector, its first class, how many of them the row has) for
-  // the vectors of the thread, four loads in flight.  With WAVE every lane of
-  // the wave takes part in each call, past the row's end too (then with no
-  // score of the row).
-  template <bool WAVE = false, typename F>
+  // f(scores of a vector, its first class) for the vectors of the thread, four
+  // loads in flight.  Every lane takes part in each call; past the row's end it
+  // gets scores of -inf.
+  template <typename F>
   __device__ __forceinline__ void each(F f) const {
     for (int v = 0; v < span; v += 4) {
       uint4 raw[4];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int c0 = first_class(v + q);
-        raw[q] = ldg16(z + (v + q < span && c0 < C ? c0 : 0));
-      }
+      for (int q = 0; q < 4; ++q) raw[q] = load_row(z, v + q < span ? first_class(v + q) : C, C, -INFINITY);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
-        const int c0 = first_class(v + q);
-        const int left = v + q < span ? C - c0 : 0;
-        if (!WAVE && left <= 0) continue;
+        if (v + q >= span) break;
         float x[VE];
         unpack<T>(raw[q], x);
-        f(x, c0, left < VE ? (left > 0 ? left : 0) : VE);
+        f(x, first_class(v + q));
       }
     }
   }
@@ -89,12 +83,11 @@ __device__ __forceinline__ int list_top(const Row r, int K, TopList<NT>& sh, flo
   if (t == 0) sh.count = 0;
   bad = false;
   mx = -INFINITY;
-  r.each([&](const float (&v)[VE], int, int nv) {
+  r.each([&](const float (&v)[VE], int) {
 #pragma unroll
     for (int i = 0; i < VE; ++i) {
-      const bool here = i < nv;
-      bad |= here && !(v[i] < INFINITY);
-      mx = here && v[i] > mx ? v[i] : mx;
+      bad |= !(v[i] < INFINITY);
+      mx = fmaxf(mx, v[i]);                              // NaN is passed over
     }
   });
   const int full = r.C / (64 * VE) < NW ? r.C / (64 * VE) : NW;   // at least 1: shorter rows have a lane group
@@ -112,14 +105,14 @@ __device__ __forceinline__ int list_top(const Row r, int K, TopList<NT>& sh, flo
   b = sh.b[0];
   for (int i = 1; i < full; ++i) b = fminf(b, sh.b[i]);
   auto list = [&](double from) {
-    r.each([&](const float (&v)[VE], int c0, int nv) {
-      bool any = false;
+    r.each([&](const float (&v)[VE], int c0) {
+      float most = v[0];
 #pragma unroll
-      for (int i = 0; i < VE; ++i) any |= v[i] >= b && v[i] > -INFINITY && i < nv;
-      if (!any) return;
+      for (int i = 1; i < VE; ++i) most = fmaxf(most, v[i]);
+      if (!(most >= b)) return;
 #pragma unroll
       for (int i = 0; i < VE; ++i) {
-        if (!(v[i] >= b && v[i] > -INFINITY) || i >= nv) continue;
+        if (!(v[i] >= b && v[i] > -INFINITY)) continue;
         const Item64 e = score_item(v[i], c0 + i);
         if (e.v < from) continue;
         const int at = atomicAdd(&sh.count, 1);
@@ -138,10 +131,10 @@ __device__ __forceinline__ int list_top(const Row r, int K, TopList<NT>& sh, flo
       const uint64_t mid = lo + (hi - lo) / 2 + 1;
       const double m = __longlong_as_double((long long)mid);
       int n = 0;
-      r.each([&](const float (&v)[VE], int c0, int nv) {
+      r.each([&](const float (&v)[VE], int c0) {
 #pragma unroll
         for (int i = 0; i < VE; ++i)
-          if (i < nv && v[i] >= b && v[i] > -INFINITY) n += score_item(v[i], c0 + i).v >= m ? 1 : 0;
+          if (v[i] >= b && v[i] > -INFINITY) n += score_item(v[i], c0 + i).v >= m ? 1 : 0;
       });
       n = block_reduce<NW>(n, sh.n, AddF());
       if (n >= K) { lo = mid; cnt = n; }

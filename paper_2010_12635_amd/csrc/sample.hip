@@ -303,10 +303,17 @@ __global__ __launch_bounds__(NT) void sample_top_kernel(SampleParams p) {
 // key.  Then the classes are walked in their own order, a range of them a
 // wave.  For top_k the weights are 1.
 //
+// Under top_p the first histogram takes weights above 2^-12 only: the others
+// are many, add up to little, and an atomic each would cost more than the rest
+// of the pass; where the border is not among them it is done again down to
+// (1 - top_p) / (2 C), below which it cannot lie (what weighs less adds up to
+// (1 - top_p) / 2 at most, the whole to 1 at least).
+//
 // W = float: weights carry 2^-22 (the exponent in 64 bits, the base-2
-// exponential in 32: one unit in its last place and a rounding), sums are in 64
-// bits; where a running sum comes within LONG_EPS of its border the row is done
-// again with W = double.
+// exponential in 32: one unit in its last place and a rounding), those below the
+// histogram 2^-18 (exponent in 32 bits, |x| <= 20 on their average or next to
+// nothing), sums are in 64 bits; where a running sum comes within its bound of a
+// border the row is done again with W = double.
 template <typename W> struct LongDraw;
 template <> struct LongDraw<float> {
   static __device__ __forceinline__ double weight(float z, float zmax, const SampleParams& p) {
@@ -338,6 +345,9 @@ struct LongShared {
   int count, hit;
   double above, mass, border;
 };
+
+// Weights above 2^-NEAR take part in the first histogram.
+constexpr float NEAR = 12.f;
 
 template <typename W, typename Row>
 struct LongSample {
@@ -380,50 +390,62 @@ struct LongSample {
   }
 
   // Moves `border` to the last item that top_k (COUNT) or top_p keeps among
-  // the items from `border` on.  Returns whether that is certain.
-  template <bool COUNT>
-  __device__ __forceinline__ bool select(double& border, float zmin) {
+  // the items from `border` on (LIMIT; else among all).  Returns whether that is
+  // certain.
+  template <bool COUNT, bool LIMIT>
+  __device__ __forceinline__ bool select(double& border) {
     const int t = threadIdx.x;
-    const double limit = border;
+    const float zl = key_score(item_key(Item64{border}));
+    const int cl = item_class(Item64{border});
     auto weight = [&](float z) -> double { return COUNT ? 1.0 : D::weight(z, zmax, p); };
-    auto inside = [&](float z, int c) { return z > -INFINITY && score_item(z, c).v >= limit; };
-    // Bins of the first histogram.  Under top_p they reach down to weights
-    // 2^-x0 = (1 - top_p) / (2 C): what lies below weighs less than
-    // (1 - top_p) / 2, the whole at least 1, so the border is never there.
-    float scale;
+    auto inside = [&](float z, int c) { return LIMIT ? z > zl || (z == zl && c <= cl) : z > -INFINITY; };
+    // The first histogram: bin floor((zmax - z) scale), BINS and more below it.
+    float scale, near = NEAR;
     if (COUNT) {
-      const float range = zmax - zmin;
+      float low = INFINITY;
+      r.each([&](const float (&v)[VE], int) {
+#pragma unroll
+        for (int i = 0; i < VE; ++i) low = v[i] > -INFINITY ? fminf(low, v[i]) : low;
+      });
+      const float range = zmax - block_reduce<NW>(low, sh.f, MinF());
       scale = range > 0.f && range < INFINITY ? (float)BINS / range : 0.f;
       scale = scale < INFINITY ? scale : 0.f;
-    } else {
-      scale = p.k * ((float)BINS / (1.f + log2f((float)p.C) - log2f((float)(1.0 - p.top_p))));
     }
-    auto bin1 = [&](float z) -> int {                    // BINS or more: below the bins
-      const float x = (zmax - z) * scale;
-      return COUNT ? (x < (float)BINS ? (int)x : BINS - 1) : x < (float)BINS ? (int)x : BINS;
-    };
-    for (int i = t; i < BINS; i += NT) sh.bin[i] = 0.0;
-    if (t == 0) sh.above = 0.0;
-    __syncthreads();
-    double rest = 0.0;
-    r.each([&](const float (&v)[VE], int c0, int nv) {
-#pragma unroll
-      for (int i = 0; i < VE; ++i) {
-        if (i >= nv || !inside(v[i], c0 + i)) continue;
-        const int b = bin1(v[i]);
-        const double w = weight(v[i]);
-        if (b < BINS) lds_add(&sh.bin[b], w);
-        else rest += w;
-      }
-    });
-    rest = block_reduce<NW>(rest, sh.d, AddF());
+    const float far = 1.f + log2f((float)p.C) - log2f((float)(1.0 - p.top_p));
     double want = (double)p.top_k, eps = 0.0;
-    if (!COUNT) {
-      double s = 0.0;
-      for (int i = t; i < BINS; i += NT) s += sh.bin[i];
-      const double total = block_reduce<NW>(s, sh.d, AddF()) + rest;
-      want = p.top_p * total;
-      eps = D::EPS * total;
+    for (;;) {
+      if (!COUNT) scale = p.k * ((float)BINS / near);
+      for (int i = t; i < BINS; i += NT) sh.bin[i] = 0.0;
+      if (t == 0) sh.above = 0.0;
+      __syncthreads();
+      double rest = 0.0;
+      float low_rest = 0.f;
+      r.each([&](const float (&v)[VE], int c0) {
+#pragma unroll
+        for (int i = 0; i < VE; ++i) {
+          const float d = zmax - v[i];
+          const float x = d * scale;
+          if (COUNT) {
+            if (inside(v[i], c0 + i)) lds_add(&sh.bin[x < (float)BINS ? (int)x : BINS - 1], 1.0);
+          } else {
+            const bool in = !LIMIT || inside(v[i], c0 + i);   // -inf weighs nothing
+            const bool close = x < (float)BINS;
+            if (sizeof(W) == 4) low_rest += in && !close ? __builtin_amdgcn_exp2f(-d * p.k) : 0.f;
+            else if (in && !close) rest += weight(v[i]);
+            if (in && close) lds_add(&sh.bin[(int)x], weight(v[i]));
+          }
+        }
+      });
+      rest += (double)low_rest;
+      rest = block_reduce<NW>(rest, sh.d, AddF());       // the histogram is complete, too
+      if (COUNT) break;
+      double sum = 0.0;
+      for (int i = t; i < BINS; i += NT) sum += sh.bin[i];
+      sum = block_reduce<NW>(sum, sh.d, AddF());
+      want = p.top_p * (sum + rest);
+      eps = D::EPS * (sum + 8.0 * rest);
+      if (want + eps < sum || near >= far) break;
+      near = far;
     }
     uint32_t klo = 0, khi = 0;                           // the range of keys, from the first histogram on
     int shift = -1;
@@ -433,23 +455,28 @@ struct LongSample {
       const double above = sh.above, mass = sh.mass;
       // the members of the bin: how many, their keys, and the first MEMBERS
       auto member = [&](float z, int c) {
-        if (!inside(z, c)) return false;
-        if (shift < 0) return bin1(z) == hit;
-        const uint32_t key = score_key(z);
-        return key >= klo && key <= khi && (int)((khi - key) >> shift) == hit;
+        bool m;
+        if (shift < 0) {
+          const float x = (zmax - z) * scale;
+          m = x >= (float)hit && (x < (float)(hit + 1) || (COUNT && hit == BINS - 1));
+        } else {
+          const uint32_t key = score_key(z);
+          m = key >= klo && key <= khi && (int)((khi - key) >> shift) == hit;
+        }
+        return m && inside(z, c);
       };
       if (t == 0) sh.count = 0;
       __syncthreads();
       uint32_t lo = 0xffffffffu, hi = 0;
-      r.each([&](const float (&v)[VE], int c0, int nv) {
+      r.each([&](const float (&v)[VE], int c0) {
 #pragma unroll
         for (int i = 0; i < VE; ++i) {
-          if (i >= nv || !member(v[i], c0 + i)) continue;
+          if (!member(v[i], c0 + i)) continue;
           const uint32_t key = score_key(v[i]);
           lo = key < lo ? key : lo;
           hi = key > hi ? key : hi;
           const int at = atomicAdd(&sh.count, 1);
-          if (at < MEMBERS) { sh.item[at] = score_item(v[i], c0 + i).v; sh.weight[at] = weight(v[i]); }
+          if (at < MEMBERS) sh.item[at] = score_item(v[i], c0 + i).v;
         }
       });
       lo = block_reduce<NW>(lo, sh.u, MinF());
@@ -458,6 +485,8 @@ struct LongSample {
       if (n <= MEMBERS) {
         // a member is kept if what comes before it is below `want`
         const double mine = t < n ? sh.item[t] : 0.0;
+        if (t < n) sh.weight[t] = weight(key_score(item_key(Item64{mine})));
+        __syncthreads();
         double before = above, least = 1.7e308, most = mine;
         if (t < n)
           for (int j = 0; j < n; ++j) before += sh.item[j] > mine ? sh.weight[j] : 0.0;
@@ -480,10 +509,10 @@ struct LongSample {
         while (a < b) {
           const int mid = a + (b - a) / 2;
           int m = 0;
-          r.each([&](const float (&v)[VE], int c0, int nv) {
+          r.each([&](const float (&v)[VE], int c0) {
 #pragma unroll
             for (int i = 0; i < VE; ++i)
-              m += i < nv && c0 + i <= mid && inside(v[i], c0 + i) && score_key(v[i]) == lo ? 1 : 0;
+              m += c0 + i <= mid && score_key(v[i]) == lo && inside(v[i], c0 + i) ? 1 : 0;
           });
           m = block_reduce<NW>(m, sh.n, AddF());
           if ((double)m >= take) b = mid;
@@ -499,12 +528,11 @@ struct LongSample {
       while ((hi - lo) >> shift >= (uint32_t)BINS) ++shift;
       for (int i = t; i < BINS; i += NT) sh.bin[i] = 0.0;
       __syncthreads();
-      r.each([&](const float (&v)[VE], int c0, int nv) {
+      r.each([&](const float (&v)[VE], int c0) {
 #pragma unroll
         for (int i = 0; i < VE; ++i) {
-          if (i >= nv || !inside(v[i], c0 + i)) continue;
           const uint32_t key = score_key(v[i]);
-          if (key >= klo && key <= khi) lds_add(&sh.bin[(khi - key) >> shift], weight(v[i]));
+          if (key >= klo && key <= khi && inside(v[i], c0 + i)) lds_add(&sh.bin[(khi - key) >> shift], weight(v[i]));
         }
       });
       __syncthreads();
@@ -514,18 +542,19 @@ struct LongSample {
   // The draw among the items from `border` on that min-p keeps.
   __device__ __forceinline__ bool draw(double border, float u, int32_t* label, float* prob) {
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    const float least = least_kept(p, zmax);
     const float zb = key_score(item_key(Item64{border}));
     const int cb = item_class(Item64{border});
+    const float least = fmaxf(least_kept(p, zmax), zb);
     auto weight = [&](float z, int c) -> double {
-      return (z > zb || (z == zb && c <= cb)) && z >= least && z > -INFINITY ? D::weight(z, zmax, p) : 0.0;
+      return z >= least && (z > zb || c <= cb) ? D::weight(z, zmax, p) : 0.0;
     };
     double sum = 0.0;
     int last = -1;
-    r.each([&](const float (&v)[VE], int c0, int nv) {
+    r.each([&](const float (&v)[VE], int c0) {
 #pragma unroll
       for (int i = 0; i < VE; ++i) {
-        const double w = i < nv ? weight(v[i], c0 + i) : 0.0;
+        if (!(v[i] >= least)) continue;
+        const double w = weight(v[i], c0 + i);
         sum += w;
         last = w > 0.0 ? c0 + i : last;
       }
@@ -554,18 +583,18 @@ struct LongSample {
       int at = none ? sh.n[owner] : -1;
       double w_at = 0.0;
       bool done = false;
-      r.template each<true>([&](const float (&v)[VE], int c0, int nv) {
+      r.each([&](const float (&v)[VE], int c0) {
         // every lane comes here for every vector of the wave; done and before are the wave's
         if (done) return;
         double w[VE], own = 0.0;
 #pragma unroll
-        for (int i = 0; i < VE; ++i) own += w[i] = i < nv ? weight(v[i], c0 + i) : 0.0;
+        for (int i = 0; i < VE; ++i) own += w[i] = weight(v[i], c0 + i);
         const double upto = wave_scan(own);
         double x = __shfl_up(upto, 1);
         x = before + (lane == 0 ? 0.0 : x);
         bool here = false;
         if (none) {
-          here = at >= c0 && at < c0 + nv;
+          here = at >= c0 && at < c0 + VE;
         } else {
           const uint64_t hits = __ballot(own > 0.0 && before + upto > want);
           here = hits && lane == __ffsll((unsigned long long)hits) - 1;
@@ -611,11 +640,15 @@ struct LongSample {
     return sh.hit != 0;
   }
 
-  __device__ __forceinline__ bool run(float u, float zmin, int32_t* label, float* prob) {
+  __device__ __forceinline__ bool run(float u, int32_t* label, float* prob) {
     double border = item64(KEY_NEG_INF + 1, 0x3fffffff).v;   // every score's item is above
     bool sure = true;
-    if (p.top_k < p.C) sure &= select<true>(border, zmin);
-    if (p.top_p < 1.0) sure &= select<false>(border, zmin);
+    if (p.top_k < p.C) {
+      sure &= select<true, false>(border);
+      if (p.top_p < 1.0) sure &= select<false, true>(border);
+    } else if (p.top_p < 1.0) {
+      sure &= select<false, false>(border);
+    }
     return sure && draw(border, u, label, prob);
   }
 };
@@ -629,25 +662,22 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleParams p) {
   if (p.mask && p.mask[row] == 0) return;
   const Row r(reinterpret_cast<const T*>(p.logits) + row * p.ld, (int)p.C);
   const float u = p.u[row];
-  float mx = -INFINITY, mn = INFINITY;
+  float mx = -INFINITY;
   bool bad = false;
-  r.each([&](const float (&v)[Row::VE], int, int nv) {
+  r.each([&](const float (&v)[Row::VE], int) {
 #pragma unroll
     for (int i = 0; i < Row::VE; ++i) {
-      const bool here = i < nv;
-      bad |= here && !(v[i] < INFINITY);
-      mx = here && v[i] > mx ? v[i] : mx;
-      mn = here && v[i] < mn && v[i] > -INFINITY ? v[i] : mn;
+      bad |= !(v[i] < INFINITY);
+      mx = fmaxf(mx, v[i]);
     }
   });
   bad = __syncthreads_or(bad) || !(u >= 0.f && u < 1.f);
   const float zmax = block_reduce<NW>(mx, sh.f, MaxF());
-  const float zmin = block_reduce<NW>(mn, sh.f, MinF());
   if (!row_answerable(p, row, bad, zmax)) return;
   int32_t* label = p.labels + row;
   float* prob = p.prob ? p.prob + row : nullptr;
-  if (LongSample<float, Row>{p, r, sh, zmax}.run(u, zmin, label, prob)) return;
-  LongSample<double, Row>{p, r, sh, zmax}.run(u, zmin, label, prob);
+  if (LongSample<float, Row>{p, r, sh, zmax}.run(u, label, prob)) return;
+  LongSample<double, Row>{p, r, sh, zmax}.run(u, label, prob);
 }
 
 // ------------------------------------------------------------- launches ----
@@ -679,7 +709,7 @@ hipError_t launch_rows(const SampleParams& p, hipStream_t s) {
     else hipLaunchKernelGGL((sample_top_kernel<T, 1024>), grid, dim3(1024), 0, s, p);
   } else {
     if (nvec <= 8 * 256) hipLaunchKernelGGL((sample_row_kernel<T, 256>), grid, dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((sample_row_kernel<T, 1024>), grid, dim3(1024), 0, s, p);
+    else hipLaunchKernelGGL((sample_row_kernel<T, 512>), grid, dim3(512), 0, s, p);
   }
   return hipGetLastError();
 }
