@@ -18,13 +18,45 @@ __device__ __forceinline__ float key_score(uint32_t k) {
 }
 constexpr uint32_t KEY_NEG_INF = 0x007fffffu;            // score_key(-inf)
 
-// Reductions over the NW waves of a workgroup, every thread ending with the
-// result, in a fixed order.  sh: NW elements of shared memory, free again
-// when the call returns.
+// Reductions over a wave, every lane ending with the result, in a fixed order:
+// within rows of 16 lanes by DPP moves, then over the four rows' results (a
+// move costs a few cycles, an exchange through shared memory's crossbar a
+// hundred).
+template <int CTRL, typename V>
+__device__ __forceinline__ V dpp_move(V v) {
+  static_assert(sizeof(V) == 4 || sizeof(V) == 8, "whole registers");
+  constexpr int N = sizeof(V) / 4;
+  int w[N];
+  __builtin_memcpy(w, &v, sizeof(V));
+#pragma unroll
+  for (int i = 0; i < N; ++i) w[i] = __builtin_amdgcn_update_dpp(0, w[i], CTRL, 0xF, 0xF, true);
+  __builtin_memcpy(&v, w, sizeof(V));
+  return v;
+}
+template <typename V>
+__device__ __forceinline__ V from_lane(V v, int lane) {
+  constexpr int N = sizeof(V) / 4;
+  int w[N];
+  __builtin_memcpy(w, &v, sizeof(V));
+#pragma unroll
+  for (int i = 0; i < N; ++i) w[i] = __builtin_amdgcn_readlane(w[i], lane);
+  __builtin_memcpy(&v, w, sizeof(V));
+  return v;
+}
+template <typename V, typename F>
+__device__ __forceinline__ V wave_reduce(V v, F f) {
+  v = f(v, dpp_move<0xB1>(v));                           // lanes differing in bit 0, then bit 1
+  v = f(v, dpp_move<0x4E>(v));
+  v = f(v, dpp_move<0x141>(v));                          // halves of 8 and rows of 16, mirrored
+  v = f(v, dpp_move<0x140>(v));
+  return f(f(from_lane(v, 0), from_lane(v, 16)), f(from_lane(v, 32), from_lane(v, 48)));
+}
+
+// The same over the NW waves of a workgroup.  sh: NW elements of shared memory,
+// free again when the call returns.
 template <int NW, typename V, typename F>
 __device__ __forceinline__ V block_reduce(V v, V* sh, F f) {
-#pragma unroll
-  for (int m = 32; m > 0; m >>= 1) v = f(v, __shfl_xor(v, m));
+  v = wave_reduce(v, f);
   if constexpr (NW == 1) return v;
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
   __syncthreads();
@@ -38,16 +70,25 @@ struct AddF { template <typename V> __device__ V operator()(V a, V b) const { re
 struct MaxF { template <typename V> __device__ V operator()(V a, V b) const { return a > b ? a : b; } };
 struct MinF { template <typename V> __device__ V operator()(V a, V b) const { return a < b ? a : b; } };
 
-// Inclusive sum over the lanes below and the lane itself.
+// Sum over the lanes up to the lane itself (before it: 0 for lane 0).
 template <typename V>
 __device__ __forceinline__ V wave_scan(V v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    const V o = __shfl_up(v, m);
-    if (lane >= m) v += o;
-  }
-  return v;
+  const int lane = threadIdx.x & 63, in_row = lane & 15;
+  V o = dpp_move<0x111>(v);                              // row_shr by 1, 2, 4, 8
+  v += in_row >= 1 ? o : V(0);
+  o = dpp_move<0x112>(v);
+  v += in_row >= 2 ? o : V(0);
+  o = dpp_move<0x114>(v);
+  v += in_row >= 4 ? o : V(0);
+  o = dpp_move<0x118>(v);
+  v += in_row >= 8 ? o : V(0);
+  const V a = from_lane(v, 15), b = a + from_lane(v, 31), c = b + from_lane(v, 47);
+  return lane < 16 ? v : v + (lane < 32 ? a : lane < 48 ? b : c);
+}
+template <typename V>
+__device__ __forceinline__ V wave_before(V upto) {
+  const V o = __shfl_up(upto, 1);
+  return (threadIdx.x & 63) == 0 ? V(0) : o;
 }
 
 }  // namespace gcn

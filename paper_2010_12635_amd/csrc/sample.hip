@@ -337,13 +337,13 @@ template <int NT>
 struct LongShared {
   double bin[BINS];
   double item[MEMBERS], weight[MEMBERS];
-  double d[NT / 64];
-  int64_t i64[NT / 64];
+  double d[NT / 64], rest[NT / 64];
   float f[NT / 64];
   uint32_t u[NT / 64];
   int n[NT / 64];
-  int count, hit;
-  double above, mass, border;
+  int count, hit, doubt;
+  uint64_t least, most;
+  double above, mass;
 };
 
 // Weights above 2^-NEAR take part in the first histogram.
@@ -360,33 +360,52 @@ struct LongSample {
   LongShared<NT>& sh;
   float zmax;
 
-  // The last bin that holds something and before which the running sum is
-  // below `want`: sh.hit, its start added to sh.above, its sum in sh.mass.
-  __device__ __forceinline__ void find_bin(double want) {
+  __device__ __forceinline__ void clear_bins() {
+    for (int i = threadIdx.x; i < BINS; i += NT) sh.bin[i] = 0.0;
+    if (threadIdx.x == 0) { sh.hit = -1; sh.count = 0; }
+  }
+
+  // With the histogram complete (a barrier since): the last bin that holds
+  // something and before which the running sum from `above` on is below want,
+  // where want = share (above + the sum of the bins + rest): its number, the sum
+  // before it and its own.  rest: this wave's part.
+  struct Found { int bin; double above, mass, want, sum, rest; };
+  __device__ __forceinline__ Found find_bin(double above, double rest, double share, double want) {
     constexpr int PER = BINS / NT;
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    if (t == 0) sh.hit = -1;
     double own[PER], sum = 0.0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) sum += own[i] = sh.bin[t * PER + i];
     const double upto = wave_scan(sum);
-    if (lane == 63) sh.d[wave] = upto;
-    const double above = sh.above;
+    if (lane == 63) { sh.d[wave] = upto; sh.rest[wave] = rest; }
     __syncthreads();
-    double run = __shfl_up(upto, 1);
-    if (lane == 0) run = 0.0;
-    for (int i = 0; i < wave; ++i) run += sh.d[i];
+    Found r;
+    double run = above + wave_before(upto);
+    r.sum = 0.0;
+    r.rest = 0.0;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+      run += i < wave ? sh.d[i] : 0.0;
+      r.sum += sh.d[i];
+      r.rest += sh.rest[i];
+    }
+    r.want = share > 0.0 ? share * (r.sum + r.rest) : want;
     int held = -1;
     double start = 0.0, mass = 0.0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      if (own[i] > 0.0 && above + run < want) { held = t * PER + i; start = run; mass = own[i]; }
+      if (own[i] > 0.0 && run < r.want) { held = t * PER + i; start = run; mass = own[i]; }
       run += own[i];
     }
-    if (held >= 0) atomicMax(&sh.hit, held);
+    const int most = wave_reduce(held, MaxF());
+    if (held >= 0 && held == most) atomicMax(&sh.hit, held);
     __syncthreads();
-    if (held >= 0 && held == sh.hit) { sh.above = above + start; sh.mass = mass; }
+    r.bin = sh.hit;
+    if (held >= 0 && held == r.bin) { sh.above = start; sh.mass = mass; }
     __syncthreads();
+    r.above = sh.above;
+    r.mass = sh.mass;
+    return r;
   }
 
   // Moves `border` to the last item that top_k (COUNT) or top_p keeps among
@@ -412,11 +431,11 @@ struct LongSample {
       scale = scale < INFINITY ? scale : 0.f;
     }
     const float far = 1.f + log2f((float)p.C) - log2f((float)(1.0 - p.top_p));
-    double want = (double)p.top_k, eps = 0.0;
+    Found f;
+    double eps = 0.0;
     for (;;) {
       if (!COUNT) scale = p.k * ((float)BINS / near);
-      for (int i = t; i < BINS; i += NT) sh.bin[i] = 0.0;
-      if (t == 0) sh.above = 0.0;
+      clear_bins();
       __syncthreads();
       double rest = 0.0;
       float low_rest = 0.f;
@@ -436,24 +455,20 @@ struct LongSample {
           }
         }
       });
-      rest += (double)low_rest;
-      rest = block_reduce<NW>(rest, sh.d, AddF());       // the histogram is complete, too
+      if (!COUNT) rest = wave_reduce(rest + (double)low_rest, AddF());
+      __syncthreads();
+      f = find_bin(0.0, rest, COUNT ? 0.0 : p.top_p, (double)p.top_k);
       if (COUNT) break;
-      double sum = 0.0;
-      for (int i = t; i < BINS; i += NT) sum += sh.bin[i];
-      sum = block_reduce<NW>(sum, sh.d, AddF());
-      want = p.top_p * (sum + rest);
-      eps = D::EPS * (sum + 8.0 * rest);
-      if (want + eps < sum || near >= far) break;
+      eps = D::EPS * (f.sum + 8.0 * f.rest);
+      if (f.want + eps < f.sum || near >= far) break;
       near = far;
     }
+    const double want = f.want;
     uint32_t klo = 0, khi = 0;                           // the range of keys, from the first histogram on
     int shift = -1;
     for (;;) {
-      find_bin(want);
-      const int hit = sh.hit;
-      const double above = sh.above, mass = sh.mass;
-      // the members of the bin: how many, their keys, and the first MEMBERS
+      const int hit = f.bin;
+      // the members of the bin: how many, and the first MEMBERS
       auto member = [&](float z, int c) {
         bool m;
         if (shift < 0) {
@@ -465,8 +480,35 @@ struct LongSample {
         }
         return m && inside(z, c);
       };
-      if (t == 0) sh.count = 0;
+      if (threadIdx.x == 0) { sh.least = ~0ull; sh.most = 0; sh.doubt = 0; }
+      r.each([&](const float (&v)[VE], int c0) {
+#pragma unroll
+        for (int i = 0; i < VE; ++i) {
+          if (!member(v[i], c0 + i)) continue;
+          const int at = atomicAdd(&sh.count, 1);
+          if (at < MEMBERS) {
+            sh.item[at] = score_item(v[i], c0 + i).v;
+            sh.weight[at] = weight(v[i]);
+          }
+        }
+      });
       __syncthreads();
+      const int n = sh.count;
+      if (n <= MEMBERS) {
+        // a member is kept if what comes before it is below `want`
+        if (t < n) {
+          const double mine = sh.item[t];
+          double before = f.above;
+          for (int j = 0; j < n; ++j) before += sh.item[j] > mine ? sh.weight[j] : 0.0;
+          const uint64_t bits = (uint64_t)__double_as_longlong(mine);
+          if (before < want) atomicMin((unsigned long long*)&sh.least, (unsigned long long)bits);
+          atomicMax((unsigned long long*)&sh.most, (unsigned long long)bits);
+          if (eps > 0.0 && !(fabs(before - want) > eps && fabs(f.above + f.mass - want) > eps)) sh.doubt = 1;
+        }
+        __syncthreads();
+        border = __longlong_as_double((long long)(sh.least != ~0ull ? sh.least : sh.most));
+        return sh.doubt == 0;
+      }
       uint32_t lo = 0xffffffffu, hi = 0;
       r.each([&](const float (&v)[VE], int c0) {
 #pragma unroll
@@ -475,33 +517,14 @@ struct LongSample {
           const uint32_t key = score_key(v[i]);
           lo = key < lo ? key : lo;
           hi = key > hi ? key : hi;
-          const int at = atomicAdd(&sh.count, 1);
-          if (at < MEMBERS) sh.item[at] = score_item(v[i], c0 + i).v;
         }
       });
       lo = block_reduce<NW>(lo, sh.u, MinF());
       hi = block_reduce<NW>(hi, sh.u, MaxF());
-      const int n = sh.count;
-      if (n <= MEMBERS) {
-        // a member is kept if what comes before it is below `want`
-        const double mine = t < n ? sh.item[t] : 0.0;
-        if (t < n) sh.weight[t] = weight(key_score(item_key(Item64{mine})));
-        __syncthreads();
-        double before = above, least = 1.7e308, most = mine;
-        if (t < n)
-          for (int j = 0; j < n; ++j) before += sh.item[j] > mine ? sh.weight[j] : 0.0;
-        bool sure = true;
-        if (t < n && before < want) least = mine;
-        if (eps > 0.0 && t < n) sure = fabs(before - want) > eps && fabs(above + mass - want) > eps;
-        least = block_reduce<NW>(least, sh.d, MinF());
-        most = block_reduce<NW>(most, sh.d, MaxF());
-        border = least < 1e308 ? least : most;
-        return !__syncthreads_or(!sure);
-      }
       if (lo == hi) {
         // equal scores: the lowest `take` classes
         const double w = weight(key_score(lo));
-        const double q = (want - above) / w;
+        const double q = (want - f.above) / w;
         double take = ceil(q);
         take = take < 1.0 ? 1.0 : take > (double)n ? (double)n : take;
         const bool sure = eps == 0.0 || fabs(q - rint(q)) * w > eps;
@@ -526,7 +549,7 @@ struct LongSample {
       khi = hi;
       shift = 0;
       while ((hi - lo) >> shift >= (uint32_t)BINS) ++shift;
-      for (int i = t; i < BINS; i += NT) sh.bin[i] = 0.0;
+      clear_bins();
       __syncthreads();
       r.each([&](const float (&v)[VE], int c0) {
 #pragma unroll
@@ -536,6 +559,7 @@ struct LongSample {
         }
       });
       __syncthreads();
+      f = find_bin(f.above, 0.0, 0.0, want);
     }
   }
 
@@ -559,9 +583,10 @@ struct LongSample {
         last = w > 0.0 ? c0 + i : last;
       }
     });
-    sum = block_reduce<1>(sum, (double*)nullptr, AddF());
-    last = block_reduce<1>(last, (int*)nullptr, MaxF());
+    sum = wave_reduce(sum, AddF());
+    last = wave_reduce(last, MaxF());
     if (lane == 0) { sh.d[wave] = sum; sh.n[wave] = last; }
+    if (t == 0) sh.doubt = 0;
     __syncthreads();
     double total = 0.0, run = 0.0;
     for (int i = 0; i < NW; ++i) total += sh.d[i];
@@ -576,8 +601,6 @@ struct LongSample {
     const bool none = owner < 0;                         // rounding: the last class kept
     if (none) owner = fallback;
     bool sure = true;
-    if (t == 0) sh.hit = 1;
-    __syncthreads();
     if (wave == owner) {
       const double eps = D::EPS * total;
       int at = none ? sh.n[owner] : -1;
@@ -589,9 +612,9 @@ struct LongSample {
         double w[VE], own = 0.0;
 #pragma unroll
         for (int i = 0; i < VE; ++i) own += w[i] = weight(v[i], c0 + i);
+        if (!__ballot(own > 0.0)) return;
         const double upto = wave_scan(own);
-        double x = __shfl_up(upto, 1);
-        x = before + (lane == 0 ? 0.0 : x);
+        double x = before + wave_before(upto);
         bool here = false;
         if (none) {
           here = at >= c0 && at < c0 + VE;
@@ -624,11 +647,11 @@ struct LongSample {
             *label = at;
             if (prob) *prob = (float)(w_at / total);
           } else {
-            sh.hit = 0;
+            sh.doubt = 1;
           }
         }
         done = __ballot(here) != 0;
-        before += __shfl(upto, 63);
+        before += from_lane(upto, 63);
       });
       // sums of the walk and of the wave may differ by a rounding
       if (!done && lane == 0) {
@@ -637,7 +660,7 @@ struct LongSample {
       }
     }
     __syncthreads();
-    return sh.hit != 0;
+    return sh.doubt == 0;
   }
 
   __device__ __forceinline__ bool run(float u, int32_t* label, float* prob) {
@@ -671,9 +694,14 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleParams p) {
       mx = fmaxf(mx, v[i]);
     }
   });
-  bad = __syncthreads_or(bad) || !(u >= 0.f && u < 1.f);
-  const float zmax = block_reduce<NW>(mx, sh.f, MaxF());
-  if (!row_answerable(p, row, bad, zmax)) return;
+  mx = wave_reduce(mx, MaxF());
+  const bool wave_bad = __ballot(bad) != 0;
+  if ((threadIdx.x & 63) == 0) sh.f[threadIdx.x >> 6] = wave_bad ? INFINITY : mx;
+  __syncthreads();
+  float zmax = sh.f[0];
+#pragma unroll
+  for (int i = 1; i < NW; ++i) zmax = fmaxf(zmax, sh.f[i]);
+  if (!row_answerable(p, row, zmax == INFINITY || !(u >= 0.f && u < 1.f), zmax)) return;
   int32_t* label = p.labels + row;
   float* prob = p.prob ? p.prob + row : nullptr;
   if (LongSample<float, Row>{p, r, sh, zmax}.run(u, label, prob)) return;
