@@ -303,7 +303,7 @@ __global__ __launch_bounds__(NT) void sample_top_kernel(SampleParams p) {
 // key.  Then the classes are walked in their own order, a range of them a
 // wave.  For top_k the weights are 1.
 //
-// Under top_p the first histogram takes weights above 2^-12 only: the others
+// Under top_p the first histogram takes weights above 2^-13 only: the others
 // are many, add up to little, and an atomic each would cost more than the rest
 // of the pass; where the border is not among them it is done again down to
 // (1 - top_p) / (2 C), below which it cannot lie (what weighs less adds up to
@@ -331,7 +331,7 @@ template <> struct LongDraw<double> {
   static constexpr double EPS = 0.0;
 };
 
-constexpr int BINS = 1024, MEMBERS = 256;
+constexpr int BINS = 1024, MEMBERS = 256, NEAR_CAP = 512;
 
 template <int NT>
 struct LongShared {
@@ -344,10 +344,14 @@ struct LongShared {
   int count, hit, doubt;
   uint64_t least, most;
   double above, mass;
+  // classes of large weight, those of each wave in the order of the classes
+  float near_z[NT / 64][NEAR_CAP];
+  int near_c[NT / 64][NEAR_CAP];
+  int near_n[NT / 64];
 };
 
 // Weights above 2^-NEAR take part in the first histogram.
-constexpr float NEAR = 12.f;
+constexpr float NEAR = 13.f;
 
 template <typename W, typename Row>
 struct LongSample {
@@ -406,6 +410,24 @@ struct LongSample {
     r.above = sh.above;
     r.mass = sh.mass;
     return r;
+  }
+
+  // The n listed members of a bin: one is kept if what comes before it is below
+  // f.want.  Returns whether that is certain for all.
+  __device__ __forceinline__ bool settle(const Found& f, int n, double eps, double& border) {
+    const int t = threadIdx.x;
+    if (t < n) {
+      const double mine = sh.item[t];
+      double before = f.above;
+      for (int j = 0; j < n; ++j) before += sh.item[j] > mine ? sh.weight[j] : 0.0;
+      const uint64_t bits = (uint64_t)__double_as_longlong(mine);
+      if (before < f.want) atomicMin((unsigned long long*)&sh.least, (unsigned long long)bits);
+      atomicMax((unsigned long long*)&sh.most, (unsigned long long)bits);
+      if (eps > 0.0 && !(fabs(before - f.want) > eps && fabs(f.above + f.mass - f.want) > eps)) sh.doubt = 1;
+    }
+    __syncthreads();
+    border = __longlong_as_double((long long)(sh.least != ~0ull ? sh.least : sh.most));
+    return sh.doubt == 0;
   }
 
   // Moves `border` to the last item that top_k (COUNT) or top_p keeps among
@@ -495,19 +517,7 @@ struct LongSample {
       __syncthreads();
       const int n = sh.count;
       if (n <= MEMBERS) {
-        // a member is kept if what comes before it is below `want`
-        if (t < n) {
-          const double mine = sh.item[t];
-          double before = f.above;
-          for (int j = 0; j < n; ++j) before += sh.item[j] > mine ? sh.weight[j] : 0.0;
-          const uint64_t bits = (uint64_t)__double_as_longlong(mine);
-          if (before < want) atomicMin((unsigned long long*)&sh.least, (unsigned long long)bits);
-          atomicMax((unsigned long long*)&sh.most, (unsigned long long)bits);
-          if (eps > 0.0 && !(fabs(before - want) > eps && fabs(f.above + f.mass - want) > eps)) sh.doubt = 1;
-        }
-        __syncthreads();
-        border = __longlong_as_double((long long)(sh.least != ~0ull ? sh.least : sh.most));
-        return sh.doubt == 0;
+        return settle(f, n, eps, border);
       }
       uint32_t lo = 0xffffffffu, hi = 0;
       r.each([&](const float (&v)[VE], int c0) {
@@ -663,6 +673,132 @@ struct LongSample {
     return sh.doubt == 0;
   }
 
+  // Rows whose mass lies on few classes: those of weights above 2^-near are
+  // listed, in the order of the classes, and everything else is done on the
+  // list, in 64 bits; the other weights enter by their sum alone, in 32 bits
+  // (good to 2^-18 of itself) or, exact, in 64.
+  enum Listed {
+    DONE,
+    BEYOND,                                              // the border is among the others
+    LONG, FAR_LONG,                                      // the list is too short, by more than a factor of 2
+    DOUBT,                                               // the sum of the others is not known well enough
+    TIES                                                 // too many equal or nearly equal scores at the border
+  };
+  __device__ __forceinline__ Listed run_listed(float near, bool exact, float u, int32_t* label, float* prob) {
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    clear_bins();
+    int n = 0;                                           // the wave's entries
+    float low_rest = 0.f;
+    double rest = 0.0;
+    r.each([&](const float (&v)[VE], int c0) {
+      bool in[VE];
+      int own = 0;
+#pragma unroll
+      for (int i = 0; i < VE; ++i) {
+        const float x = (zmax - v[i]) * p.k;
+        in[i] = x < near;
+        own += in[i] ? 1 : 0;
+        low_rest += in[i] ? 0.f : __builtin_amdgcn_exp2f(-x);
+      }
+      if (exact) {
+        for (int i = 0; i < VE; ++i) rest += in[i] ? 0.0 : Draw<double>::weight(v[i], zmax, p);
+      }
+      if (!__ballot(own > 0)) return;
+      const int upto = wave_scan(own);
+      int at = n + upto - own;
+      n += from_lane(upto, 63);
+#pragma unroll
+      for (int i = 0; i < VE; ++i) {
+        if (!in[i]) continue;
+        if (at < NEAR_CAP) { sh.near_z[wave][at] = v[i]; sh.near_c[wave][at] = c0 + i; }
+        ++at;
+      }
+    });
+    if (t == 0) { sh.least = ~0ull; sh.most = 0; sh.doubt = 0; }
+    if (lane == 0) sh.near_n[wave] = n;
+    __syncthreads();
+    int longest = 0;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) longest = sh.near_n[i] > longest ? sh.near_n[i] : longest;
+    if (longest > NEAR_CAP) return longest > 2 * NEAR_CAP ? FAR_LONG : LONG;
+    // this lane's entries: lane, lane + 64, ...
+    constexpr int PER = NEAR_CAP / 64;
+    float z[PER];
+    int c[PER];
+    double w[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int e = i * 64 + lane;
+      z[i] = e < n ? sh.near_z[wave][e] : -INFINITY;
+      c[i] = e < n ? sh.near_c[wave][e] : 0;
+      w[i] = e < n ? Draw<double>::weight(z[i], zmax, p) : 0.0;
+    }
+    double border = item64(KEY_NEG_INF + 1, 0x3fffffff).v;
+    if (p.top_p < 1.0) {
+      const float scale = p.k * ((float)BINS / near);
+      auto bin = [&](float z) { const float x = (zmax - z) * scale; return x < (float)BINS ? (int)x : BINS - 1; };
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (i * 64 + lane < n) lds_add(&sh.bin[bin(z[i])], w[i]);
+      __syncthreads();
+      rest = wave_reduce(exact ? rest : (double)low_rest, AddF());
+      const Found f = find_bin(0.0, rest, p.top_p, 0.0);
+      const double eps = exact ? 0.0 : 3.814697265625e-6 * f.rest + 1e-15 * f.sum;   // 2^-18
+      if (!(f.want + eps < f.sum)) return BEYOND;
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (i * 64 + lane < n && bin(z[i]) == f.bin) {
+          const int at = atomicAdd(&sh.count, 1);
+          if (at < MEMBERS) { sh.item[at] = score_item(z[i], c[i]).v; sh.weight[at] = w[i]; }
+        }
+      __syncthreads();
+      const int members = sh.count;
+      if (members > MEMBERS) return TIES;
+      if (!settle(f, members, eps, border)) return DOUBT;
+    }
+    const float least = least_kept(p, zmax);
+    double sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      if (!(z[i] >= least && score_item(z[i], c[i]).v >= border)) w[i] = 0.0;
+      sum += w[i];
+    }
+    sum = wave_reduce(sum, AddF());
+    if (lane == 0) sh.d[wave] = sum;
+    __syncthreads();
+    double total = 0.0;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) total += sh.d[i];
+    const double want = (double)u * total;
+    int owner = -1;
+    double before = 0.0, run = 0.0;
+    for (int i = 0; i < NW; ++i) {                       // the last that keeps anything where rounding leaves none
+      if (sh.d[i] > 0.0 && run <= want) { owner = i; before = run; }
+      run += sh.d[i];
+    }
+    if (wave != owner) return DONE;
+    int at = -1;
+    double w_at = 0.0;
+    bool passed = false;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const double upto = before + wave_scan(w[i]);
+      const uint64_t kept = __ballot(w[i] > 0.0), hits = __ballot(w[i] > 0.0 && upto > want);
+      if (kept && !passed) {
+        const int l = hits ? __ffsll((unsigned long long)hits) - 1 : 63 - __clzll(kept);
+        at = from_lane(c[i], l);
+        w_at = from_lane(w[i], l);
+        passed = hits != 0;
+      }
+      before = from_lane(upto, 63);
+    }
+    if (lane == 0) {
+      *label = at;
+      if (prob) *prob = (float)(w_at / total);
+    }
+    return DONE;
+  }
+
   __device__ __forceinline__ bool run(float u, int32_t* label, float* prob) {
     double border = item64(KEY_NEG_INF + 1, 0x3fffffff).v;   // every score's item is above
     bool sure = true;
@@ -677,7 +813,7 @@ struct LongSample {
 };
 
 template <typename T, int NT>
-__global__ __launch_bounds__(NT) void sample_row_kernel(SampleParams p) {
+__global__ __launch_bounds__(NT, 4) void sample_row_kernel(SampleParams p) {
   typedef LongRow<T, NT, true> Row;
   constexpr int NW = NT / 64;
   __shared__ LongShared<NT> sh;
@@ -704,7 +840,24 @@ __global__ __launch_bounds__(NT) void sample_row_kernel(SampleParams p) {
   if (!row_answerable(p, row, zmax == INFINITY || !(u >= 0.f && u < 1.f), zmax)) return;
   int32_t* label = p.labels + row;
   float* prob = p.prob ? p.prob + row : nullptr;
-  if (LongSample<float, Row>{p, r, sh, zmax}.run(u, label, prob)) return;
+  LongSample<float, Row> q{p, r, sh, zmax};
+  // worth trying where the filters may leave few classes: with more of them
+  // where the border is not on the list, with fewer where it is too short by
+  // less than a factor of 2
+  if (p.top_k == p.C && (p.top_p < 1.0 || p.ln_min_p > -8.0)) {
+    float near = p.top_p < 1.0 ? NEAR : (float)(-p.ln_min_p * 1.4426950408889634) + 0.01f;
+    bool grown = false, exact = false;
+    for (int i = 0; i < 4; ++i) {
+      const auto did = q.run_listed(near, exact, u, label, prob);
+      if (did == q.DONE) return;
+      __syncthreads();
+      if (did == q.FAR_LONG || did == q.TIES || p.top_p == 1.0 || (did == q.LONG && grown)) break;
+      exact = did == q.DOUBT;
+      grown |= did == q.BEYOND;
+      near *= did == q.BEYOND ? 1.4f : did == q.LONG ? 0.8f : 1.f;
+    }
+  }
+  if (q.run(u, label, prob)) return;
   LongSample<double, Row>{p, r, sh, zmax}.run(u, label, prob);
 }
 
