@@ -100,8 +100,8 @@ template <typename T> __device__ __forceinline__ uint32_t bits_neg_inf();
 template <> __device__ __forceinline__ uint32_t bits_neg_inf<f16>() { return 0xfc00u; }
 template <> __device__ __forceinline__ uint32_t bits_neg_inf<bf16>() { return 0xff80u; }
 
-// The items of 16 bytes of scores from class c0 on, the first nv of them in
-// the row.  Returns whether one was NaN (then absent) or +inf.
+// The items of 16 bytes of scores from class c0 on, the first nv of them (none
+// if nv is negative) in the row.  Returns whether one was NaN (then absent) or +inf.
 template <typename T>
 __device__ __forceinline__ bool make_items(uint4 raw, int c0, int nv, Item32 (&a)[8]) {
   bool bad = false;

@@ -52,7 +52,8 @@ __device__ __forceinline__ void list_levels(I (&a)[L]) {
   }
 }
 
-// Rows of up to 64 vectors of 16 bytes: a group of LPR lanes owns a row.
+// Rows of up to 128 vectors of 16 bytes: a group of LPR lanes owns a row, two
+// vectors a lane.
 //
 // L > 0: the first L >= K items only.  Each lane sorts its own, then lists are
 // merged pairwise across lanes: of two sorted lists of L, the larger of item
@@ -63,36 +64,54 @@ __device__ __forceinline__ void list_levels(I (&a)[L]) {
 // L = 0: the row is sorted over the group.
 template <typename T, int LPR, int L, int R>
 __global__ __launch_bounds__(256) void top_group_kernel(TopParams p) {
-  constexpr int VE = Vec<T>::N;
+  constexpr int VE = Vec<T>::N, N = 2 * VE;
   constexpr int RG = 4 * (64 / LPR);
   typedef typename ItemOf<T>::type I;
   const int lane = threadIdx.x & 63, li = lane % LPR;
   const int slot = (threadIdx.x >> 6) * (64 / LPR) + lane / LPR;
-  const int col0 = li * VE;
-  const bool col_ok = col0 < p.C;
-  const int nv = (int)(p.C - col0 < VE ? (p.C - col0 > 0 ? p.C - col0 : 0) : VE);
+  const int col0 = li * N;
+  const int C = (int)p.C;
   const T* __restrict__ logits = reinterpret_cast<const T*>(p.logits);
   bool bad = false;
   for (int64_t first = (int64_t)blockIdx.x * (R * RG); first < p.n; first += (int64_t)gridDim.x * (R * RG)) {
-    uint4 raw[R];
+    uint4 raw[R][2];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       int64_t row = first + r * RG + slot;
       row = row < p.n ? row : p.n - 1;               // in bounds; not stored below
-      raw[r] = ldg16(logits + row * p.ld + (col_ok ? col0 : 0));
+#pragma unroll
+      for (int v = 0; v < 2; ++v) raw[r][v] = ldg16(logits + row * p.ld + (col0 + v * VE < C ? col0 + v * VE : 0));
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int64_t row = first + r * RG + slot;
       const bool row_ok = row < p.n;
-      I a[VE];
-      bad |= make_items<T>(raw[r], col0, nv, a);
+      I a[2][VE];
+#pragma unroll
+      for (int v = 0; v < 2; ++v) bad |= make_items<T>(raw[r][v], col0 + v * VE, C - col0 - v * VE, a[v]);
       if constexpr (L > 0) {
         I list[L];
-        sort_items<VE>(a);
+        sort_items<VE>(a[0]);
+        sort_items<VE>(a[1]);
+        // the lane's own list: its two halves joined, or the larger part of both
+        constexpr int H = N < L ? N : L;             // items in use
+        if constexpr (L > VE) {
 #pragma unroll
-        for (int i = 0; i < L; ++i) list[i] = i < VE ? a[i < VE ? i : 0] : I{0};
-        list_levels<LPR, L, 1, VE>(list);
+          for (int i = 0; i < VE; ++i) {
+            list[i] = item_max(a[0][i], a[1][VE - 1 - i]);
+            list[VE + i] = item_min(a[0][i], a[1][VE - 1 - i]);
+          }
+          merge_bitonic<VE>(list);
+          merge_bitonic<VE>(list + VE);
+#pragma unroll
+          for (int i = N; i < L; ++i) list[i] = I{0};
+        } else {
+          static_assert(L == VE, "lists of whole vectors");
+#pragma unroll
+          for (int i = 0; i < VE; ++i) list[i] = item_max(a[0][i], a[1][VE - 1 - i]);
+          merge_bitonic<VE>(list);
+        }
+        list_levels<LPR, L, 1, H>(list);
         // entry j is written by lane j mod LPR
 #pragma unroll
         for (int q = 0; q < (L + LPR - 1) / LPR; ++q) {
@@ -103,13 +122,16 @@ __global__ __launch_bounds__(256) void top_group_kernel(TopParams p) {
           if (row_ok && j < L && j < p.K) put_entry<T>(p, row, j, e);
         }
       } else {
-        group_sort<LPR, VE>(a, li);
+        I s[N];
 #pragma unroll
-        for (int i = 0; i < VE; ++i)
-          if (row_ok && col0 + i < p.K) put_entry<T>(p, row, col0 + i, a[i]);
+        for (int i = 0; i < N; ++i) s[i] = a[i / VE][i % VE];
+        group_sort<LPR, N>(s, li);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (row_ok && col0 + i < p.K) put_entry<T>(p, row, col0 + i, s[i]);
       }
       // entries past the classes the group holds
-      constexpr int HELD = L > 0 ? L : LPR * VE;
+      constexpr int HELD = L > 0 ? L : LPR * N;
       if (HELD < GCN_MAX_TOP && row_ok)
         for (int64_t j = HELD + li; j < p.K; j += LPR) put_entry<T>(p, row, j, I{0});
     }
@@ -136,17 +158,17 @@ __global__ __launch_bounds__(NT) void top_row_kernel(TopParams p) {
 // ------------------------------------------------------------- launches ----
 
 constexpr int64_t MAX_BLOCKS = 65536;
-// Rows a lane group takes per iteration (their loads go out together): 4 when
+// Rows a lane group takes per iteration (their loads go out together): 2 when
 // that still leaves this many workgroups, else 1.
-constexpr int64_t R4_GROUPS = 16384;
+constexpr int64_t R2_GROUPS = 16384;
 
 template <typename T, int LPR, int L>
 hipError_t launch_l(const TopParams& p, hipStream_t s) {
   constexpr int64_t RG = 4 * (64 / LPR);
-  const int r = (p.n + RG - 1) / RG > R4_GROUPS ? 4 : 1;
+  const int r = (p.n + RG - 1) / RG > R2_GROUPS ? 2 : 1;
   const int64_t nb = std::min<int64_t>((p.n + r * RG - 1) / (r * RG), MAX_BLOCKS);
-  if (r == 4)
-    hipLaunchKernelGGL((top_group_kernel<T, LPR, L, 4>), dim3((unsigned)nb), dim3(256), 0, s, p);
+  if (r == 2)
+    hipLaunchKernelGGL((top_group_kernel<T, LPR, L, 2>), dim3((unsigned)nb), dim3(256), 0, s, p);
   else
     hipLaunchKernelGGL((top_group_kernel<T, LPR, L, 1>), dim3((unsigned)nb), dim3(256), 0, s, p);
   return hipGetLastError();
@@ -169,14 +191,14 @@ hipError_t launch_rows(const TopParams& p, hipStream_t s) {
 }
 template <typename T>
 hipError_t launch_t(const TopParams& p, hipStream_t s) {
-  const int64_t nvec = (p.C + Vec<T>::N - 1) / Vec<T>::N;
-  if (nvec <= 1) return launch_lpr<T, 1>(p, s);
-  if (nvec <= 2) return launch_lpr<T, 2>(p, s);
-  if (nvec <= 4) return launch_lpr<T, 4>(p, s);
-  if (nvec <= 8) return launch_lpr<T, 8>(p, s);
-  if (nvec <= 16) return launch_lpr<T, 16>(p, s);
-  if (nvec <= 32) return launch_lpr<T, 32>(p, s);
-  if (nvec <= 64) return launch_lpr<T, 64>(p, s);
+  const int64_t pairs = (p.C + 2 * Vec<T>::N - 1) / (2 * Vec<T>::N);
+  if (pairs <= 1) return launch_lpr<T, 1>(p, s);
+  if (pairs <= 2) return launch_lpr<T, 2>(p, s);
+  if (pairs <= 4) return launch_lpr<T, 4>(p, s);
+  if (pairs <= 8) return launch_lpr<T, 8>(p, s);
+  if (pairs <= 16) return launch_lpr<T, 16>(p, s);
+  if (pairs <= 32) return launch_lpr<T, 32>(p, s);
+  if (pairs <= 64) return launch_lpr<T, 64>(p, s);
   return launch_rows<T>(p, s);
 }
 
