@@ -452,7 +452,8 @@ gcn_status gcn_top_logits(int64_t n, int64_t C, int64_t ld, int32_t prec, const 
  * A row is counted if mask selects it (uint8, NULL = every row; n_mask = its
  * nonzero entries, > 0, as in gcn_loss) and it has an entry that is present.
  * dlogits_base (n x C, ld, prec) may be dlogits itself: gcn_loss followed by
- * this call on the same buffer gives the gradient of both losses together.
+ * this call on the same buffer gives the gradient of both losses together;
+ * otherwise dlogits overlaps none of the inputs.
  * dlogits may be NULL (the loss alone; dlogits_base and dlogits_colsum must
  * then be NULL).  A class >= C is left out and sets *overflow, as does a
  * loss, gradient or column sum that is not finite.  T in

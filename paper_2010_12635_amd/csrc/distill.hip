@@ -548,11 +548,32 @@ __global__ __launch_bounds__(256) void distill_segment_kernel(DistillParams p) {
   if (bad) raise_flag(p.flag);
 }
 
-// Thread t adds partials t, t + 1024, ... in that order (eight loads in
-// flight), then the threads' sums are added in a fixed order.
+// Workgroup 0, the loss: thread t adds partials t, t + 1024, ... in that order
+// (eight loads in flight), then the threads' sums are added in a fixed order.
+// Workgroups b > 0 (few partials): the column sums of classes 64 (b - 1) on, 16
+// threads a column; classes [C, ld) get 0.
 __global__ __launch_bounds__(1024) void distill_final_kernel(const float* __restrict__ part, int64_t nb, float scale,
-                                                             float* loss, int32_t* flag) {
+                                                             float* loss, int32_t* flag, const float* __restrict__ part_cs,
+                                                             int64_t ldcs, int64_t C, int64_t ld, float* colsum) {
   __shared__ float sh[16];
+  __shared__ float s_cs[16][64];
+  if (blockIdx.x > 0) {
+    const int col = threadIdx.x & 63, g = threadIdx.x >> 6;
+    const int64_t c = (int64_t)(blockIdx.x - 1) * 64 + col;
+    float a = 0.f;
+    if (c < C)
+      for (int64_t i = g; i < nb; i += 16) a += part_cs[i * ldcs + c];
+    s_cs[g][col] = a;
+    __syncthreads();
+    if (g == 0 && c < ld) {
+      a = s_cs[0][col];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) a += s_cs[i][col];
+      colsum[c] = a;
+      if (!finite_f32(a)) raise_flag(flag);
+    }
+    return;
+  }
   float a = 0.f;
   for (int64_t i = threadIdx.x; i < nb; i += 8 * 1024) {
     float v[8];
@@ -674,7 +695,10 @@ size_t distill_workspace_bytes(int prec, int64_t n, int64_t C, int64_t K) {
          up256((size_t)colsum_partials_floats(nb, cs_ld(C)) * sizeof(float));
 }
 
-// More column-sum partial rows than this are first summed in blocks of
+// Up to this many column-sum partial rows are added by the loss's last launch
+// (16 rows at a time for a column: 32 rounds).
+constexpr int64_t CS_TOGETHER = 512;
+// More than this are first summed in blocks of
 // consecutive rows, then the blocks' rows (as for the cross-entropy).
 constexpr int64_t CS_ONE_STAGE = 4096;
 
@@ -703,9 +727,12 @@ hipError_t distill_launch(int prec, DistillParams p, float* loss, float* colsum,
     e = prec == 0 ? launch_rows<float>(p, s) : prec == 1 ? launch_rows<f16>(p, s) : launch_rows<bf16>(p, s);
   }
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(distill_final_kernel, dim3(1), dim3(1024), 0, s, p.part_loss, nb, p.loss_factor, loss, p.flag);
+  // few partials: the column sums in the launch that adds up the loss
+  const bool together = colsum && nb <= CS_TOGETHER;
+  hipLaunchKernelGGL(distill_final_kernel, dim3(together ? 1 + (unsigned)((p.ld + 63) / 64) : 1), dim3(1024), 0, s,
+                     p.part_loss, nb, p.loss_factor, loss, p.flag, p.part_cs, p.ldcs, p.C, p.ld, colsum);
   e = hipGetLastError();
-  if (e != hipSuccess || !colsum) return e;
+  if (e != hipSuccess || !colsum || together) return e;
   Epilogue eb{};
   eb.out = colsum; eb.ldo = p.ld; eb.rows = 1; eb.cols = p.C; eb.mode = EPI_F32; eb.flag = p.flag;
   eb.keep_scale = 1.f;

@@ -389,6 +389,8 @@ class GCN2:
                 or not (top_values.is_contiguous() and top_classes.is_contiguous())
                 or top_values.device != dev or top_classes.device != dev):
             raise ValueError(f"a teacher is two contiguous tensors {self.n} x K on {dev}: scores and int32 classes")
+        if not 1 <= top_values.shape[1] <= G.MAX_TOP:
+            raise ValueError(f"a teacher has 1 to {G.MAX_TOP} scores a row")
         n_mask = self.n
         if mask is not None:
             mask = torch.as_tensor(mask).to(dev, torch.uint8).contiguous()

@@ -167,6 +167,9 @@ def test_refusals():
             m.set_teacher(v, c)
     with pytest.raises(ValueError):
         m.set_teacher(tv, tc, mask=np.ones(7, np.uint8))
+    wide = torch.zeros((m.n, 264), dtype=tv.dtype, device="cuda")
+    with pytest.raises(ValueError):
+        m.set_teacher(wide, wide.to(torch.int32))
     u = torch.rand(m.n, device="cuda")
     for bad in (dict(u=u.double()), dict(u=u[1:]), dict(labels=m.labels.long()), dict(mask=m.labels),
                 dict(prob=u.half()), dict(u=u.cpu())):
