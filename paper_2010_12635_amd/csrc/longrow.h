@@ -1,6 +1,8 @@
 // Rows of class scores too long for a lane group: a workgroup of NT threads
 // takes a row and reads it once from memory and then, a few passes more, from
-// its die's L2 (one row a compute unit: 32 rows share 4 MiB).
+// its die's L2 (one row a compute unit: 32 rows share 4 MiB).  Against keeping
+// the row in registers (8 vectors a thread, unrolled passes that spill): top 64
+// of 2048 rows of 50001 bf16 classes 122 and 221 us.
 #pragma once
 
 #include "sorted.h"
@@ -25,7 +27,8 @@ struct LongRow {
     else return (v * NT + (int)threadIdx.x) * VE;
   }
   // f(scores of a vector, its first class) for the vectors of the thread, four
-  // loads in flight.  Every lane takes part in each call; past the row's end it
+  // loads in flight (eight: 80 us instead of 76 for the case above, 48 instead of
+  // 35 for rows of 4001 fp32 classes).  Every lane takes part in each call; past the row's end it
   // gets scores of -inf.
   template <typename F>
   __device__ __forceinline__ void each(F f) const {

@@ -3,7 +3,12 @@
 // which no two are equal, so that ties need no care.
 //
 // Bound by the read of the scores; what has to be kept small is the number of
-// comparisons a score takes part in.
+// comparisons a score takes part in.  Measured on MI355X, whole calls, against
+// what a copy of as many bytes takes: 2^21 rows of 64 classes, fp16, K = 8 90 us
+// (71); 200000 rows of 40, fp32, K = 5 15.5 us (8); 2048 rows of 50001, bf16, K =
+// 64 77 us (40; two passes, the second from L2); one row of 131072, fp32, K = 100
+// 17.6 us, what one compute unit takes to read it (cut into 16 segments whose
+// lists a second launch joins: 21 us).
 #include <algorithm>
 
 #include "internal.h"
@@ -62,6 +67,9 @@ __device__ __forceinline__ void list_levels(I (&a)[L]) {
 // group ends with the row's list.  (Shorter lists are joined whole until they
 // have L items.)
 // L = 0: the row is sorted over the group.
+//
+// Two vectors a lane against one: 90 and 117 us for 2^21 rows of 64 fp16 classes,
+// K = 8 (half the exchanges between lanes).
 template <typename T, int LPR, int L, int R>
 __global__ __launch_bounds__(256) void top_group_kernel(TopParams p) {
   constexpr int VE = Vec<T>::N, N = 2 * VE;
