@@ -100,57 +100,8 @@ template <typename T> __device__ __forceinline__ uint32_t bits_neg_inf();
 template <> __device__ __forceinline__ uint32_t bits_neg_inf<f16>() { return 0xfc00u; }
 template <> __device__ __forceinline__ uint32_t bits_neg_inf<bf16>() { return 0xff80u; }
 
-// The items of 16 bytes of scores from class c0 on, the first nv of them (none
-// if nv is negative) in the row.  Returns whether one was NaN (then absent) or +inf.
-template <typename T>
-__device__ __forceinline__ bool make_items(uint4 raw, int c0, int nv, Item32 (&a)[8]) {
-  bool bad = false;
-  uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-  if (packed_nonfinite<T>(raw)) {                      // rare: -inf, or something to report
-    float v[8];
-    unpack<T>(raw, v);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (i < nv && !(v[i] < INFINITY)) bad = true;
-      const int sh = 16 * (i & 1);
-      if (v[i] != v[i]) w[i / 2] = (w[i / 2] & ~(0xffffu << sh)) | bits_neg_inf<T>() << sh;
-    }
-  }
-#pragma unroll
-  for (int h = 0; h < 4; ++h) {
-    // both halves at once: x ^ (negative ? 0xffff : 0x8000)
-    const uint32_t s = (w[h] >> 15) & 0x00010001u;
-    const uint32_t k = w[h] ^ (((s << 15) - s) | 0x80008000u);
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const int i = 2 * h + q;
-      uint32_t v = q ? k & 0xffff0000u : k << 16;
-      v = v == 0x7fff0000u ? 0x80000000u : v;          // -0 as +0
-      v |= 0xffffu - (uint32_t)(c0 + i);
-      a[i].v = i < nv ? v : 0u;
-    }
-  }
-  return bad;
-}
-template <typename T>
-__device__ __forceinline__ bool make_items(uint4 raw, int c0, int nv, Item64 (&a)[4]) {
-  bool bad = false;
-  float z[4];
-  unpack<float>(raw, z);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const bool here = i < nv;
-    bad |= here && !(z[i] < INFINITY);
-    const bool none = !here || z[i] != z[i];
-    a[i] = item64(none ? 0u : score_key(z[i]), (uint32_t)(c0 + i));
-  }
-  return bad;
-}
-
-// The same for scores that may be anything: NaN takes its place by its bits,
-// above +inf or below -inf, where item_regular() sees it.  p: the items of
-// consecutive vectors, one after the other.
-__device__ __forceinline__ uint32_t plus_zero(f16, uint32_t w) {   // -0 as +0, both halves
+// -0 as +0, both halves of a word.
+__device__ __forceinline__ uint32_t plus_zero(f16, uint32_t w) {
   typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
   f16x2 h;
   __builtin_memcpy(&h, &w, 4);
@@ -162,6 +113,8 @@ __device__ __forceinline__ uint32_t plus_zero(bf16, uint32_t w) {
   w = (w & 0xffffu) == 0x8000u ? w & 0xffff0000u : w;
   return w >> 16 == 0x8000u ? w & 0xffffu : w;
 }
+// The items of 16 bytes of scores from class c0 on.  NaN takes its place by its
+// bits, above +inf or below -inf, where items_regular() sees it.
 template <typename T>
 __device__ __forceinline__ void order_items(uint4 raw, int c0, Item32* p) {
   const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
@@ -180,6 +133,26 @@ __device__ __forceinline__ void order_items(uint4 raw, int c0, Item64* p) {
   unpack<float>(raw, z);
 #pragma unroll
   for (int i = 0; i < 4; ++i) p[i] = item64(score_key(z[i]), (uint32_t)(c0 + i));
+}
+// The items of 16 bytes of scores from class c0 on; NaN is absent.
+template <typename T>
+__device__ __forceinline__ void make_items(uint4 raw, int c0, Item32 (&a)[8]) {
+  uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+  float v[8];
+  unpack<T>(raw, v);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int sh = 16 * (i & 1);
+    if (v[i] != v[i]) w[i / 2] = (w[i / 2] & ~(0xffffu << sh)) | bits_neg_inf<T>() << sh;
+  }
+  order_items<T>(make_uint4(w[0], w[1], w[2], w[3]), c0, a);
+}
+template <typename T>
+__device__ __forceinline__ void make_items(uint4 raw, int c0, Item64 (&a)[4]) {
+  float z[4];
+  unpack<float>(raw, z);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) a[i] = item64(z[i] != z[i] ? KEY_NEG_INF : score_key(z[i]), (uint32_t)(c0 + i));
 }
 // Whether the row with these largest and smallest items holds neither NaN nor
 // +inf.

@@ -4,8 +4,8 @@
 //
 // Bound by the read of the scores; what has to be kept small is the number of
 // comparisons a score takes part in.  Measured on MI355X, whole calls, against
-// what a copy of as many bytes takes: 2^21 rows of 64 classes, fp16, K = 8 90 us
-// (71); 200000 rows of 40, fp32, K = 5 15.5 us (8); 2048 rows of 50001, bf16, K =
+// what a copy of as many bytes takes: 2^21 rows of 64 classes, fp16, K = 8 86 us
+// (71); 200000 rows of 40, fp32, K = 5 16 us (8); 2048 rows of 50001, bf16, K =
 // 64 77 us (40; two passes, the second from L2); one row of 131072, fp32, K = 100
 // 17.6 us, what one compute unit takes to read it (cut into 16 segments whose
 // lists a second launch joins: 21 us).
@@ -68,8 +68,9 @@ __device__ __forceinline__ void list_levels(I (&a)[L]) {
 // have L items.)
 // L = 0: the row is sorted over the group.
 //
-// Two vectors a lane against one: 90 and 117 us for 2^21 rows of 64 fp16 classes,
-// K = 8 (half the exchanges between lanes).
+// For 2^21 rows of 64 fp16 classes, K = 8: two vectors a lane 90 us, one 117 (twice
+// the exchanges between lanes); with the test for NaN at the ends of the sorted
+// vectors, where it costs two comparisons, instead of at every score 86.
 template <typename T, int LPR, int L, int R>
 __global__ __launch_bounds__(256) void top_group_kernel(TopParams p) {
   constexpr int VE = Vec<T>::N, N = 2 * VE;
@@ -88,19 +89,32 @@ __global__ __launch_bounds__(256) void top_group_kernel(TopParams p) {
       int64_t row = first + r * RG + slot;
       row = row < p.n ? row : p.n - 1;               // in bounds; not stored below
 #pragma unroll
-      for (int v = 0; v < 2; ++v) raw[r][v] = ldg16(logits + row * p.ld + (col0 + v * VE < C ? col0 + v * VE : 0));
+      for (int v = 0; v < 2; ++v) raw[r][v] = load_row(logits + row * p.ld, col0 + v * VE, C, -INFINITY);
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int64_t row = first + r * RG + slot;
       const bool row_ok = row < p.n;
+      // both vectors in order; what is not a score stands at an end: +inf and
+      // NaN without sign in front, NaN with a sign behind (absent already)
       I a[2][VE];
+      bool odd = false;
 #pragma unroll
-      for (int v = 0; v < 2; ++v) bad |= make_items<T>(raw[r][v], col0 + v * VE, C - col0 - v * VE, a[v]);
+      for (int v = 0; v < 2; ++v) {
+        order_items<T>(raw[r][v], col0 + v * VE, a[v]);
+        sort_items<VE>(a[v]);
+        odd |= !items_regular<T>(a[v][0], a[v][VE - 1]);
+      }
+      if (__ballot(odd)) {                           // rare: again, without NaN
+        bad |= odd;
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          make_items<T>(raw[r][v], col0 + v * VE, a[v]);
+          sort_items<VE>(a[v]);
+        }
+      }
       if constexpr (L > 0) {
         I list[L];
-        sort_items<VE>(a[0]);
-        sort_items<VE>(a[1]);
         // the lane's own list: its two halves joined, or the larger part of both
         constexpr int H = N < L ? N : L;             // items in use
         if constexpr (L > VE) {
@@ -132,8 +146,13 @@ __global__ __launch_bounds__(256) void top_group_kernel(TopParams p) {
       } else {
         I s[N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) s[i] = a[i / VE][i % VE];
-        group_sort<LPR, N>(s, li);
+        for (int i = 0; i < VE; ++i) {               // the second half mirrored: larger parts in front
+          s[i] = item_max(a[0][i], a[1][VE - 1 - i]);
+          s[VE + i] = item_min(a[0][i], a[1][VE - 1 - i]);
+        }
+        merge_bitonic<VE>(s);
+        merge_bitonic<VE>(s + VE);
+        group_merge_levels<LPR, N, 2>(s, li);
 #pragma unroll
         for (int i = 0; i < N; ++i)
           if (row_ok && col0 + i < p.K) put_entry<T>(p, row, col0 + i, s[i]);

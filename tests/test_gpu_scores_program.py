@@ -215,3 +215,36 @@ def test_spread_scores(C, prec):
             # see check_sample in test_gpu_scores.py
             assert (np.abs(pr.double().cpu().numpy() - wp) <= 2.0 ** -17 * wp).all()
     assert ov.item() == 0
+
+
+@pytest.mark.parametrize("prec", [0, 1, 2])
+@pytest.mark.parametrize("C", [7, 64, 300, 5000])
+def test_nan_of_either_sign(C, prec):
+    """NaN is no score whatever its sign and payload: left out of the top
+    scores, no label drawn from its row, reported by both."""
+    n, K, ld = 6, 5, round8(C)
+    rng = np.random.default_rng(C)
+    z = torch.as_tensor(rng.standard_normal((n, ld)).astype(np.float32)).cuda().to(G.torch_dtype(prec))
+    bits = z.view(torch.int32 if prec == 0 else torch.int16)
+    quiet = {0: 0x7FC00001, 1: 0x7E01, 2: 0x7FC1}[prec]
+    low = -(1 << 31) if prec == 0 else -(1 << 15)
+    bits[1, C // 2] = quiet
+    bits[3, C - 1] = quiet + low                     # the same with a sign
+    ov = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for row, flagged in ((1, True), (3, True), (2, False)):
+        ov.zero_()
+        one = z[row:row + 1].contiguous()
+        ws = torch.empty(max(G.gcn_top_logits_workspace_size(1, C, K, prec),
+                             G.gcn_sample_labels_workspace_size(1, C, prec)), dtype=torch.uint8, device="cuda")
+        v = torch.zeros((1, 8), dtype=z.dtype, device="cuda")
+        c = torch.zeros((1, 8), dtype=torch.int32, device="cuda")
+        G.gcn_top_logits(1, C, ld, prec, one, K, 8, v, c, ov, ws)
+        wv, wc = S.top_logits(one[:, :C].double().cpu().numpy(), K)
+        assert np.array_equal(c[:, :K].cpu().numpy(), wc) and np.array_equal(v[:, :K].double().cpu().numpy(), wv)
+        assert ov.item() == int(flagged)
+        for k, p in ((0, 1.0), (0, 0.9), (3, 0.9)):
+            ov.zero_()
+            y = torch.zeros(1, dtype=torch.int32, device="cuda")
+            u = torch.full((1,), 0.5, device="cuda")
+            G.gcn_sample_labels(1, C, ld, prec, one, None, u, 1.0, k, p, 0.0, y, None, ov, ws)
+            assert (y.item() == -1) == flagged and ov.item() == int(flagged)
