@@ -59,6 +59,7 @@ __global__ __launch_bounds__(256) void distill_group_kernel(DistillParams p) {
   float acc_cs[VE];
 #pragma unroll
   for (int i = 0; i < VE; ++i) { acc_cs[i] = 0.f; mine[col0 + i] = 0.f; }
+  wave_sync();
   const float k = LOG2E * p.inv_T;
   const float sc = p.scale * (p.loss_scale ? *p.loss_scale : 1.f);
   bool bad = false;

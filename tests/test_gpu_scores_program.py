@@ -248,3 +248,29 @@ def test_nan_of_either_sign(C, prec):
             u = torch.full((1,), 0.5, device="cuda")
             G.gcn_sample_labels(1, C, ld, prec, one, None, u, 1.0, k, p, 0.0, y, None, ov, ws)
             assert (y.item() == -1) == flagged and ov.item() == int(flagged)
+
+
+@pytest.mark.parametrize("C", [7, 64, 3000])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_teacher_that_is_not_finite(C, value):
+    """A teacher's NaN or +inf makes the loss non-finite and is reported; rows
+    outside the mask are not looked at."""
+    n, K, ld = 5, 3, round8(C)
+    z = torch.zeros((n, ld), device="cuda")
+    v = torch.zeros((n, 8), device="cuda")
+    c = torch.full((n, 8), -1, dtype=torch.int32, device="cuda")
+    c[:, :K] = torch.arange(K, device="cuda")
+    v[2, 1] = value
+    ws = torch.empty(G.gcn_distill_workspace_size(n, C, K, 0), dtype=torch.uint8, device="cuda")
+    mask = torch.ones(n, dtype=torch.uint8, device="cuda")
+    for out in (False, True):
+        mask[2] = 0 if out else 1
+        ov = torch.zeros(1, dtype=torch.int32, device="cuda")
+        loss, d = torch.zeros(1, device="cuda"), torch.zeros((n, ld), device="cuda")
+        G.gcn_distill(n, C, ld, 0, z, K, 8, 0, v, c, mask, n - out, 1.0, 1.0, None, None, loss, d, ov, ws)
+        assert ov.item() == (0 if out else 1)
+        assert bool(torch.isfinite(loss).item()) == out
+        # K of C equal scores named: ln(C / K)
+        if out:
+            assert abs(loss.item() - np.log(C / K)) < 1e-6 * np.log(C)
+            assert torch.isfinite(d[:, :C]).all() and (d[2] == 0).all()
