@@ -10,7 +10,7 @@
 //
 // Bound by the read of the scores (and the base) and the write of the gradient.
 // Measured on MI355X, whole calls, against what a copy of as many bytes takes:
-// 2^21 rows of 64 classes, fp16, 8 entries, with base and column sums 212 us
+// 2^21 rows of 64 classes, fp16, 8 entries, with base and column sums 203 us
 // (175); 2048 rows of 50001, bf16 117 us (79); 200000 rows of 40, fp32, with
 // base and column sums 34 us (21); 12 rows of 131072, fp32 16.5 us, two of its
 // three launches the segments' two passes.
@@ -601,12 +601,12 @@ __global__ __launch_bounds__(1024) void distill_final_kernel(const float* __rest
   }
 }
 
-// Entries a lane holds: up to 4 (2^21 rows of 64 classes, 32 entries, fp16: 327 us,
-// read again whenever needed 654).
-// Workgroups and rows per iteration as in the cross-entropy kernel: R = 4
-// rows a group when one would give more than 16384 workgroups, and at most
-// 65536 workgroups, each walking on.
-constexpr int64_t R4_GROUPS = 16384, MAX_BLOCKS = 65536;
+// Entries a lane holds: up to 4 (2^21 rows of 64 classes, 32 entries, fp16: 292 us,
+// read again whenever needed about twice that).
+// Rows a group takes per iteration: 2 when one would give more than 16384
+// workgroups (2^21 rows of 64 fp16 classes: 203 us, 4 rows 214: fewer waves hold
+// the registers of 4), and at most 65536 workgroups, each walking on.
+constexpr int64_t R2_GROUPS = 16384, MAX_BLOCKS = 65536;
 
 int vec_elems(int prec) { return prec == 0 ? 4 : 8; }
 bool in_group(int prec, int64_t C) { return C <= 64 * vec_elems(prec); }
@@ -620,7 +620,7 @@ int64_t blocks_of(int64_t n, int64_t rows) {
   const int64_t nb = (n + rows - 1) / rows;
   return nb < MAX_BLOCKS ? nb : MAX_BLOCKS;
 }
-int rows_per_group(int64_t n, int64_t rg) { return (n + rg - 1) / rg > R4_GROUPS ? 4 : 1; }
+int rows_per_group(int64_t n, int64_t rg) { return (n + rg - 1) / rg > R2_GROUPS ? 2 : 1; }
 int64_t group_blocks(int prec, int64_t n, int64_t C) {
   const int64_t rg = 4 * (64 / lanes_per_row(prec, C));
   return blocks_of(n, rows_per_group(n, rg) * rg);
@@ -629,8 +629,8 @@ int64_t group_blocks(int prec, int64_t n, int64_t C) {
 template <typename T, int LPR, int KPL>
 hipError_t launch_one(const DistillParams& p, int64_t nb, hipStream_t s) {
   constexpr int64_t RG = 4 * (64 / LPR);
-  if (rows_per_group(p.n, RG) == 4)
-    hipLaunchKernelGGL((distill_group_kernel<T, LPR, 4, KPL>), dim3((unsigned)nb), dim3(256), 0, s, p);
+  if (rows_per_group(p.n, RG) == 2)
+    hipLaunchKernelGGL((distill_group_kernel<T, LPR, 2, KPL>), dim3((unsigned)nb), dim3(256), 0, s, p);
   else
     hipLaunchKernelGGL((distill_group_kernel<T, LPR, 1, KPL>), dim3((unsigned)nb), dim3(256), 0, s, p);
   return hipGetLastError();
