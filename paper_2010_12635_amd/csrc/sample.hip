@@ -350,7 +350,8 @@ struct LongShared {
   double bin[BINS];
   double item[MEMBERS], weight[MEMBERS];
   double d[NT / 64], rest[NT / 64];
-  float f[NT / 64];
+  float f[NT / 64];                                      // the waves' maxima: written once a row
+  float low[NT / 64];
   uint32_t u[NT / 64];
   int n[NT / 64];
   int count, hit, doubt;
@@ -460,7 +461,8 @@ struct LongSample {
 #pragma unroll
         for (int i = 0; i < VE; ++i) low = v[i] > -INFINITY ? fminf(low, v[i]) : low;
       });
-      const float range = zmax - block_reduce<NW>(low, sh.f, MinF());
+      // not in sh.f: a wave may still be reading the maxima there
+      const float range = zmax - block_reduce<NW>(low, sh.low, MinF());
       scale = range > 0.f && range < INFINITY ? (float)BINS / range : 0.f;
       scale = scale < INFINITY ? scale : 0.f;
     }

@@ -1,0 +1,50 @@
+"""Long rows' draws where the waves of a workgroup are far apart in time: rows
+just past a lane group's width, where a pass over the row is a few
+instructions, and as many rows at once as the chip holds, each with scores of
+its own level, so that what one wave takes from another at the wrong moment
+changes the answer.  Labels against the float64 oracle, and the same bits in
+every repetition."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import scores_oracle as S
+from paper_2010_12635_amd import gcn as G
+from paper_2010_12635_amd.model import round8
+
+pytestmark = pytest.mark.gpu
+
+
+def draws(z, C, prec, u, T, k, p, m):
+    n = z.shape[0]
+    ws = torch.empty(G.gcn_sample_labels_workspace_size(n, C, prec), dtype=torch.uint8, device="cuda")
+    ov = torch.zeros(1, dtype=torch.int32, device="cuda")
+    out = []
+    for _ in range(4):
+        y = torch.full((n,), -7, dtype=torch.int32, device="cuda")
+        pr = torch.full((n,), -7.0, device="cuda")
+        G.gcn_sample_labels(n, C, z.shape[1], prec, z, None, u, T, k, p, m, y, pr, ov, ws)
+        out.append((y, pr))
+    assert ov.item() == 0
+    for y, pr in out[1:]:
+        assert torch.equal(y, out[0][0]) and torch.equal(pr, out[0][1])
+    return out[0]
+
+
+@pytest.mark.parametrize("prec", [0, 1, 2])
+def test_many_short_rows_under_top_k(prec):
+    """256 < top_k < C: the lowest score of the row is looked for right after
+    its largest."""
+    n, C = 1500, 1025 if prec else 513
+    k = 260 if prec == 0 else 500
+    rng = np.random.default_rng(prec)
+    z = rng.standard_normal((n, C)) * 2 + 20 * rng.standard_normal((n, 1))
+    zt = torch.full((n, round8(C)), float("nan"), dtype=G.torch_dtype(prec), device="cuda")
+    zt[:, :C] = torch.as_tensor(z.astype(np.float32)).cuda().to(zt.dtype)
+    zh = zt[:, :C].double().cpu().numpy()
+    u = rng.random(n).astype(np.float32)
+    for p, T in ((1.0, 1.0), (0.9, 2.0)):
+        print(f"[waves] top_k={k} prec={prec} p={p} T={T}", flush=True)
+        y, _ = draws(zt, C, prec, torch.as_tensor(u).cuda(), T, k, p, 0.0)
+        wy, _ = S.sample_labels(zh, u.astype(np.float64), T, k, float(np.float32(p)), 0.0)
+        assert np.array_equal(y.cpu().numpy(), wy)
