@@ -875,6 +875,7 @@ __global__ __launch_bounds__(NT, 4) void sample_row_kernel(SampleParams p) {
     }
   }
   if (q.run(u, label, prob)) return;
+  __syncthreads();                                       // every wave has seen the doubt: it is cleared next
   LongSample<double, Row>{p, r, sh, zmax}.run(u, label, prob);
 }
 

@@ -48,3 +48,24 @@ def test_many_short_rows_under_top_k(prec):
         y, _ = draws(zt, C, prec, torch.as_tensor(u).cuda(), T, k, p, 0.0)
         wy, _ = S.sample_labels(zh, u.astype(np.float64), T, k, float(np.float32(p)), 0.0)
         assert np.array_equal(y.cpu().numpy(), wy)
+
+
+@pytest.mark.parametrize("prec", [0, 1, 2])
+@pytest.mark.parametrize("C", [1025, 2049, 9001])
+def test_doubt_without_a_border(C, prec):
+    """No top-k and no top-p: every row's u lies on a running sum exactly, so
+    that the draw in 32 bits is in doubt and the one in 64 bits follows it at
+    once.  Scores are equal in a power of two of classes and out of the row in
+    the others: the answers are whole numbers."""
+    n, half = 700, 512
+    print(f"[waves] doubt C={C} prec={prec}", flush=True)
+    rng = np.random.default_rng(C)
+    z = np.full((n, C), -np.inf)
+    at = np.stack([np.sort(rng.permutation(C)[:half]) for _ in range(n)])
+    z[np.arange(n)[:, None], at] = rng.integers(-3, 4, (n, 1))
+    zt = torch.full((n, round8(C)), float("nan"), dtype=G.torch_dtype(prec), device="cuda")
+    zt[:, :C] = torch.as_tensor(z.astype(np.float32)).cuda().to(zt.dtype)
+    j = rng.integers(0, half, n)
+    y, pr = draws(zt, C, prec, torch.as_tensor((j / half).astype(np.float32)).cuda(), 0.5, 0, 1.0, 0.0)
+    assert np.array_equal(y.cpu().numpy(), at[np.arange(n), j])
+    assert (pr == 1 / half).all()
