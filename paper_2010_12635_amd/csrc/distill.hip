@@ -268,17 +268,18 @@ __device__ __forceinline__ float scaled(float z, float k) {
   return z * k;
 }
 
-// A reference M and a sum of powers relative to it (0 where M is -inf).
+// A reference m and a sum of powers 2^((z - m) k) relative to it (0 where m is
+// -inf).
 struct MaxSum { float m, s; };
-__device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b) {
+__device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b, float k) {
   const float m = fmaxf(a.m, b.m);
-  const float fa = a.m > -INFINITY ? __builtin_amdgcn_exp2f(a.m - m) : 0.f;
-  const float fb = b.m > -INFINITY ? __builtin_amdgcn_exp2f(b.m - m) : 0.f;
+  const float fa = a.m > -INFINITY ? __builtin_amdgcn_exp2f((a.m - m) * k) : 0.f;
+  const float fb = b.m > -INFINITY ? __builtin_amdgcn_exp2f((b.m - m) * k) : 0.f;
   return {m, a.s * fa + b.s * fb};                   // a NaN stays in s
 }
-__device__ __forceinline__ MaxSum wave_join(MaxSum v) {
+__device__ __forceinline__ MaxSum wave_join(MaxSum v, float k) {
   const float m = group_max<64>(v.m);
-  v.s *= v.m > -INFINITY ? __builtin_amdgcn_exp2f(v.m - m) : 0.f;
+  v.s *= v.m > -INFINITY ? __builtin_amdgcn_exp2f((v.m - m) * k) : 0.f;
   return {m, group_sum<64>(v.s)};
 }
 
@@ -342,9 +343,8 @@ struct Entry {
   __device__ __forceinline__ void share(EntryTable& tab, float k) const {
     const int w = threadIdx.x >> 6;
     if (w >= TW) return;
-    const float m = scaled(t, k);
     const bool some = __ballot(c >= 0) != 0;
-    const MaxSum a = wave_join(MaxSum{c >= 0 ? m : -INFINITY, c < 0 ? 0.f : m == m ? 1.f : m});
+    const MaxSum a = wave_join(MaxSum{t, c < 0 ? 0.f : t == t ? 1.f : t}, k);   // absent: t = -inf
     if ((threadIdx.x & 63) == 0) { tab.part[w] = a; tab.some[w] = some ? 1 : 0; }
     tab.c[threadIdx.x] = c;
   }
@@ -357,8 +357,11 @@ struct Entry {
     if (w >= TW) return;
     MaxSum r = tab.part[0];
 #pragma unroll
-    for (int i = 1; i < TW; ++i) r = join(r, tab.part[i]);
-    const float y = fmaf(t, k, -r.m);                  // log2 of q r
+    for (int i = 1; i < TW; ++i) r = join(r, tab.part[i], k);
+    // Subtracted first, as in the sum: t k rounded on its own would be off by
+    // 2^-24 t k, another amount in q than in the sum, and the q would not sum to
+    // 1 (fp16 scores near 60000 at the lowest temperature: one entry's q was 16)
+    const float y = (t - r.m) * k;                     // log2 of q r
     const float q = c >= 0 ? __builtin_amdgcn_exp2f(y) / r.s : 0.f;
     tab.q[threadIdx.x] = q;
     // sum of q (log2 q - log2 p): an entry of weight 0 adds nothing
@@ -445,12 +448,12 @@ __global__ __launch_bounds__(NT, 4) void distill_row_kernel(DistillParams p) {
     mine.s += vector_sum<T>(raw[v], M, k);
     forget(raw[v]);
   }
-  mine = wave_join(mine);
+  mine = wave_join(mine, 1.f);
   if (lane == 0) s_part[wave] = mine;
   __syncthreads();
   MaxSum all = s_part[0];
 #pragma unroll
-  for (int i = 1; i < NW; ++i) all = join(all, s_part[i]);
+  for (int i = 1; i < NW; ++i) all = join(all, s_part[i], 1.f);
   const bool counts = e.counts(s_tab);
   e.weigh(s_tab, all, k);
   const float sc = p.scale * (p.loss_scale ? *p.loss_scale : 1.f);
@@ -504,12 +507,12 @@ __global__ __launch_bounds__(256) void distill_part_kernel(DistillParams p) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) mine.s += vector_sum<T>(raw[q], M, k);
   }
-  mine = wave_join(mine);
+  mine = wave_join(mine, 1.f);
   if ((t & 63) == 0) s_part[t >> 6] = mine;
   __syncthreads();
   if (t == 0) {
     MaxSum a = s_part[0];
-    for (int i = 1; i < 4; ++i) a = join(a, s_part[i]);
+    for (int i = 1; i < 4; ++i) a = join(a, s_part[i], 1.f);
     reinterpret_cast<MaxSum*>(p.part_ms)[blockIdx.x] = a;
   }
 }
@@ -533,8 +536,8 @@ __global__ __launch_bounds__(256) void distill_segment_kernel(DistillParams p) {
   // the row's reference and sum, by every wave: its segments a lane each, in turn
   const MaxSum* part = reinterpret_cast<const MaxSum*>(p.part_ms) + g.row * p.segs;
   MaxSum all{-INFINITY, 0.f};
-  for (int i = t & 63; i < p.segs; i += 64) all = join(all, part[i]);
-  all = wave_join(all);
+  for (int i = t & 63; i < p.segs; i += 64) all = join(all, part[i], 1.f);
+  all = wave_join(all, 1.f);
   __syncthreads();                                   // the table is there, the base's entries are read
   const bool counts = e.counts(s_tab);
   e.weigh(s_tab, all, k);
