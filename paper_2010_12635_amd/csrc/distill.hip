@@ -258,15 +258,10 @@ __global__ __launch_bounds__(256) void distill_group_kernel(DistillParams p) {
 // workgroup each: first every segment's maximum and sum of exponentials, then,
 // from those of the whole row, its part of the gradient.
 
-// With k = log2(e) / T everything is in powers of 2: M = k max z as rounded, X_c
-// = z_c k - M (one rounding), p_c = 2^X_c / S, S = sum of the 2^X_c.
-
-// z k rounded on its own: a product that the compiler joins with a later
-// subtraction would make M - M what the rounding left.
-__device__ __forceinline__ float scaled(float z, float k) {
-#pragma clang fp contract(off)
-  return z * k;
-}
+// With k = log2(e) / T powers are of 2: p_c = 2^((z_c - M) k) / S, M = max z.  The
+// difference is taken before the product: z k could leave the range (the lowest
+// finite number is a score), and M k rounded on its own would be off by more than
+// the powers' own exponents where |M| / T is large.
 
 // A reference m and a sum of powers 2^((z - m) k) relative to it (0 where m is
 // -inf).
@@ -292,14 +287,14 @@ __device__ __forceinline__ float vector_max(uint4 raw) {
   for (int i = 1; i < Vec<T>::N; ++i) m = fmaxf(m, v[i]);
   return m;
 }
-// Sum of 2^(z k - M); a lane that has seen only -inf takes M = 0.
+// Sum of 2^((z - M) k); a lane that has seen only -inf takes M = 0.
 template <typename T>
 __device__ __forceinline__ float vector_sum(uint4 raw, float M, float k) {
   float v[Vec<T>::N];
   unpack<T>(raw, v);
   float s = 0.f;
 #pragma unroll
-  for (int i = 0; i < Vec<T>::N; ++i) s += __builtin_amdgcn_exp2f(fmaf(v[i], k, -M));
+  for (int i = 0; i < Vec<T>::N; ++i) s += __builtin_amdgcn_exp2f((v[i] - M) * k);
   return s;
 }
 // Keeps the compiler from holding unpacked scores between two passes.
@@ -352,7 +347,7 @@ struct Entry {
     return (tab.some[0] | tab.some[1] | tab.some[2] | tab.some[3]) != 0;
   }
   // The weights, and the waves' parts of the row's loss, to shared memory.
-  __device__ __forceinline__ void weigh(EntryTable& tab, MaxSum row, float k) const {
+  __device__ __forceinline__ void weigh(EntryTable& tab, MaxSum row, float k, float inv_T) const {
     const int w = threadIdx.x >> 6;
     if (w >= TW) return;
     MaxSum r = tab.part[0];
@@ -364,28 +359,28 @@ struct Entry {
     const float y = (t - r.m) * k;                     // log2 of q r
     const float q = c >= 0 ? __builtin_amdgcn_exp2f(y) / r.s : 0.f;
     tab.q[threadIdx.x] = q;
-    // sum of q (log2 q - log2 p): an entry of weight 0 adds nothing
-    const float a = q > 0.f || q != q ? q * (y - fmaf(z, k, -row.m)) : 0.f;
-    const float sum = group_sum<64>(a);
-    if ((threadIdx.x & 63) == 0) tab.loss[w] = w == 0 ? sum - log2f(r.s) + log2f(row.s) : sum;
+    // T times the sum of q (ln q r - ln p s): an entry of weight 0 adds nothing
+    const float a = q > 0.f || q != q ? q * ((t - r.m) - (z - row.m)) : 0.f;
+    const float sum = group_sum<64>(a) * inv_T;
+    if ((threadIdx.x & 63) == 0) tab.loss[w] = w == 0 ? sum - logf(r.s) + logf(row.s) : sum;
   }
   // After a barrier: the row's loss.
   static __device__ __forceinline__ float loss(const EntryTable& tab) {
-    return ((tab.loss[0] + tab.loss[1]) + (tab.loss[2] + tab.loss[3])) * 0.693147180559945309f;
+    return (tab.loss[0] + tab.loss[1]) + (tab.loss[2] + tab.loss[3]);
   }
   // After the row is written: what the entry's class gets.
   __device__ __forceinline__ bool store(const DistillParams& p, const EntryTable& tab, T* d, float base, float M, float k,
                                         float inv_s, float sc) const {
     float qs = 0.f;
     for (int j = 0; j < p.K; ++j) qs += tab.c[j] == c ? tab.q[j] : 0.f;
-    const T o = from_f32<T>((__builtin_amdgcn_exp2f(fmaf(z, k, -M)) * inv_s - qs) * sc + base);
+    const T o = from_f32<T>((__builtin_amdgcn_exp2f((z - M) * k) * inv_s - qs) * sc + base);
     d[c] = o;
     return !finite_f32(to_f32<T>(o));
   }
 };
 static_assert(TW == 4, "the waves' parts are joined by hand");
 
-// 2^(z k - M) f, added to the base, of a vector from class c0 on.  Returns
+// 2^((z - M) k) f, added to the base, of a vector from class c0 on.  Returns
 // whether an element is not finite.
 template <typename T>
 __device__ __forceinline__ bool store_gradient(T* d, const T* base, int c0, int C, uint4 raw, float M, float k, float f) {
@@ -393,7 +388,7 @@ __device__ __forceinline__ bool store_gradient(T* d, const T* base, int c0, int 
   float g[VE], v[VE];
   unpack<T>(raw, v);
 #pragma unroll
-  for (int i = 0; i < VE; ++i) g[i] = __builtin_amdgcn_exp2f(fmaf(v[i], k, -M)) * f;
+  for (int i = 0; i < VE; ++i) g[i] = __builtin_amdgcn_exp2f((v[i] - M) * k) * f;
   if (base) {
     float bv[VE];
     unpack<T>(load_row(base, c0, C, 0.f), bv);
@@ -440,7 +435,6 @@ __global__ __launch_bounds__(NT, 4) void distill_row_kernel(DistillParams p) {
   MaxSum mine{-INFINITY, 0.f};
 #pragma unroll
   for (int v = 0; v < NV; ++v) mine.m = fmaxf(mine.m, vector_max<T>(raw[v]));
-  mine.m = scaled(mine.m, k);
   const float M = mine.m > -INFINITY ? mine.m : 0.f;
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
@@ -448,14 +442,14 @@ __global__ __launch_bounds__(NT, 4) void distill_row_kernel(DistillParams p) {
     mine.s += vector_sum<T>(raw[v], M, k);
     forget(raw[v]);
   }
-  mine = wave_join(mine, 1.f);
+  mine = wave_join(mine, k);
   if (lane == 0) s_part[wave] = mine;
   __syncthreads();
   MaxSum all = s_part[0];
 #pragma unroll
-  for (int i = 1; i < NW; ++i) all = join(all, s_part[i], 1.f);
+  for (int i = 1; i < NW; ++i) all = join(all, s_part[i], k);
   const bool counts = e.counts(s_tab);
-  e.weigh(s_tab, all, k);
+  e.weigh(s_tab, all, k, p.inv_T);
   const float sc = p.scale * (p.loss_scale ? *p.loss_scale : 1.f);
   const float inv_s = 1.f / all.s;
   if (d) {
@@ -500,19 +494,19 @@ __global__ __launch_bounds__(256) void distill_part_kernel(DistillParams p) {
     float m = vector_max<T>(raw[0]);
 #pragma unroll
     for (int q = 1; q < 4; ++q) m = fmaxf(m, vector_max<T>(raw[q]));
-    m = fmaxf(mine.m, scaled(m, k));
+    m = fmaxf(mine.m, m);
     const float M = m > -INFINITY ? m : 0.f;
-    mine.s *= mine.m > -INFINITY ? __builtin_amdgcn_exp2f(mine.m - m) : 1.f;
+    mine.s *= mine.m > -INFINITY ? __builtin_amdgcn_exp2f((mine.m - m) * k) : 1.f;
     mine.m = m;
 #pragma unroll
     for (int q = 0; q < 4; ++q) mine.s += vector_sum<T>(raw[q], M, k);
   }
-  mine = wave_join(mine, 1.f);
+  mine = wave_join(mine, k);
   if ((t & 63) == 0) s_part[t >> 6] = mine;
   __syncthreads();
   if (t == 0) {
     MaxSum a = s_part[0];
-    for (int i = 1; i < 4; ++i) a = join(a, s_part[i], 1.f);
+    for (int i = 1; i < 4; ++i) a = join(a, s_part[i], k);
     reinterpret_cast<MaxSum*>(p.part_ms)[blockIdx.x] = a;
   }
 }
@@ -536,11 +530,11 @@ __global__ __launch_bounds__(256) void distill_segment_kernel(DistillParams p) {
   // the row's reference and sum, by every wave: its segments a lane each, in turn
   const MaxSum* part = reinterpret_cast<const MaxSum*>(p.part_ms) + g.row * p.segs;
   MaxSum all{-INFINITY, 0.f};
-  for (int i = t & 63; i < p.segs; i += 64) all = join(all, part[i], 1.f);
-  all = wave_join(all, 1.f);
+  for (int i = t & 63; i < p.segs; i += 64) all = join(all, part[i], k);
+  all = wave_join(all, k);
   __syncthreads();                                   // the table is there, the base's entries are read
   const bool counts = e.counts(s_tab);
-  e.weigh(s_tab, all, k);
+  e.weigh(s_tab, all, k, p.inv_T);
   const float sc = p.scale * (p.loss_scale ? *p.loss_scale : 1.f);
   const float inv_s = 1.f / all.s;
   if (d) {

@@ -92,3 +92,58 @@ def test_teacher_of_lowest_scores(n, C, prec):
         v = np.full((n, 4), LOWEST[prec])
         v[1, 2] = 1.0                             # one entry far above the others
         check(rng.standard_normal((n, C)) * min(T, 1.0), v, classes(rng, n, C, 4), prec, prec, T)
+
+
+@pytest.mark.parametrize("prec", [0, 1, 2], ids=NAMES.get)
+@pytest.mark.parametrize("n,C", SIZES)
+def test_student_of_lowest_scores(n, C, prec):
+    """Rows masked with the type's lowest number: nothing weighs there unless
+    nothing else is left, and then all weigh the same."""
+    rng = np.random.default_rng(C)
+    for T in (1.0, G.MIN_TEMPERATURE, 1.3, 3.0):
+        print(f"[range] lowest student T={T} n={n} C={C} {NAMES[prec]}", flush=True)
+        z = rng.standard_normal((n, C)) * min(T, 1.0)
+        c = classes(rng, n, C, 4)
+        v = rng.standard_normal((n, 4)) * T
+        away = rng.random((n, C)) < 0.6
+        np.put_along_axis(away, c, False, 1)
+        z[away] = LOWEST[prec]
+        z[1] = LOWEST[prec]
+        check(z, v, c, prec, prec, T)
+        check(np.full((n, C), LOWEST[prec]), v, c, prec, prec, T)
+
+
+@pytest.mark.parametrize("n,C", SIZES)
+def test_named_lowest_score(n, C):
+    """A teacher that names a class of the lowest score: a loss near the end of
+    the range, but a finite one, and a gradient of ordinary size."""
+    rng = np.random.default_rng(C)
+    for T in (1.0, 4.0):
+        print(f"[range] named T={T} n={n} C={C}", flush=True)
+        z = rng.standard_normal((n, C))
+        c = classes(rng, n, C, 3)
+        z[0, c[0, 1]] = LOWEST[0] if T == 1.0 else LOWEST[0] / 8
+        check(z, rng.standard_normal((n, 3)), c, 0, 0, T)
+
+
+@pytest.mark.parametrize("prec", [0, 2], ids=NAMES.get)
+@pytest.mark.parametrize("n,C", SIZES)
+def test_large_student(n, C, prec):
+    """Scores far from 0 whose differences are of ordinary size against the
+    temperature, and the largest numbers of both signs together."""
+    rng = np.random.default_rng(C)
+    for level, step, T in ((1.0e7, 1.0, 0.5), (-1.0e7, 1.0, 0.25), (1.0e7, 2.0 ** -9, G.MIN_TEMPERATURE),
+                           (1.0e30, 0.0, 1.0), (-3.0e38, 0.0, 0.3)):
+        print(f"[range] student {level} T={T} n={n} C={C} {NAMES[prec]}", flush=True)
+        z = level + step * rng.integers(-3, 4, (n, C))
+        c = classes(rng, n, C, 5)
+        z = np.asarray(torch.as_tensor(z.astype(np.float32)).to(G.torch_dtype(prec)).double())
+        top = z.max(1)
+        for i in range(n):                        # bf16 keeps 8 bits: the differences may be large
+            z[i, c[i]] = top[i]
+        check(z, rng.standard_normal((n, 5)) * T, c, prec, prec, T)
+    z = rng.standard_normal((n, C))
+    c = classes(rng, n, C, 2)
+    z[:, :] = -LOWEST[prec] * np.where(rng.random((n, C)) < 0.5, 1.0, -1.0)
+    z[np.arange(n)[:, None], c] = -LOWEST[prec]
+    check(z, rng.standard_normal((n, 2)), c, prec, prec, 1.0)
