@@ -36,14 +36,25 @@ namespace {
 // their own order.
 //
 // Weights and sums are in 32 bits (W = float); a border is believed only where
-// no running sum lies within DRAW_EPS of it.  With e = 2^-24: a weight's
-// exponent x = (z - max) log2(e) / T carries 3 e |x| (difference, constant,
-// product), so a sum S of weights is off by at most S (3 e ln C + 4 e) with the
-// base-2 exponential's 4 e (the mean of |x| under the weights is at most log2
-// C), its N + 7 adds by (N + 7) e, and p S or u S by 2 e: below 2^-18 S for C
-// <= 1024.  Where one does, W = double settles it, for the wave: about one wave
-// in three hundred for 64 classes a row.
-constexpr float DRAW_EPS = 3.814697265625e-6f;           // 2^-18
+// no running sum lies within DRAW_EPS of it, relative to the total S.  With e =
+// 2^-24, what a comparison of a running sum with a share q of S may be off by:
+//   weights: an exponent x = (z - max) log2(e) / T carries 3 e |x| (difference,
+//     constant, product), the base-2 exponential 4 e.  The sum up to a border
+//     less q S has every weight with a factor of at most 1, and the mean of |x|
+//     ln 2 under the weights is at most ln C: S (3 ln C + 4) e;
+//   additions, L = log2 LPR: N - 1 in the lane, L over the lanes and N on the way
+//     through the lane's own for the running sum; N - 1 and L for S;
+//   the share's product and the bound's own addition: 2 e S.
+// That is 85 e S for 1024 16-bit classes, 69 e S for 64: below 2^-17 S.  Where a
+// sum does come as close, W = double settles it, for the wave.
+constexpr float DRAW_EPS = 7.62939453125e-6f;            // 2^-17
+constexpr double draw_error(int N, int LPR) {            // in units of e S
+  double ln_c = 0.0;
+  int L = 0;
+  for (int l = LPR; l > 1; l /= 2) ++L;
+  for (int c = LPR * N; c > 1; c /= 2) ln_c += 0.69314718056;
+  return 3.0 * ln_c + 4.0 + (2 * N - 1 + L) + (N - 1 + L) + 2.0;
+}
 
 template <typename W> struct Draw;
 template <> struct Draw<float> {
@@ -75,6 +86,7 @@ template <typename W, typename T, int LPR, bool FILTER, typename I, int N>
 __device__ __forceinline__ bool group_draw(const SampleParams& p, const float (&z)[N], const I (&a)[N], const I (&s)[N],
                                            int li, float zmax, float u, int32_t& label, float& prob) {
   typedef Draw<W> D;
+  static_assert(draw_error(N, LPR) < (double)DRAW_EPS * (1 << 24), "the bound covers the comparisons");
   const int col0 = li * N;
   bool sure = true;
   I border{0};

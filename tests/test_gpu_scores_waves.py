@@ -69,3 +69,20 @@ def test_doubt_without_a_border(C, prec):
     y, pr = draws(zt, C, prec, torch.as_tensor((j / half).astype(np.float32)).cuda(), 0.5, 0, 1.0, 0.0)
     assert np.array_equal(y.cpu().numpy(), at[np.arange(n), j])
     assert (pr == 1 / half).all()
+
+
+@pytest.mark.parametrize("prec,C,n", [(1, 1024, 4000), (2, 1024, 4000), (0, 512, 4000), (1, 64, 30000)])
+def test_many_draws_in_lane_groups(prec, C, n):
+    """Thousands of rows a case, the widest rows of a lane group among them:
+    the labels are those of 64 bits, the few rows near a border too."""
+    print(f"[waves] groups n={n} C={C} prec={prec}", flush=True)
+    rng = np.random.default_rng(C + prec)
+    z = rng.standard_normal((n, C)) * np.where(np.arange(n) % 2, 3.0, 0.2)[:, None]
+    zt = torch.full((n, round8(C)), float("nan"), dtype=G.torch_dtype(prec), device="cuda")
+    zt[:, :C] = torch.as_tensor(z.astype(np.float32)).cuda().to(zt.dtype)
+    zh = zt[:, :C].double().cpu().numpy()
+    u = rng.random(n).astype(np.float32)
+    for k, p, m in ((0, 1.0, 0.0), (C // 2, 0.9, 0.0)):
+        y, _ = draws(zt, C, prec, torch.as_tensor(u).cuda(), 0.9, k, p, m)
+        wy, _ = S.sample_labels(zh, u.astype(np.float64), float(np.float32(0.9)), k, float(np.float32(p)), m)
+        assert np.array_equal(y.cpu().numpy(), wy)
