@@ -36,7 +36,7 @@ namespace {
 // their own order.
 //
 // Weights and sums are in 32 bits (W = float); a border is believed only where
-// no running sum lies within DRAW_EPS of it, relative to the total S.  With e =
+// no running sum lies within draw_eps() of it, relative to the total S.  With e =
 // 2^-24, what a comparison of a running sum with a share q of S may be off by:
 //   weights: an exponent x = (z - max) log2(e) / T carries 3 e |x| (difference,
 //     constant, product), the base-2 exponential 4 e.  The sum up to a border
@@ -45,15 +45,16 @@ namespace {
 //   additions, L = log2 LPR: N - 1 in the lane, L over the lanes and N on the way
 //     through the lane's own for the running sum; N - 1 and L for S;
 //   the share's product and the bound's own addition: 2 e S.
-// That is 85 e S for 1024 16-bit classes, 69 e S for 64: below 2^-17 S.  Where a
-// sum does come as close, W = double settles it, for the wave.
-constexpr float DRAW_EPS = 7.62939453125e-6f;            // 2^-17
-constexpr double draw_error(int N, int LPR) {            // in units of e S
+// That is 85 e S for 1024 16-bit classes, 69 e S for 64 (and a thousandth for
+// products of errors).  Where a sum does come as close, W = double settles it, for
+// the wave: with 128 e for every width 2^21 rows of 64 take 279 us instead of 271.
+constexpr float draw_eps(int N, int LPR) {
   double ln_c = 0.0;
   int L = 0;
   for (int l = LPR; l > 1; l /= 2) ++L;
   for (int c = LPR * N; c > 1; c /= 2) ln_c += 0.69314718056;
-  return 3.0 * ln_c + 4.0 + (2 * N - 1 + L) + (N - 1 + L) + 2.0;
+  const double in_e = 3.0 * ln_c + 4.0 + (2 * N - 1 + L) + (N - 1 + L) + 2.0;
+  return (float)(in_e * 1.001 / (1 << 24));
 }
 
 template <typename W> struct Draw;
@@ -61,13 +62,11 @@ template <> struct Draw<float> {
   static __device__ __forceinline__ float weight(float z, float zmax, const SampleParams& p) {
     return __builtin_amdgcn_exp2f((z - zmax) * p.k);
   }
-  static constexpr float EPS = DRAW_EPS;
 };
 template <> struct Draw<double> {
   static __device__ __forceinline__ double weight(float z, float zmax, const SampleParams& p) {
     return exp(((double)z - (double)zmax) / p.T);
   }
-  static constexpr double EPS = 0.0;
 };
 
 // The smallest score that min-p keeps.  (double)z >= max + T ln(min_p) holds
@@ -86,7 +85,7 @@ template <typename W, typename T, int LPR, bool FILTER, typename I, int N>
 __device__ __forceinline__ bool group_draw(const SampleParams& p, const float (&z)[N], const I (&a)[N], const I (&s)[N],
                                            int li, float zmax, float u, int32_t& label, float& prob) {
   typedef Draw<W> D;
-  static_assert(draw_error(N, LPR) < (double)DRAW_EPS * (1 << 24), "the bound covers the comparisons");
+  constexpr W EPS = sizeof(W) == 4 ? (W)draw_eps(N, LPR) : W(0);
   const int col0 = li * N;
   bool sure = true;
   I border{0};
@@ -105,7 +104,7 @@ __device__ __forceinline__ bool group_draw(const SampleParams& p, const float (&
       const W total = group_sum<LPR>(sum);
       W run = group_sum_before<LPR>(sum, li);
       const W want = (W)p.top_p * total;
-      const W lo = want - D::EPS * total, hi = want + D::EPS * total;
+      const W lo = want - EPS * total, hi = want + EPS * total;
       int n_lo = 0, n_hi = 0;                            // past the last weight the sum is the total
 #pragma unroll
       for (int i = 0; i < N; ++i) {
@@ -136,7 +135,7 @@ __device__ __forceinline__ bool group_draw(const SampleParams& p, const float (&
   W run = group_sum_before<LPR>(sum, li);
   int at;
   if constexpr (sizeof(W) == 4) {
-    const W lo = want - D::EPS * total, hi = want + D::EPS * total;
+    const W lo = want - EPS * total, hi = want + EPS * total;
     int n_lo = 0, n_hi = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
