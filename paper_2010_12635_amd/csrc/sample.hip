@@ -464,8 +464,14 @@ struct LongSample {
     const int cl = item_class(Item64{border});
     auto weight = [&](float z) -> double { return COUNT ? 1.0 : D::weight(z, zmax, p); };
     auto inside = [&](float z, int c) { return LIMIT ? z > zl || (z == zl && c <= cl) : z > -INFINITY; };
-    // The first histogram: bin floor((zmax - z) scale), BINS and more below it.
+    // The first histogram: bin floor((zmax - z) scale), BINS below it.  With COUNT
+    // the last bin takes what is below, and what a range past fp32 makes of the
+    // product (scale 0 times an infinite difference).
     float scale, near = NEAR;
+    auto first_bin = [&](float z) {
+      const float x = (zmax - z) * scale;
+      return x < (float)BINS ? (int)x : COUNT ? BINS - 1 : BINS;
+    };
     if (COUNT) {
       float low = INFINITY;
       r.each([&](const float (&v)[VE], int) {
@@ -489,16 +495,15 @@ struct LongSample {
         float low_rest = 0.f;
 #pragma unroll
         for (int i = 0; i < VE; ++i) {
-          const float d = zmax - v[i];
-          const float x = d * scale;
+          const int b = first_bin(v[i]);
           if (COUNT) {
-            if (inside(v[i], c0 + i)) lds_add(&sh.bin[x < (float)BINS ? (int)x : BINS - 1], 1.0);
+            if (inside(v[i], c0 + i)) lds_add(&sh.bin[b], 1.0);
           } else {
             const bool in = !LIMIT || inside(v[i], c0 + i);   // -inf weighs nothing
-            const bool close = x < (float)BINS;
-            if (sizeof(W) == 4) low_rest += in && !close ? __builtin_amdgcn_exp2f(-d * p.k) : 0.f;
+            const bool close = b < BINS;
+            if (sizeof(W) == 4) low_rest += in && !close ? __builtin_amdgcn_exp2f((v[i] - zmax) * p.k) : 0.f;
             else if (in && !close) rest += weight(v[i]);
-            if (in && close) lds_add(&sh.bin[(int)x], weight(v[i]));
+            if (in && close) lds_add(&sh.bin[b], weight(v[i]));
           }
         }
         rest += (double)low_rest;
@@ -520,8 +525,7 @@ struct LongSample {
       auto member = [&](float z, int c) {
         bool m;
         if (shift < 0) {
-          const float x = (zmax - z) * scale;
-          m = x >= (float)hit && (x < (float)(hit + 1) || (COUNT && hit == BINS - 1));
+          m = first_bin(z) == hit;
         } else {
           const uint32_t key = score_key(z);
           m = key >= klo && key <= khi && (int)((khi - key) >> shift) == hit;
