@@ -630,21 +630,15 @@ struct LongSample {
     __syncthreads();
     double total = 0.0, run = 0.0;
     for (int i = 0; i < NW; ++i) total += sh.d[i];
-    const double want = (double)u * total;
-    int owner = -1, fallback = 0;
+    const double want = (double)u * total;               // below the total: u <= 1 - 2^-24
+    int owner = -1;                                      // some wave: the sums end with the total
     double before = 0.0;
     for (int i = 0; i < NW; ++i) {
-      if (sh.n[i] >= 0) fallback = i;
       if (owner < 0 && sh.n[i] >= 0 && run + sh.d[i] > want) { owner = i; before = run; }
       run += sh.d[i];
     }
-    const bool none = owner < 0;                         // rounding: the last class kept
-    if (none) owner = fallback;
-    bool sure = true;
     if (wave == owner) {
       const double eps = D::EPS * total;
-      int at = none ? sh.n[owner] : -1;
-      double w_at = 0.0;
       bool done = false;
       r.each([&](const float (&v)[VE], int c0) {
         // every lane comes here for every vector of the wave; done and before are the wave's
@@ -655,48 +649,42 @@ struct LongSample {
         if (!__ballot(own > 0.0)) return;
         const double upto = wave_scan(own);
         double x = before + wave_before(upto);
-        bool here = false;
-        if (none) {
-          here = at >= c0 && at < c0 + VE;
-        } else {
-          const uint64_t hits = __ballot(own > 0.0 && before + upto > want);
-          here = hits && lane == __ffsll((unsigned long long)hits) - 1;
-        }
-        // the class in this lane: its sum passes `want` (the lane's last kept one
-        // where the order of additions leaves none)
-        if (here) {
-          int c = -1, kept = -1;
-          double wc = 0.0, wl = 0.0;
+        const uint64_t hits = __ballot(own > 0.0 && before + upto > want);
+        // the class in this lane: its sum passes `want`; where the order of
+        // additions leaves none, the lane's last kept one, unless in doubt
+        if (hits && lane == __ffsll((unsigned long long)hits) - 1) {
+          int at = -1;
+          double w_at = 0.0;
+          bool passed = false, sure = false;
 #pragma unroll
           for (int i = 0; i < VE; ++i) {
-            if (w[i] > 0.0) {
+            if (w[i] > 0.0 && !passed) {
               const double y = x + w[i];
-              if (c < 0 && (none ? c0 + i == at : y > want)) {
-                c = c0 + i;
-                wc = w[i];
-                if (eps > 0.0) sure = fabs(x - want) > eps && fabs(y - want) > eps;
-              }
+              at = c0 + i;
+              w_at = w[i];
+              passed = y > want;
+              sure = passed && fabs(x - want) > eps && fabs(y - want) > eps;
               x = y;
-              kept = c0 + i;
-              wl = w[i];
             }
           }
-          at = c >= 0 ? c : kept;
-          w_at = c >= 0 ? wc : wl;
-          if (sure) {
+          if (sure || D::EPS == 0.0) {
             *label = at;
             if (prob) *prob = (float)(w_at / total);
           } else {
             sh.doubt = 1;
           }
         }
-        done = __ballot(here) != 0;
+        done = hits != 0;
         before += from_lane(upto, 63);
       });
-      // sums of the walk and of the wave may differ by a rounding
+      // sums of the walk and of the wave may differ by a rounding: the wave's last
       if (!done && lane == 0) {
-        *label = sh.n[owner];
-        if (prob) *prob = (float)(D::weight(to_f32<typename Row::Elem>(r.z[sh.n[owner]]), zmax, p) / total);
+        if (D::EPS == 0.0) {
+          *label = sh.n[owner];
+          if (prob) *prob = (float)(D::weight(to_f32<typename Row::Elem>(r.z[sh.n[owner]]), zmax, p) / total);
+        } else {
+          sh.doubt = 1;
+        }
       }
     }
     __syncthreads();

@@ -86,3 +86,28 @@ def test_many_draws_in_lane_groups(prec, C, n):
         y, _ = draws(zt, C, prec, torch.as_tensor(u).cuda(), 0.9, k, p, m)
         wy, _ = S.sample_labels(zh, u.astype(np.float64), float(np.float32(0.9)), k, float(np.float32(p)), m)
         assert np.array_equal(y.cpu().numpy(), wy)
+
+
+@pytest.mark.parametrize("prec", [0, 1, 2])
+@pytest.mark.parametrize("C", [64, 900, 1300, 9001, 50001])
+def test_u_next_to_running_sums(C, prec):
+    """u is the fp32 number nearest to a running sum's share, or its neighbour:
+    32 bits cannot tell on which side of it the draw falls, 64 bits can."""
+    n = 200 if C < 9000 else 40
+    print(f"[waves] next to sums C={C} prec={prec}", flush=True)
+    rng = np.random.default_rng(C)
+    z = rng.standard_normal((n, C)) * np.where(np.arange(n) % 2, 2.0, 0.3)[:, None]
+    zt = torch.full((n, round8(C)), float("nan"), dtype=G.torch_dtype(prec), device="cuda")
+    zt[:, :C] = torch.as_tensor(z.astype(np.float32)).cuda().to(zt.dtype)
+    zh = zt[:, :C].double().cpu().numpy()
+    w = np.exp(zh - zh.max(1, keepdims=True))
+    run = np.cumsum(w, 1) / w.sum(1, keepdims=True)
+    u = run[np.arange(n), rng.integers(0, C - 1, n)].astype(np.float32)
+    u = np.where(np.arange(n) % 3 == 0, np.nextafter(u, np.float32(0)), u)
+    # a share p of the sum can be the definition's to 2^-53 only: sums that
+    # equal u to 12 digits decide nothing
+    sure = np.abs(run - u.astype(np.float64)[:, None]).min(1) > 1e-12
+    assert sure.sum() > 0.9 * n
+    y, _ = draws(zt, C, prec, torch.as_tensor(u).cuda(), 1.0, 0, 1.0, 0.0)
+    wy, _ = S.sample_labels(zh, u.astype(np.float64), 1.0)
+    assert np.array_equal(y.cpu().numpy()[sure], wy[sure])
