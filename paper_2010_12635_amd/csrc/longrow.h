@@ -47,8 +47,8 @@ struct LongRow {
   }
 };
 
-// Sum into shared memory.
-__device__ __forceinline__ void lds_add(double* at, double v) {
+// Sum into shared memory: whole numbers, whose sums know no order.
+__device__ __forceinline__ void lds_add(uint64_t* at, uint64_t v) {
   __hip_atomic_fetch_add(at, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
 }
 

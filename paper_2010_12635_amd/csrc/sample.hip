@@ -336,6 +336,14 @@ __global__ __launch_bounds__(NT) void sample_top_kernel(SampleParams p) {
 // below 128 e for |x| <= 55, and what lies beyond weighs next to nothing.  Other
 // sums are in 64 bits.  Where a running sum comes within its bound of a border
 // the row is done again with W = double.
+//
+// Sums that several threads add to in no fixed order are whole numbers, so that
+// the order cannot show: the bins' in one word of 64 bits with frac() of them
+// behind the point, what is rounded away in the bound, or, where that has to be
+// exact, in two words, 31 bits and 32 more; a border's members, MEMBERS at most,
+// in one word with 54.  (64-bit float atomics, whose sums differ from run to run:
+// 1024 rows of 50001 nearly equal classes 469 us instead of 480, 16384 of 4001
+// 201 instead of 204.)
 constexpr double REST_EPS = 7.62939453125e-6;            // 2^-17
 template <typename W> struct LongDraw;
 template <> struct LongDraw<float> {
@@ -356,10 +364,13 @@ template <> struct LongDraw<double> {
 
 constexpr int BINS = 1024, MEMBERS = 256, NEAR_CAP = 512;
 
+enum Sums { COUNTS, WORD, PAIR };                        // what a bin holds
+
 template <int NT>
 struct LongShared {
-  double bin[BINS];
-  double item[MEMBERS], weight[MEMBERS];
+  uint64_t bin[BINS], fine[BINS];                        // fine: the second words of PAIR
+  double item[MEMBERS];
+  uint64_t weight[MEMBERS];
   double d[NT / 64], rest[NT / 64];
   float f[NT / 64];                                      // the waves' maxima: written once a row
   float low[NT / 64];
@@ -388,9 +399,41 @@ struct LongSample {
   LongShared<NT>& sh;
   float zmax;
 
+  static constexpr Sums WEIGHTS = sizeof(W) == 4 ? WORD : PAIR;
+  // Bits behind the point of a word: C 2^frac is below 2^62, 2^frac below 2^52.
+  __device__ __forceinline__ int frac() const { return min(51, 30 + __clz((int)p.C)); }
+  // w <= 1 as a word: the number's last 52 bits when 2^52 is added.
+  __device__ __forceinline__ uint64_t word(double w) const {
+    const double x = fma(w, ldexp(1.0, frac()), 0x1p52);
+    return (uint64_t)__double_as_longlong(x) & 0xfffffffffffffull;
+  }
+
+  template <Sums S>
   __device__ __forceinline__ void clear_bins() {
-    for (int i = threadIdx.x; i < BINS; i += NT) sh.bin[i] = 0.0;
+    for (int i = threadIdx.x; i < BINS; i += NT) {
+      sh.bin[i] = 0;
+      if (S == PAIR) sh.fine[i] = 0;
+    }
     if (threadIdx.x == 0) { sh.hit = -1; sh.count = 0; }
+  }
+  __device__ __forceinline__ void add_pair(int b, double w) {
+    const double hi = w * 2147483648.0;                  // w <= 1
+    const uint32_t h = (uint32_t)hi;
+    lds_add(&sh.bin[b], h);
+    lds_add(&sh.fine[b], (uint32_t)((hi - (double)h) * 4294967296.0));
+  }
+  template <Sums S>
+  __device__ __forceinline__ void add_score(int b, float z) {
+    if constexpr (S == COUNTS) lds_add(&sh.bin[b], 1);
+    else if constexpr (S == WORD) lds_add(&sh.bin[b], word(D::weight(z, zmax, p)));
+    else add_pair(b, Draw<double>::weight(z, zmax, p));
+  }
+  template <Sums S>
+  __device__ __forceinline__ double bin_sum(int b) const {
+    const double x = (double)sh.bin[b];
+    if constexpr (S == COUNTS) return x;
+    else if constexpr (S == WORD) return ldexp(x, -frac());
+    else return x * 0x1p-31 + (double)sh.fine[b] * 0x1p-63;
   }
 
   // With the histogram complete (a barrier since): the last bin that holds
@@ -398,12 +441,13 @@ struct LongSample {
   // where want = share (above + the sum of the bins + rest): its number, the sum
   // before it and its own.  rest: this wave's part.
   struct Found { int bin; double above, mass, want, sum, rest; };
+  template <Sums S>
   __device__ __forceinline__ Found find_bin(double above, double rest, double share, double want) {
     constexpr int PER = BINS / NT;
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     double own[PER], sum = 0.0;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) sum += own[i] = sh.bin[t * PER + i];
+    for (int i = 0; i < PER; ++i) sum += own[i] = bin_sum<S>(t * PER + i);
     const double upto = wave_scan(sum);
     if (lane == 63) { sh.d[wave] = upto; sh.rest[wave] = rest; }
     __syncthreads();
@@ -436,14 +480,17 @@ struct LongSample {
     return r;
   }
 
+  static __device__ __forceinline__ uint64_t member_weight(double w) { return (uint64_t)(w * 0x1p54); }
+
   // The n listed members of a bin: one is kept if what comes before it is below
   // f.want.  Returns whether that is certain for all.
   __device__ __forceinline__ bool settle(const Found& f, int n, double eps, double& border) {
     const int t = threadIdx.x;
     if (t < n) {
       const double mine = sh.item[t];
-      double before = f.above;
-      for (int j = 0; j < n; ++j) before += sh.item[j] > mine ? sh.weight[j] : 0.0;
+      uint64_t ahead = 0;                                // listed in no fixed order
+      for (int j = 0; j < n; ++j) ahead += sh.item[j] > mine ? sh.weight[j] : 0;
+      const double before = f.above + (double)ahead * 0x1p-54;
       const uint64_t bits = (uint64_t)__double_as_longlong(mine);
       if (before < f.want) atomicMin((unsigned long long*)&sh.least, (unsigned long long)bits);
       atomicMax((unsigned long long*)&sh.most, (unsigned long long)bits);
@@ -459,7 +506,7 @@ struct LongSample {
   // certain.
   template <bool COUNT, bool LIMIT>
   __device__ __forceinline__ bool select(double& border) {
-    const int t = threadIdx.x;
+    constexpr Sums S = COUNT ? COUNTS : WEIGHTS;
     const float zl = key_score(item_key(Item64{border}));
     const int cl = item_class(Item64{border});
     auto weight = [&](float z) -> double { return COUNT ? 1.0 : D::weight(z, zmax, p); };
@@ -488,7 +535,7 @@ struct LongSample {
     double eps = 0.0;
     for (;;) {
       if (!COUNT) scale = p.k * ((float)BINS / near);
-      clear_bins();
+      clear_bins<S>();
       __syncthreads();
       double rest = 0.0;
       r.each([&](const float (&v)[VE], int c0) {
@@ -497,22 +544,22 @@ struct LongSample {
         for (int i = 0; i < VE; ++i) {
           const int b = first_bin(v[i]);
           if (COUNT) {
-            if (inside(v[i], c0 + i)) lds_add(&sh.bin[b], 1.0);
+            if (inside(v[i], c0 + i)) add_score<S>(b, v[i]);
           } else {
             const bool in = !LIMIT || inside(v[i], c0 + i);   // -inf weighs nothing
             const bool close = b < BINS;
             if (sizeof(W) == 4) low_rest += in && !close ? __builtin_amdgcn_exp2f((v[i] - zmax) * p.k) : 0.f;
             else if (in && !close) rest += weight(v[i]);
-            if (in && close) lds_add(&sh.bin[b], weight(v[i]));
+            if (in && close) add_score<S>(b, v[i]);
           }
         }
         rest += (double)low_rest;
       });
       if (!COUNT) rest = wave_reduce(rest, AddF());
       __syncthreads();
-      f = find_bin(0.0, rest, COUNT ? 0.0 : p.top_p, (double)p.top_k);
+      f = find_bin<S>(0.0, rest, COUNT ? 0.0 : p.top_p, (double)p.top_k);
       if (COUNT) break;
-      eps = D::EPS > 0.0 ? D::EPS * f.sum + REST_EPS * f.rest : 0.0;
+      eps = D::EPS > 0.0 ? D::EPS * f.sum + REST_EPS * f.rest + ldexp((double)p.C, -frac()) : 0.0;
       if (f.want + eps < f.sum || near >= far) break;
       near = far;
     }
@@ -540,7 +587,7 @@ struct LongSample {
           const int at = atomicAdd(&sh.count, 1);
           if (at < MEMBERS) {
             sh.item[at] = score_item(v[i], c0 + i).v;
-            sh.weight[at] = weight(v[i]);
+            sh.weight[at] = member_weight(weight(v[i]));
           }
         }
       });
@@ -589,17 +636,17 @@ struct LongSample {
       khi = hi;
       shift = 0;
       while ((hi - lo) >> shift >= (uint32_t)BINS) ++shift;
-      clear_bins();
+      clear_bins<S>();
       __syncthreads();
       r.each([&](const float (&v)[VE], int c0) {
 #pragma unroll
         for (int i = 0; i < VE; ++i) {
           const uint32_t key = score_key(v[i]);
-          if (key >= klo && key <= khi && inside(v[i], c0 + i)) lds_add(&sh.bin[(khi - key) >> shift], weight(v[i]));
+          if (key >= klo && key <= khi && inside(v[i], c0 + i)) add_score<S>((int)((khi - key) >> shift), v[i]);
         }
       });
       __syncthreads();
-      f = find_bin(f.above, 0.0, 0.0, want);
+      f = find_bin<S>(f.above, 0.0, 0.0, want);
     }
   }
 
@@ -704,7 +751,8 @@ struct LongSample {
   };
   __device__ __forceinline__ Listed run_listed(float near, bool exact, float u, int32_t* label, float* prob) {
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
-    clear_bins();
+    if (exact) clear_bins<PAIR>();
+    else clear_bins<WORD>();
     int n = 0;                                           // the wave's entries
     double rest = 0.0;
     r.each([&](const float (&v)[VE], int c0) {
@@ -759,17 +807,20 @@ struct LongSample {
       auto bin = [&](float z) { const float x = (zmax - z) * scale; return x < (float)BINS ? (int)x : BINS - 1; };
 #pragma unroll
       for (int i = 0; i < PER; ++i)
-        if (i * 64 + lane < n) lds_add(&sh.bin[bin(z[i])], w[i]);
+        if (i * 64 + lane < n) {
+          if (exact) add_pair(bin(z[i]), w[i]);
+          else lds_add(&sh.bin[bin(z[i])], word(w[i]));
+        }
       __syncthreads();
       rest = wave_reduce(rest, AddF());
-      const Found f = find_bin(0.0, rest, p.top_p, 0.0);
-      const double eps = exact ? 0.0 : REST_EPS * f.rest + 1e-12 * f.sum;
+      const Found f = exact ? find_bin<PAIR>(0.0, rest, p.top_p, 0.0) : find_bin<WORD>(0.0, rest, p.top_p, 0.0);
+      const double eps = exact ? 0.0 : REST_EPS * f.rest + 1e-12 * f.sum + ldexp((double)(NW * NEAR_CAP), -frac());
       if (!(f.want + eps < f.sum)) return BEYOND;
 #pragma unroll
       for (int i = 0; i < PER; ++i)
         if (i * 64 + lane < n && bin(z[i]) == f.bin) {
           const int at = atomicAdd(&sh.count, 1);
-          if (at < MEMBERS) { sh.item[at] = score_item(z[i], c[i]).v; sh.weight[at] = w[i]; }
+          if (at < MEMBERS) { sh.item[at] = score_item(z[i], c[i]).v; sh.weight[at] = member_weight(w[i]); }
         }
       __syncthreads();
       const int members = sh.count;

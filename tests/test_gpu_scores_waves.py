@@ -111,3 +111,29 @@ def test_u_next_to_running_sums(C, prec):
     y, _ = draws(zt, C, prec, torch.as_tensor(u).cuda(), 1.0, 0, 1.0, 0.0)
     wy, _ = S.sample_labels(zh, u.astype(np.float64), 1.0)
     assert np.array_equal(y.cpu().numpy()[sure], wy[sure])
+
+
+@pytest.mark.parametrize("prec", [0, 2])
+def test_same_bits_whatever_the_timing(prec):
+    """Sums that threads add to as they come: rows of nearly equal scores (all
+    classes in the histograms), of few different ones and of large top-k, many
+    times over beside another stream's work."""
+    n, C = 48, 30011
+    rng = np.random.default_rng(prec)
+    rows = [rng.standard_normal(C) * 0.1, rng.integers(0, 5, C) / 3.0, rng.standard_normal(C) * 3,
+            np.where(rng.random(C) < 0.5, 0.0, 1.0 / 3.0)]
+    z = np.stack([rng.permutation(rows[i % 4]) for i in range(n)])
+    zt = torch.full((n, round8(C)), float("nan"), dtype=G.torch_dtype(prec), device="cuda")
+    zt[:, :C] = torch.as_tensor(z.astype(np.float32)).cuda().to(zt.dtype)
+    u = torch.as_tensor(rng.random(n).astype(np.float32)).cuda()
+    side = torch.cuda.Stream()
+    busy = torch.ones(1 << 24, device="cuda")
+    for k, p, m in ((0, 0.75, 0.0), (5000, 0.5, 0.0), (0, 0.999, 0.01)):
+        print(f"[waves] timing prec={prec} k={k} p={p}", flush=True)
+        first = draws(zt, C, prec, u, 1.0, k, p, m)
+        for _ in range(6):
+            with torch.cuda.stream(side):
+                busy.mul_(1.0)
+            y, pr = draws(zt, C, prec, u, 1.0, k, p, m)
+            assert torch.equal(y, first[0]) and torch.equal(pr, first[1])
+        torch.cuda.synchronize()
