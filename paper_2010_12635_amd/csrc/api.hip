@@ -735,7 +735,7 @@ gcn_status gcn_top_logits(int64_t n, int64_t C, int64_t ld, int32_t prec, const 
   if (!aligned16(logits) || !aligned16(top_values) || !aligned16(top_classes)) return GCN_ERR_ALIGNMENT;
   if (!workspace || workspace_bytes < top_workspace_bytes(prec, n, C, K)) return GCN_ERR_WORKSPACE;
   if (!aligned16(workspace)) return GCN_ERR_ALIGNMENT;
-  TopParams p;
+  TopParams p{};
   p.n = n; p.C = C; p.ld = ld; p.K = K; p.ld_top = ld_top;
   p.logits = logits; p.values = top_values; p.classes = top_classes; p.flag = overflow;
   GCN_HIP(top_launch(prec, p, workspace, s));
@@ -772,7 +772,7 @@ gcn_status gcn_distill(int64_t n, int64_t C, int64_t ld, int32_t prec, const voi
     return GCN_ERR_ALIGNMENT;
   if (!workspace || workspace_bytes < distill_workspace_bytes(prec, n, C, K)) return GCN_ERR_WORKSPACE;
   if (!aligned16(workspace)) return GCN_ERR_ALIGNMENT;
-  DistillParams p;
+  DistillParams p{};
   p.n = n; p.C = C; p.ld = ld; p.K = K; p.ld_top = ld_top;
   p.logits = logits; p.top_prec = top_prec; p.top_values = top_values; p.top_classes = top_classes;
   p.mask = mask;
@@ -808,7 +808,7 @@ gcn_status gcn_sample_labels(int64_t n, int64_t C, int64_t ld, int32_t prec, con
   if (!aligned16(logits) || !aligned16(u) || !aligned16(labels) || !aligned16(prob)) return GCN_ERR_ALIGNMENT;
   if (!workspace || workspace_bytes < sample_workspace_bytes(prec, n, C)) return GCN_ERR_WORKSPACE;
   if (!aligned16(workspace)) return GCN_ERR_ALIGNMENT;
-  SampleParams p;
+  SampleParams p{};
   p.n = n; p.C = C; p.ld = ld; p.logits = logits; p.mask = mask; p.u = u;
   p.greedy = temperature == 0.f;                         // a draw among one class, at any temperature
   p.T = p.greedy ? 1.0 : (double)temperature;

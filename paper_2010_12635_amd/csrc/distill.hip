@@ -417,7 +417,7 @@ __global__ __launch_bounds__(NT, 4) void distill_row_kernel(DistillParams p) {
   constexpr int NW = NT / 64;
   __shared__ MaxSum s_part[NW];
   __shared__ EntryTable s_tab;
-  const int64_t row = blockIdx.x;
+  const int64_t row = p.row0 + blockIdx.x;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int C = (int)p.C;
   const T* __restrict__ z = reinterpret_cast<const T*>(p.logits) + row * p.ld;
@@ -466,12 +466,12 @@ __global__ __launch_bounds__(NT, 4) void distill_row_kernel(DistillParams p) {
   if (bad) raise_flag(p.flag);
 }
 
-// Segments: workgroup (row, s) = (blockIdx.x / segs, blockIdx.x % segs).
+// Segments: workgroup (row, s) = (row0 + blockIdx.x / segs, blockIdx.x % segs).
 struct Segment {
   int64_t row;
   int s, lo, hi;                                     // vectors [lo, hi)
   __device__ __forceinline__ Segment(const DistillParams& p, int VE)
-      : row(blockIdx.x / p.segs), s((int)(blockIdx.x % p.segs)), lo(s * p.seg) {
+      : row(p.row0 + blockIdx.x / p.segs), s((int)(blockIdx.x % p.segs)), lo(s * p.seg) {
     const int nvec = (int)((p.C + VE - 1) / VE);
     hi = lo + p.seg < nvec ? lo + p.seg : nvec;
   }
@@ -507,7 +507,7 @@ __global__ __launch_bounds__(256) void distill_part_kernel(DistillParams p) {
   if (t == 0) {
     MaxSum a = s_part[0];
     for (int i = 1; i < 4; ++i) a = join(a, s_part[i], k);
-    reinterpret_cast<MaxSum*>(p.part_ms)[blockIdx.x] = a;
+    reinterpret_cast<MaxSum*>(p.part_ms)[g.row * p.segs + g.s] = a;
   }
 }
 
@@ -670,22 +670,24 @@ LongPlan long_plan(int prec, int64_t n, int64_t C) {
 }
 
 template <typename T>
-hipError_t launch_rows(const DistillParams& p, hipStream_t s) {
-  const int64_t nvec = (p.C + Vec<T>::N - 1) / Vec<T>::N;
-  if (p.segs == 0) {
-    const dim3 grid((unsigned)p.n);
-    if (nvec <= 4 * 256) hipLaunchKernelGGL((distill_row_kernel<T, 256, 4>), grid, dim3(256), 0, s, p);
-    else if (nvec <= 8 * 256) hipLaunchKernelGGL((distill_row_kernel<T, 256, 8>), grid, dim3(256), 0, s, p);
-    else if (nvec <= 8 * 512) hipLaunchKernelGGL((distill_row_kernel<T, 512, 8>), grid, dim3(512), 0, s, p);
-    else hipLaunchKernelGGL((distill_row_kernel<T, 512, 16>), grid, dim3(512), 0, s, p);
+hipError_t launch_rows(const DistillParams& params, hipStream_t s) {
+  const int64_t nvec = (params.C + Vec<T>::N - 1) / Vec<T>::N;
+  return launch_long_rows(params, params.segs > 0 ? params.segs : 1, [&](const DistillParams& p, int64_t rows) {
+    if (p.segs == 0) {
+      const dim3 grid((unsigned)rows);
+      if (nvec <= 4 * 256) hipLaunchKernelGGL((distill_row_kernel<T, 256, 4>), grid, dim3(256), 0, s, p);
+      else if (nvec <= 8 * 256) hipLaunchKernelGGL((distill_row_kernel<T, 256, 8>), grid, dim3(256), 0, s, p);
+      else if (nvec <= 8 * 512) hipLaunchKernelGGL((distill_row_kernel<T, 512, 8>), grid, dim3(512), 0, s, p);
+      else hipLaunchKernelGGL((distill_row_kernel<T, 512, 16>), grid, dim3(512), 0, s, p);
+      return hipGetLastError();
+    }
+    const dim3 grid((unsigned)(rows * p.segs));
+    hipLaunchKernelGGL((distill_part_kernel<T>), grid, dim3(256), 0, s, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((distill_segment_kernel<T>), grid, dim3(256), 0, s, p);
     return hipGetLastError();
-  }
-  const dim3 grid((unsigned)(p.n * p.segs));
-  hipLaunchKernelGGL((distill_part_kernel<T>), grid, dim3(256), 0, s, p);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((distill_segment_kernel<T>), grid, dim3(256), 0, s, p);
-  return hipGetLastError();
+  });
 }
 
 size_t up256(size_t b) { return (b + 255) & ~size_t(255); }

@@ -177,6 +177,7 @@ hipError_t loss_launch(int prec, int64_t n, int64_t C, int64_t ld, const void* l
 // gcn_sample_labels).
 struct TopParams {
   int64_t n, C, ld, K, ld_top;
+  int64_t row0;         // first row of a launch (long rows: launch_long_rows)
   const void* logits;
   void* values;
   int32_t* classes;
@@ -187,6 +188,7 @@ hipError_t top_launch(int prec, const TopParams& p, void* ws, hipStream_t s);
 
 struct DistillParams {
   int64_t n, C, ld, K, ld_top;
+  int64_t row0;         // as in TopParams
   const void* logits;
   int top_prec;
   const void* top_values;
@@ -211,6 +213,7 @@ hipError_t distill_launch(int prec, DistillParams p, float* loss, float* colsum,
 
 struct SampleParams {
   int64_t n, C, ld;
+  int64_t row0;         // as in TopParams
   const void* logits;
   const uint8_t* mask;
   const float* u;

@@ -6,6 +6,20 @@
 
 namespace gcn {
 
+// Long rows take a workgroup each (or several): a launch takes as many rows as
+// fill 2^18 workgroups, whatever their threads (HIP launches less than 2^32
+// threads), and the next one goes on at row0.  launch(p, rows) launches.
+constexpr int64_t LAUNCH_WORKGROUPS = 1 << 18;
+template <typename P, typename F>
+hipError_t launch_long_rows(P p, int64_t workgroups_a_row, F launch) {
+  const int64_t most = LAUNCH_WORKGROUPS / workgroups_a_row > 0 ? LAUNCH_WORKGROUPS / workgroups_a_row : 1;
+  for (p.row0 = 0; p.row0 < p.n; p.row0 += most) {
+    const hipError_t e = launch(p, p.n - p.row0 < most ? p.n - p.row0 : most);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 // A score as an unsigned key of the same order: a larger score has a larger
 // key, equal scores (-0 and +0 among them) equal keys.  NaN has no place in
 // the order and is dealt with before.

@@ -271,7 +271,7 @@ __global__ __launch_bounds__(NT) void sample_top_kernel(SampleParams p) {
   __shared__ TopList<NT> sh;
   __shared__ double s_item[GCN_MAX_TOP], s_w[GCN_MAX_TOP], s_d[NW];
   __shared__ int s_cls[GCN_MAX_TOP];
-  const int64_t row = blockIdx.x;
+  const int64_t row = p.row0 + blockIdx.x;
   if (p.mask && p.mask[row] == 0) return;
   const int t = threadIdx.x;
   const LongRow<T, NT> r(reinterpret_cast<const T*>(p.logits) + row * p.ld, (int)p.C);
@@ -888,7 +888,7 @@ __global__ __launch_bounds__(NT, 4) void sample_row_kernel(SampleParams p) {
   typedef LongRow<T, NT, true> Row;
   constexpr int NW = NT / 64;
   __shared__ LongShared<NT> sh;
-  const int64_t row = blockIdx.x;
+  const int64_t row = p.row0 + blockIdx.x;
   if (p.mask && p.mask[row] == 0) return;
   const Row r(reinterpret_cast<const T*>(p.logits) + row * p.ld, (int)p.C);
   const float u = p.u[row];
@@ -954,17 +954,19 @@ hipError_t launch_lpr(const SampleParams& p, hipStream_t s) {
   return p.top_k < p.C || p.top_p < 1.0 ? launch_filter<T, LPR, true>(p, s) : launch_filter<T, LPR, false>(p, s);
 }
 template <typename T>
-hipError_t launch_rows(const SampleParams& p, hipStream_t s) {
-  const int64_t nvec = (p.C + Vec<T>::N - 1) / Vec<T>::N;
-  const dim3 grid((unsigned)p.n);
-  if (p.top_k <= GCN_MAX_TOP) {
-    if (nvec <= 8 * 256 && p.top_k <= 32) hipLaunchKernelGGL((sample_top_kernel<T, 256>), grid, dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((sample_top_kernel<T, 1024>), grid, dim3(1024), 0, s, p);
-  } else {
-    if (nvec <= 8 * 256) hipLaunchKernelGGL((sample_row_kernel<T, 256>), grid, dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((sample_row_kernel<T, 512>), grid, dim3(512), 0, s, p);
-  }
-  return hipGetLastError();
+hipError_t launch_rows(const SampleParams& params, hipStream_t s) {
+  const int64_t nvec = (params.C + Vec<T>::N - 1) / Vec<T>::N;
+  return launch_long_rows(params, 1, [&](const SampleParams& p, int64_t rows) {
+    const dim3 grid((unsigned)rows);
+    if (p.top_k <= GCN_MAX_TOP) {
+      if (nvec <= 8 * 256 && p.top_k <= 32) hipLaunchKernelGGL((sample_top_kernel<T, 256>), grid, dim3(256), 0, s, p);
+      else hipLaunchKernelGGL((sample_top_kernel<T, 1024>), grid, dim3(1024), 0, s, p);
+    } else {
+      if (nvec <= 8 * 256) hipLaunchKernelGGL((sample_row_kernel<T, 256>), grid, dim3(256), 0, s, p);
+      else hipLaunchKernelGGL((sample_row_kernel<T, 512>), grid, dim3(512), 0, s, p);
+    }
+    return hipGetLastError();
+  });
 }
 template <typename T>
 hipError_t launch_t(const SampleParams& p, hipStream_t s) {

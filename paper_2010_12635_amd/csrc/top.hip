@@ -171,7 +171,7 @@ __global__ __launch_bounds__(256) void top_group_kernel(TopParams p) {
 template <typename T, int NT>
 __global__ __launch_bounds__(NT) void top_row_kernel(TopParams p) {
   __shared__ TopList<NT> sh;
-  const int64_t row = blockIdx.x;
+  const int64_t row = p.row0 + blockIdx.x;
   const LongRow<T, NT> r(reinterpret_cast<const T*>(p.logits) + row * p.ld, (int)p.C);
   const int K = (int)p.K;
   float mx;
@@ -207,14 +207,16 @@ hipError_t launch_lpr(const TopParams& p, hipStream_t s) {
   return launch_l<T, LPR, 0>(p, s);
 }
 template <typename T>
-hipError_t launch_rows(const TopParams& p, hipStream_t s) {
-  const int64_t nvec = (p.C + Vec<T>::N - 1) / Vec<T>::N;
-  const dim3 grid((unsigned)p.n);
-  // the bound of step 2 is close where K is small against the threads
-  if (nvec <= 8 * 256 && p.K <= 32) hipLaunchKernelGGL((top_row_kernel<T, 256>), grid, dim3(256), 0, s, p);
-  else if (nvec <= 8 * 512 && p.K <= 64) hipLaunchKernelGGL((top_row_kernel<T, 512>), grid, dim3(512), 0, s, p);
-  else hipLaunchKernelGGL((top_row_kernel<T, 1024>), grid, dim3(1024), 0, s, p);
-  return hipGetLastError();
+hipError_t launch_rows(const TopParams& params, hipStream_t s) {
+  const int64_t nvec = (params.C + Vec<T>::N - 1) / Vec<T>::N;
+  return launch_long_rows(params, 1, [&](const TopParams& p, int64_t rows) {
+    const dim3 grid((unsigned)rows);
+    // the bound of step 2 is close where K is small against the threads
+    if (nvec <= 8 * 256 && p.K <= 32) hipLaunchKernelGGL((top_row_kernel<T, 256>), grid, dim3(256), 0, s, p);
+    else if (nvec <= 8 * 512 && p.K <= 64) hipLaunchKernelGGL((top_row_kernel<T, 512>), grid, dim3(512), 0, s, p);
+    else hipLaunchKernelGGL((top_row_kernel<T, 1024>), grid, dim3(1024), 0, s, p);
+    return hipGetLastError();
+  });
 }
 template <typename T>
 hipError_t launch_t(const TopParams& p, hipStream_t s) {
