@@ -481,7 +481,8 @@ gcn_status gcn_distill(int64_t n, int64_t C, int64_t ld, int32_t prec, const voi
  *               running sum of the kept weights exceeds u[i] times their sum
  *   prob[i]   = its weight over that sum (fp32 [n]; may be NULL)
  * The label is that of the definition in 64-bit arithmetic, whatever prec is.
- * T = 0 takes the first class of the order (u is then not read; prob = 1).
+ * T = 0 takes the first class of the order (u is then not read and may be
+ * NULL; prob = 1).
  * A row without classes (every score -infinity) gives label -1 and prob 0;
  * so does a row that holds NaN or +infinity, or whose u lies outside [0, 1),
  * and sets *overflow to 1.  Rows that mask does not select keep their labels

@@ -804,7 +804,7 @@ gcn_status gcn_sample_labels(int64_t n, int64_t C, int64_t ld, int32_t prec, con
   if (!(temperature == 0.f || (temperature >= GCN_MIN_TEMPERATURE && temperature <= GCN_MAX_TEMPERATURE)) ||
       top_k < 0 || !(top_p > 0.f && top_p <= 1.f) || !(min_p >= 0.f && min_p <= 1.f))
     return GCN_ERR_INVALID_ARG;
-  if (!logits || !u || !labels) return GCN_ERR_INVALID_ARG;
+  if (!logits || (!u && temperature != 0.f) || !labels) return GCN_ERR_INVALID_ARG;
   if (!aligned16(logits) || !aligned16(u) || !aligned16(labels) || !aligned16(prob)) return GCN_ERR_ALIGNMENT;
   if (!workspace || workspace_bytes < sample_workspace_bytes(prec, n, C)) return GCN_ERR_WORKSPACE;
   if (!aligned16(workspace)) return GCN_ERR_ALIGNMENT;
