@@ -369,7 +369,10 @@ gcn_status gcn_layer_bwd_noalloc(const gcn_adj* A, const gcn_layer* L, int32_t p
 /* ---------------------------------------------------------------------------
  * gcn_loss: masked mean softmax cross-entropy over logits (n x C, ld, prec)
  * and labels (int32 in [0, C)); mask (uint8, NULL = every row) selects the
- * n_mask training rows (n_mask = number of nonzero mask entries, > 0).
+ * n_mask training rows (n_mask = number of nonzero mask entries, > 0).  A row
+ * whose label is negative (gcn_sample_labels writes -1 where a row has no
+ * answer) is left out of all outputs as if mask did not select it; n_mask
+ * stays the divisor.
  * This is the training loss of the semi-supervised vertex classification
  * that the paper scores by accuracy (Section "Experimental Setup", its
  * experiments subsection; the GCN of Section "Graph Convolutions" with the

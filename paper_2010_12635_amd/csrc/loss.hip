@@ -116,7 +116,7 @@ __global__ __launch_bounds__(256) void softmax_ce_kernel(LossParams p) {
 #pragma unroll
       for (int i = 0; i < VE; ++i) zy = i == ky ? z[i] : zy;
       zy = group_sum<LPR>(zy);
-      const bool in_mask = row_ok && msk[r] != 0;
+      const bool in_mask = row_ok && msk[r] != 0 && y >= 0;   // a row without a label is left out
       if (row_ok && col_ok) {
         float d[VE];
         const float s_in = in_mask ? sc : 0.f;

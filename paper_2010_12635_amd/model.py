@@ -435,7 +435,8 @@ class GCN2:
         the scores of the last forward pass into ``labels`` (int32 [n]) and
         its probability into ``prob`` (fp32 [n]), from the uniform numbers
         ``u`` (fp32 [n], None at temperature 0); the other entries keep their
-        values, so that ``labels`` may be the training labels.  Asynchronous."""
+        values, so that ``labels`` may be the training labels: a vertex without
+        an answer gets -1 and is then left out of the loss.  Asynchronous."""
         for name, t, dt in (("u", u, torch.float32), ("labels", labels, torch.int32), ("prob", prob, torch.float32),
                             ("mask", mask, torch.uint8)):
             if t is not None and (t.dtype != dt or tuple(t.shape) != (self.n,) or not t.is_contiguous()
