@@ -384,19 +384,26 @@ class GCN2:
             return
         dev = self.loss.device
         precs = {dt: p for p, dt in ((p, G.torch_dtype(p)) for p in (G.GCN_F32, G.GCN_F16, G.GCN_BF16))}
-        if (top_values.dim() != 2 or top_values.shape[0] != self.n or top_values.shape != top_classes.shape
+        if (top_classes is None or top_values.dim() != 2 or top_values.shape[0] != self.n
+                or top_values.shape != top_classes.shape
                 or top_classes.dtype != torch.int32 or top_values.dtype not in precs
                 or not (top_values.is_contiguous() and top_classes.is_contiguous())
                 or top_values.device != dev or top_classes.device != dev):
             raise ValueError(f"a teacher is two contiguous tensors {self.n} x K on {dev}: scores and int32 classes")
         if not 1 <= top_values.shape[1] <= G.MAX_TOP:
             raise ValueError(f"a teacher has 1 to {G.MAX_TOP} scores a row")
+        if not G.MIN_TEMPERATURE <= temperature <= G.MAX_TEMPERATURE:
+            raise ValueError(f"temperature: {G.MIN_TEMPERATURE} to {G.MAX_TEMPERATURE}")
+        if not 0 < ctypes.c_float(weight).value < float("inf"):     # as the library receives it
+            raise ValueError("weight: positive and finite in fp32")
         n_mask = self.n
         if mask is not None:
             mask = torch.as_tensor(mask).to(dev, torch.uint8).contiguous()
             if tuple(mask.shape) != (self.n,):
                 raise ValueError(f"the mask holds one entry for each of the {self.n} rows")
             n_mask = int(torch.count_nonzero(mask).item())
+            if n_mask == 0:
+                raise ValueError("the mask selects no row to learn from")
         K = top_values.shape[1]
         if K % 8:      # the library's layout: rows padded to a multiple of 8
             pad = round8(K)

@@ -1,0 +1,53 @@
+"""GCN2.set_teacher: what no step could run with is refused at once, and steps
+on any stream find the teacher whole."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2010_12635_amd import gcn as G
+from paper_2010_12635_amd import inputs as I
+from tests.test_gpu_student import make
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def wl():
+    return I.workload("er2k", 0, n_override=512)
+
+
+def teacher_of(wl, K=8):
+    m = make(wl, 1, seed=5)
+    m.forward(0, training=False)
+    v, c = m.top_logits(K)
+    return v[:, :K].contiguous(), c[:, :K].contiguous()
+
+
+@pytest.mark.parametrize("bad", [
+    dict(mask=np.zeros(512, np.uint8)), dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=2.0 ** -11),
+    dict(temperature=1025.0), dict(temperature=float("nan")), dict(weight=0.0), dict(weight=-1.0),
+    dict(weight=float("inf")), dict(weight=float("nan")), dict(weight=1e-60), dict(weight=1e60),
+    dict(top_classes=None)],
+    ids=lambda d: next(iter(d)))
+def test_refusals(wl, bad):
+    v, c = teacher_of(wl)
+    m = make(wl, 1)
+    m.set_teacher(v, c, weight=0.25)
+    kept = m.teacher
+    with pytest.raises(ValueError):
+        m.set_teacher(**dict(dict(top_values=v, top_classes=c), **bad))
+    assert m.teacher is kept                      # the teacher it had still teaches
+    m.step(0)
+    torch.cuda.synchronize()
+    assert m.overflow.item() == 0 and np.isfinite(m.distill_loss.item())
+
+
+def test_ends_of_the_ranges(wl):
+    v, c = teacher_of(wl)
+    m = make(wl, 0)
+    for T in (G.MIN_TEMPERATURE, G.MAX_TEMPERATURE):
+        m.set_teacher(v, c, temperature=T, weight=1e-3)
+        m.forward(0)
+        m.loss_and_backward()
+        torch.cuda.synchronize()
+        assert m.overflow.item() == 0
