@@ -376,13 +376,16 @@ class GCN2:
         over the rows of ``mask`` (uint8, None = every row) is added to the
         cross-entropy.  ``distill_loss`` holds its value after a step, ``loss``
         the cross-entropy's as before.  Not while an epoch is captured: the
-        graph would go on with what it recorded."""
+        graph would go on with what it recorded.  Waits for the device: steps
+        that still run may read the teacher they had, later ones may run on any
+        stream."""
         if self.graph is not None:
             raise ValueError("the captured epoch keeps its own losses: set the teacher before capture()")
+        dev = self.loss.device
         if top_values is None:
+            torch.cuda.synchronize(dev)
             self.teacher = None
             return
-        dev = self.loss.device
         precs = {dt: p for p, dt in ((p, G.torch_dtype(p)) for p in (G.GCN_F32, G.GCN_F16, G.GCN_BF16))}
         if (top_classes is None or top_values.dim() != 2 or top_values.shape[0] != self.n
                 or top_values.shape != top_classes.shape
@@ -411,7 +414,9 @@ class GCN2:
             c = torch.full((self.n, pad), -1, dtype=torch.int32, device=dev)
             v[:, :K], c[:, :K] = top_values, top_classes
             top_values, top_classes = v, c
-        self.distill_loss = torch.zeros(1, dtype=torch.float32, device=dev)
+        distill_loss = torch.zeros(1, dtype=torch.float32, device=dev)
+        torch.cuda.synchronize(dev)
+        self.distill_loss = distill_loss
         self.teacher = dict(prec=precs[top_values.dtype], values=top_values, classes=top_classes, K=K, mask=mask,
                             n_mask=n_mask, temperature=float(temperature), weight=float(weight))
 

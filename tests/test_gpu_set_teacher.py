@@ -51,3 +51,25 @@ def test_ends_of_the_ranges(wl):
         m.loss_and_backward()
         torch.cuda.synchronize()
         assert m.overflow.item() == 0
+
+
+@pytest.mark.parametrize("K", [5, 8])
+def test_step_on_another_stream(wl, K):
+    """The copies that set_teacher makes (K not a multiple of 8) lie behind
+    other work of the current stream; a step on another stream waits for them."""
+    v, c = teacher_of(wl, K)
+    a, b = make(wl, 1), make(wl, 1)
+    a.set_teacher(v, c)
+    a.step(0)
+    busy = torch.ones(1 << 26, device="cuda")
+    side = torch.cuda.Stream()
+    b.set_teacher(v, c)                           # a first teacher, replaced while its step may run
+    b.forward(0)
+    torch.cuda.synchronize()
+    b.loss_and_backward(side)
+    for _ in range(200):
+        busy.mul_(1.0)
+    b.set_teacher(v, c)
+    b.loss_and_backward(side)
+    torch.cuda.synchronize()
+    assert torch.equal(a.distill_loss, b.distill_loss) and torch.equal(a.grad, b.grad)
