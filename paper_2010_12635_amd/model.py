@@ -408,7 +408,8 @@ class GCN2:
             if n_mask == 0:
                 raise ValueError("the mask selects no row to learn from")
         K = top_values.shape[1]
-        if K % 8:      # the library's layout: rows padded to a multiple of 8
+        # the library's layout: rows padded to a multiple of 8, aligned to 16 bytes
+        if K % 8 or top_values.data_ptr() % 16 or top_classes.data_ptr() % 16:
             pad = round8(K)
             v = torch.full((self.n, pad), float("-inf"), dtype=top_values.dtype, device=dev)
             c = torch.full((self.n, pad), -1, dtype=torch.int32, device=dev)

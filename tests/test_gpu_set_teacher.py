@@ -53,6 +53,20 @@ def test_ends_of_the_ranges(wl):
         assert m.overflow.item() == 0
 
 
+def test_views_off_alignment(wl):
+    """A contiguous view whose memory starts off 16 bytes is copied."""
+    v, c = teacher_of(wl)
+    vv = torch.empty(v.numel() + 1, dtype=v.dtype, device="cuda")[1:].view_as(v).copy_(v)
+    cc = torch.empty(c.numel() + 1, dtype=c.dtype, device="cuda")[1:].view_as(c).copy_(c)
+    a, b = make(wl, 1), make(wl, 1)
+    a.set_teacher(v, c)
+    b.set_teacher(vv, cc)
+    for m in (a, b):
+        m.step(0)
+    torch.cuda.synchronize()
+    assert torch.equal(a.grad, b.grad) and torch.equal(a.distill_loss, b.distill_loss)
+
+
 @pytest.mark.parametrize("K", [5, 8])
 def test_step_on_another_stream(wl, K):
     """The copies that set_teacher makes (K not a multiple of 8) lie behind
