@@ -6,7 +6,7 @@
 // comparisons a score takes part in.  Measured on MI355X, whole calls, against
 // what a copy of as many bytes takes: 2^21 rows of 64 classes, fp16, K = 8 86 us
 // (71); 200000 rows of 40, fp32, K = 5 16 us (8); 2048 rows of 50001, bf16, K =
-// 64 77 us (40; two passes, the second from L2); one row of 131072, fp32, K = 100
+// 64 72 us (40; two passes, the second from L2); one row of 131072, fp32, K = 100
 // 17.6 us, what one compute unit takes to read it (cut into 16 segments whose
 // lists a second launch joins: 21 us).
 #include <algorithm>
@@ -185,9 +185,26 @@ __global__ __launch_bounds__(NT) void top_row_kernel(TopParams p) {
 // ------------------------------------------------------------- launches ----
 
 constexpr int64_t MAX_BLOCKS = 65536;
-// Rows a lane group takes per iteration (their loads go out together): 2 when
-// that still leaves this many workgroups, else 1.
+// Rows a lane group takes per iteration (their loads go out together): 2 where one
+// would give more than this many workgroups, else 1.  Above, two and one: 2^21 x
+// 64 fp16 85 and 86 us, 2^20 x 64 fp32 76 and 79 (2^18 x 512 fp16, sorted: 237 and
+// 233); below: 200000 x 40 fp32 16.9 and 16.2, 2^18 x 64 fp16 12.6 and 12.3.
 constexpr int64_t R2_GROUPS = 16384;
+// Threads of a long row's workgroup.  256, 512 and 1024 threads, us:
+//   16384 x  1100 fp16  K = 64  131  225  428   K = 128  990 1210 1664
+//    8192 x  4001 fp32  K = 64   58   78  140   K = 256  822  400  473
+//    4096 x 16001 fp16  K = 20   41   39   76   K = 256  546  271  323
+//    2048 x 50001 bf16  K = 64   76   72   77   K = 256  691  192  182
+//     128 x 50001 bf16  K = 64   28   18   14
+//    2048 x 131072 fp32 K = 8   346  331  316
+// Few threads where the pass is short and the bound of list_top close enough
+// (its list grows with K against the threads), many where a row is long or there
+// are not two rows a compute unit.
+constexpr int64_t SHORT_VECS = 1024, MIDDLE_VECS = 4096, LONG_VECS = 8192, FEW_ROWS = 512, SMALL_K = 128;
+int row_threads(int64_t n, int64_t nvec, int64_t K) {
+  if (nvec <= SHORT_VECS && K <= SMALL_K) return 256;
+  return nvec <= MIDDLE_VECS || (nvec <= LONG_VECS && n > FEW_ROWS) ? 512 : 1024;
+}
 
 template <typename T, int LPR, int L>
 hipError_t launch_l(const TopParams& p, hipStream_t s) {
@@ -211,10 +228,11 @@ hipError_t launch_rows(const TopParams& params, hipStream_t s) {
   const int64_t nvec = (params.C + Vec<T>::N - 1) / Vec<T>::N;
   return launch_long_rows(params, 1, [&](const TopParams& p, int64_t rows) {
     const dim3 grid((unsigned)rows);
-    // the bound of step 2 is close where K is small against the threads
-    if (nvec <= 8 * 256 && p.K <= 32) hipLaunchKernelGGL((top_row_kernel<T, 256>), grid, dim3(256), 0, s, p);
-    else if (nvec <= 8 * 512 && p.K <= 64) hipLaunchKernelGGL((top_row_kernel<T, 512>), grid, dim3(512), 0, s, p);
-    else hipLaunchKernelGGL((top_row_kernel<T, 1024>), grid, dim3(1024), 0, s, p);
+    switch (row_threads(p.n, nvec, p.K)) {
+      case 256: hipLaunchKernelGGL((top_row_kernel<T, 256>), grid, dim3(256), 0, s, p); break;
+      case 512: hipLaunchKernelGGL((top_row_kernel<T, 512>), grid, dim3(512), 0, s, p); break;
+      default: hipLaunchKernelGGL((top_row_kernel<T, 1024>), grid, dim3(1024), 0, s, p);
+    }
     return hipGetLastError();
   });
 }
