@@ -14,8 +14,8 @@
 // class, long ones by their passes over the row.  Measured on MI355X, whole
 // calls, against what a copy of as many bytes takes: 2^21 rows of 64 classes,
 // fp16, every filter 268 us (51), without filters 101 us (57); 2048 rows of 7
-// classes, fp32 8.5 us; 1024 rows of 50001, bf16, top-p 107-113 us (20), top-k and
-// top-p 55 us; one row of 131072, fp32, top-k and top-p 20 us.
+// classes, fp32 8.5 us; 1024 rows of 50001, bf16, top-p 107-117 us (20), top-k and
+// top-p 45 us; one row of 131072, fp32, top-k and top-p 20 us.
 #include <algorithm>
 
 #include "internal.h"
@@ -936,33 +936,58 @@ __global__ __launch_bounds__(NT, 4) void sample_row_kernel(SampleParams p) {
 // ------------------------------------------------------------- launches ----
 
 constexpr int64_t MAX_BLOCKS = 65536;
-constexpr int64_t R2_GROUPS = 16384;      // 2 rows a group and iteration from this many workgroups on
+// Rows a lane group takes per iteration: 2 where one would give more than
+// R2_GROUPS workgroups and two rows' registers leave waves enough, else 1.  Two
+// and one, us: without filters 2^21 x 64 fp16 101 and 112, 2^20 x 64 fp32 67 and
+// 71, 2^18 x 512 fp16 116 and 122; with them 2^21 x 32 fp16 126 and 134, x 64 271
+// and 283, 2^20 x 128 299 and 316, but 2^19 x 256 397 and 356, 2^18 x 512 489 and
+// 413, 2^17 x 1000 618 and 647; 2^20 x 64 fp32 189 and 176, 2^19 x 128 238 and
+// 217, 2^18 x 256 298 and 299.  Fewer workgroups: 200000 x 40 fp32 43 and 39.
+constexpr int64_t R2_GROUPS = 16384;
+template <typename T, int LPR, bool FILTER>
+constexpr bool two_rows() { return !FILTER || (sizeof(T) == 2 && LPR != 16 && LPR != 32); }
 
 template <typename T, int LPR, bool FILTER>
 hipError_t launch_filter(const SampleParams& p, hipStream_t s) {
   constexpr int64_t RG = 4 * (64 / LPR);
-  const int r = (p.n + RG - 1) / RG > R2_GROUPS ? 2 : 1;
+  const int r = two_rows<T, LPR, FILTER>() && (p.n + RG - 1) / RG > R2_GROUPS ? 2 : 1;
   const int64_t nb = std::min<int64_t>((p.n + r * RG - 1) / (r * RG), MAX_BLOCKS);
-  if (r == 2)
-    hipLaunchKernelGGL((sample_group_kernel<T, LPR, 2, FILTER>), dim3((unsigned)nb), dim3(256), 0, s, p);
-  else
-    hipLaunchKernelGGL((sample_group_kernel<T, LPR, 1, FILTER>), dim3((unsigned)nb), dim3(256), 0, s, p);
+  if constexpr (two_rows<T, LPR, FILTER>()) {
+    if (r == 2) {
+      hipLaunchKernelGGL((sample_group_kernel<T, LPR, 2, FILTER>), dim3((unsigned)nb), dim3(256), 0, s, p);
+      return hipGetLastError();
+    }
+  }
+  hipLaunchKernelGGL((sample_group_kernel<T, LPR, 1, FILTER>), dim3((unsigned)nb), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 template <typename T, int LPR>
 hipError_t launch_lpr(const SampleParams& p, hipStream_t s) {
   return p.top_k < p.C || p.top_p < 1.0 ? launch_filter<T, LPR, true>(p, s) : launch_filter<T, LPR, false>(p, s);
 }
+// Threads of a long row's workgroup, from both sides of each rule, us.
+// Up to GCN_MAX_TOP classes, 256 and 1024 threads:
+//   16384 x  4001 fp16  k = 20  94  385   k = 64  154  556   k = 128  314  837
+//    2048 x 30001 fp16  k = 64  56   86   k = 128  94  126   k = 256  474  241
+//    1024 x 50001 bf16  k = 50  45   56   k = 200 155  116
+//     256 x 50001 bf16  k = 50  31   25;  2048 x 131072 fp32, k = 50  354  318
+// (as for top scores, the list grows with k against the threads).
+bool small_top(int64_t n, int64_t nvec, int64_t k) { return k <= 128 && (nvec <= 2048 || (nvec <= 8192 && n > 512)); }
+// Other limits, 256 and 512 threads: 16384 x 1100 fp16 174 and 334, x 4001 203 and
+// 358; 4096 x 16001 114 and 123, 2048 x 30001 147 and 103; 512 x 4001 13.0 and
+// 14.4, 512 x 16001 37 and 22.
+bool small_row(int64_t n, int64_t nvec) { return nvec <= 512 || (nvec <= 2048 && n > 1024); }
+
 template <typename T>
 hipError_t launch_rows(const SampleParams& params, hipStream_t s) {
   const int64_t nvec = (params.C + Vec<T>::N - 1) / Vec<T>::N;
   return launch_long_rows(params, 1, [&](const SampleParams& p, int64_t rows) {
     const dim3 grid((unsigned)rows);
     if (p.top_k <= GCN_MAX_TOP) {
-      if (nvec <= 8 * 256 && p.top_k <= 32) hipLaunchKernelGGL((sample_top_kernel<T, 256>), grid, dim3(256), 0, s, p);
+      if (small_top(p.n, nvec, p.top_k)) hipLaunchKernelGGL((sample_top_kernel<T, 256>), grid, dim3(256), 0, s, p);
       else hipLaunchKernelGGL((sample_top_kernel<T, 1024>), grid, dim3(1024), 0, s, p);
     } else {
-      if (nvec <= 8 * 256) hipLaunchKernelGGL((sample_row_kernel<T, 256>), grid, dim3(256), 0, s, p);
+      if (small_row(p.n, nvec)) hipLaunchKernelGGL((sample_row_kernel<T, 256>), grid, dim3(256), 0, s, p);
       else hipLaunchKernelGGL((sample_row_kernel<T, 512>), grid, dim3(512), 0, s, p);
     }
     return hipGetLastError();
