@@ -601,8 +601,10 @@ __global__ __launch_bounds__(1024) void distill_final_kernel(const float* __rest
 // Entries a lane holds: up to 4 (2^21 rows of 64 classes, 32 entries, fp16: 292 us,
 // read again whenever needed about twice that).
 // Rows a group takes per iteration: 2 when one would give more than 16384
-// workgroups (2^21 rows of 64 fp16 classes: 203 us, 4 rows 214: fewer waves hold
-// the registers of 4), and at most 65536 workgroups, each walking on.
+// workgroups, and at most 65536 workgroups, each walking on.  Two and one, us: 2^21
+// x 64 fp16 203 and 207 (four 214: fewer waves hold their registers), with 32
+// entries 294 and 331, 2^18 x 512 222 and 240; with fewer workgroups 2^17 x 64 16.7
+// and 15.9, 2^19 x 64 52.5 and 51.6, 200000 x 40 fp32 33 and 35.
 constexpr int64_t R2_GROUPS = 16384, MAX_BLOCKS = 65536;
 
 int vec_elems(int prec) { return prec == 0 ? 4 : 8; }
@@ -653,15 +655,18 @@ hipError_t launch_group(int lpr, const DistillParams& p, int64_t nb, hipStream_t
 }
 
 // Long rows: a workgroup each where a row fits its registers (512 threads, 16
-// vectors) and there are rows for most compute units; else segments of at
-// least 1024 vectors (4 a thread), SEGMENT_GROUPS workgroups in all if the rows
-// allow, and at most 8192 vectors each (12 rows of 131072 fp32 classes: a
-// workgroup a row 220 us, segments 16.5 us).
-constexpr int64_t ROW_VECS = 8192, SEG_VECS = 1024, ROW_WORKGROUPS = 192, SEGMENT_GROUPS = 512;
+// vectors); rows longer than that, and rows of more than 32768 classes (16-bit) too
+// few for most compute units, in segments of at least 1024 vectors (4 a thread),
+// SEGMENT_GROUPS workgroups in all if the rows allow, and at most 8192 vectors each
+// (12 rows of 131072 fp32 classes: a workgroup a row 220 us, segments 16.5 us).  A
+// workgroup a row and segments, us: 4 x 9001 fp32 13.5 and 16.7, 64 x 32001 fp32
+// 14.6 and 16.5, 64 x 30001 bf16 13.6 and 16.7, 64 x 50001 bf16 19.1 and 16.9, 128 x
+// 50001 20.4 and 18.7, 192 x 50001 21.5 and 23.1, 4 x 60001 19.5 and 16.8.
+constexpr int64_t ROW_VECS = 8192, ROW_CLASSES = 32768, SEG_VECS = 1024, ROW_WORKGROUPS = 192, SEGMENT_GROUPS = 512;
 struct LongPlan { int segs, seg; };                  // segs = 0: a workgroup a row
 LongPlan long_plan(int prec, int64_t n, int64_t C) {
   const int64_t nvec = (C + vec_elems(prec) - 1) / vec_elems(prec);
-  if (nvec <= ROW_VECS && (n >= ROW_WORKGROUPS || nvec <= SEG_VECS)) return {0, 0};
+  if (nvec <= ROW_VECS && (C <= ROW_CLASSES || n >= ROW_WORKGROUPS)) return {0, 0};
   const int64_t want = (SEGMENT_GROUPS + n - 1) / n;
   const int64_t most = (nvec + SEG_VECS - 1) / SEG_VECS, least = (nvec + ROW_VECS - 1) / ROW_VECS;
   const int64_t segs = want > most ? most : want < least ? least : want;

@@ -147,3 +147,14 @@ def test_large_student(n, C, prec):
     z[:, :] = -LOWEST[prec] * np.where(rng.random((n, C)) < 0.5, 1.0, -1.0)
     z[np.arange(n)[:, None], c] = -LOWEST[prec]
     check(z, rng.standard_normal((n, 2)), c, prec, prec, 1.0)
+
+
+@pytest.mark.parametrize("prec", [0, 1], ids=NAMES.get)
+@pytest.mark.parametrize("C", [32768, 32769, 65535, 65536, 65537])
+def test_either_side_of_segments(C, prec):
+    """The widths and row counts at which rows are cut into segments."""
+    rng = np.random.default_rng(C)
+    for n in (2, 191, 192):
+        print(f"[range] segments n={n} C={C} {NAMES[prec]}", flush=True)
+        z = rng.standard_normal((n, C)) * 3
+        check(z, rng.standard_normal((n, 6)) * 2, rng.integers(0, C - 6, (n, 1)) + np.arange(6), prec, prec, 1.5)
