@@ -815,8 +815,8 @@ gcn_status gcn_sample_labels(int64_t n, int64_t C, int64_t ld, int32_t prec, con
   p.kd = 1.4426950408889634074 / p.T;
   p.k = (float)p.kd;
   p.top_k = p.greedy ? 1 : top_k == 0 || top_k > C ? C : top_k;
-  p.top_p = top_p;
-  p.ln_min_p = std::log((double)min_p);                  // min_p = 0: -inf, no limit
+  p.top_p = p.greedy ? 1.0 : (double)top_p;
+  p.ln_min_p = std::log(p.greedy ? 0.0 : (double)min_p);   // min_p = 0: -inf, no limit
   p.labels = labels; p.prob = prob; p.flag = overflow;
   GCN_HIP(sample_launch(prec, p, workspace, s));
   return finish(hipSuccess, s);

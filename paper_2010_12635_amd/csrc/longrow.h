@@ -2,7 +2,8 @@
 // takes a row and reads it once from memory and then, a few passes more, from
 // its die's L2 (one row a compute unit: 32 rows share 4 MiB).  Against keeping
 // the row in registers (8 vectors a thread, unrolled passes that spill): top 64
-// of 2048 rows of 50001 bf16 classes 122 and 221 us.
+// of 2048 rows of 50001 bf16 classes, of 1024 threads, 122 us when that was tried
+// (72 now) and 221.
 #pragma once
 
 #include "sorted.h"
@@ -27,7 +28,7 @@ struct LongRow {
     else return (v * NT + (int)threadIdx.x) * VE;
   }
   // f(scores of a vector, its first class) for the vectors of the thread, four
-  // loads in flight (eight: 80 us instead of 76 for the case above, 48 instead of
+  // loads in flight (eight: 73 us instead of 72 for the case above, 48 instead of
   // 35 for rows of 4001 fp32 classes).  Every lane takes part in each call; past the row's end it
   // gets scores of -inf.
   template <typename F>

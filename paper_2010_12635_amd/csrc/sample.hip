@@ -14,7 +14,7 @@
 // class, long ones by their passes over the row.  Measured on MI355X, whole
 // calls, against what a copy of as many bytes takes: 2^21 rows of 64 classes,
 // fp16, every filter 268 us (51), without filters 101 us (57); 2048 rows of 7
-// classes, fp32 8.5 us; 1024 rows of 50001, bf16, top-p 107-117 us (20), top-k and
+// classes, fp32 8.5 us; 1024 rows of 50001, bf16, top-p 108-115 us (20), top-k and
 // top-p 45 us; one row of 131072, fp32, top-k and top-p 20 us.
 #include <algorithm>
 
@@ -194,7 +194,7 @@ __global__ __launch_bounds__(256) void sample_group_kernel(SampleParams p) {
     for (int r = 0; r < R; ++r) {
       const int64_t row = first + r * RG + slot;
       raw[r][0] = raw[r][1] = make_uint4(0, 0, 0, 0);
-      us[r] = 0.f;
+      us[r] = 0.5f;                                      // greedy: half of one class's weight, no border near
       if (on[r]) {                                       // rows left out are not read
         raw[r][0] = load_row(logits + row * p.ld, col0, C, -INFINITY);
         raw[r][1] = load_row(logits + row * p.ld, col0 + VE, C, -INFINITY);
