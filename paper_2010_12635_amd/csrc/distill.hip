@@ -12,7 +12,7 @@
 // Measured on MI355X, whole calls, against what a copy of as many bytes takes:
 // 2^21 rows of 64 classes, fp16, 8 entries, with base and column sums 203 us
 // (175); 2048 rows of 50001, bf16 117 us (79); 200000 rows of 40, fp32, with
-// base and column sums 34 us (21); 12 rows of 131072, fp32 16.5 us, two of its
+// base and column sums 34 us (21); 12 rows of 131072, fp32 15 us, two of its
 // three launches the segments' two passes.
 #include "internal.h"
 #include "lanes.h"
