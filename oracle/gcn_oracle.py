@@ -386,7 +386,8 @@ def softmax_ce(logits, labels, mask=None, loss_scale=1.0):
     loss = mean over masked rows i of (logsumexp(z_i) - z_i[y_i]);
     dlogits = loss_scale * (softmax(z_i) - onehot(y_i)) / |mask| on masked
     rows and 0 elsewhere; n_correct counts masked rows whose arg-max (lowest
-    index on ties) equals the label.  Returns (loss, dlogits, n_correct)."""
+    index on ties) equals the label.  A row of a negative label counts in |mask|
+    only.  Returns (loss, dlogits, n_correct)."""
     z = np.asarray(logits, np.float64)
     n, c = z.shape
     m = np.ones(n, bool) if mask is None else np.asarray(mask).astype(bool)
@@ -396,6 +397,7 @@ def softmax_ce(logits, labels, mask=None, loss_scale=1.0):
     se = ez.sum(axis=1, keepdims=True)
     lse = zmax[:, 0] + np.log(se[:, 0])
     y = np.asarray(labels, np.int64)
+    m = m & (y >= 0)
     per_row = lse - z[np.arange(n), y]
     loss = per_row[m].sum() / cnt if cnt else 0.0
     sm = ez / se
