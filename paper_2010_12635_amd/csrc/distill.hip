@@ -11,7 +11,7 @@
 // Bound by the read of the scores (and the base) and the write of the gradient.
 // Measured on MI355X, whole calls, against what a copy of as many bytes takes:
 // 2^21 rows of 64 classes, fp16, 8 entries, with base and column sums 203 us
-// (175); 2048 rows of 50001, bf16 117 us (79); 200000 rows of 40, fp32, with
+// (175); 2048 rows of 50001, bf16 111 us (79); 200000 rows of 40, fp32, with
 // base and column sums 34 us (21); 12 rows of 131072, fp32 15 us, two of its
 // three launches the segments' two passes.
 #include "internal.h"
@@ -261,7 +261,25 @@ __global__ __launch_bounds__(256) void distill_group_kernel(DistillParams p) {
 // With k = log2(e) / T powers are of 2: p_c = 2^((z_c - M) k) / S, M = max z.  The
 // difference is taken before the product: z k could leave the range (the lowest
 // finite number is a score), and M k rounded on its own would be off by more than
-// the powers' own exponents where |M| / T is large.
+// the powers' own exponents where |M| / T is large.  In fp16 neither can happen far
+// enough to matter (|z k| < 2^27): there the product is joined with the
+// subtraction, M k rounded, in one instruction with the conversion, and what the
+// rounding left, M k - fl(M k), at most 4 and exact, goes into a factor of the row
+// (16384 rows of 4001 classes with base: 102 us instead of 106).
+template <typename T>
+struct Power {
+  float m, k;
+  __device__ __forceinline__ Power(float M, float k_) : m(M), k(k_) {}
+  __device__ __forceinline__ float operator()(float z) const { return __builtin_amdgcn_exp2f((z - m) * k); }
+  __device__ __forceinline__ float factor() const { return 1.f; }
+};
+template <>
+struct Power<f16> {
+  float mk, k, rest;
+  __device__ __forceinline__ Power(float M, float k_) : mk(M * k_), k(k_), rest(fmaf(M, k_, -mk)) {}
+  __device__ __forceinline__ float operator()(float z) const { return __builtin_amdgcn_exp2f(fmaf(z, k, -mk)); }
+  __device__ __forceinline__ float factor() const { return __builtin_amdgcn_exp2f(-rest); }
+};
 
 // A reference m and a sum of powers 2^((z - m) k) relative to it (0 where m is
 // -inf).
@@ -271,6 +289,17 @@ __device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b, float k) {
   const float fa = a.m > -INFINITY ? __builtin_amdgcn_exp2f((a.m - m) * k) : 0.f;
   const float fb = b.m > -INFINITY ? __builtin_amdgcn_exp2f((b.m - m) * k) : 0.f;
   return {m, a.s * fa + b.s * fb};                   // a NaN stays in s
+}
+// All of the waves' parts at once: a power for each.
+template <int N>
+__device__ __forceinline__ MaxSum join_all(const MaxSum (&part)[N], float k) {
+  float m = part[0].m;
+#pragma unroll
+  for (int i = 1; i < N; ++i) m = fmaxf(m, part[i].m);
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) s += part[i].m > -INFINITY ? part[i].s * __builtin_amdgcn_exp2f((part[i].m - m) * k) : part[i].s * 0.f;
+  return {m, s};
 }
 __device__ __forceinline__ MaxSum wave_join(MaxSum v, float k) {
   const float m = group_max<64>(v.m);
@@ -287,14 +316,15 @@ __device__ __forceinline__ float vector_max(uint4 raw) {
   for (int i = 1; i < Vec<T>::N; ++i) m = fmaxf(m, v[i]);
   return m;
 }
-// Sum of 2^((z - M) k); a lane that has seen only -inf takes M = 0.
+// Sum of 2^((z - M) k), without the factor; a lane that has seen only -inf takes
+// M = 0.
 template <typename T>
-__device__ __forceinline__ float vector_sum(uint4 raw, float M, float k) {
+__device__ __forceinline__ float vector_sum(uint4 raw, Power<T> power) {
   float v[Vec<T>::N];
   unpack<T>(raw, v);
   float s = 0.f;
 #pragma unroll
-  for (int i = 0; i < Vec<T>::N; ++i) s += __builtin_amdgcn_exp2f((v[i] - M) * k);
+  for (int i = 0; i < Vec<T>::N; ++i) s += power(v[i]);
   return s;
 }
 // Keeps the compiler from holding unpacked scores between two passes.
@@ -350,9 +380,7 @@ struct Entry {
   __device__ __forceinline__ void weigh(EntryTable& tab, MaxSum row, float k, float inv_T) const {
     const int w = threadIdx.x >> 6;
     if (w >= TW) return;
-    MaxSum r = tab.part[0];
-#pragma unroll
-    for (int i = 1; i < TW; ++i) r = join(r, tab.part[i], k);
+    const MaxSum r = join_all(tab.part, k);
     // Subtracted first, as in the sum: t k rounded on its own would be off by
     // 2^-24 t k, another amount in q than in the sum, and the q would not sum to
     // 1 (fp16 scores near 60000 at the lowest temperature: one entry's q was 16)
@@ -380,15 +408,15 @@ struct Entry {
 };
 static_assert(TW == 4, "the waves' parts are joined by hand");
 
-// 2^((z - M) k) f, added to the base, of a vector from class c0 on.  Returns
-// whether an element is not finite.
+// 2^((z - M) k) f, added to the base, of a vector from class c0 on; f holds the
+// power's factor.  Returns whether an element is not finite.
 template <typename T>
-__device__ __forceinline__ bool store_gradient(T* d, const T* base, int c0, int C, uint4 raw, float M, float k, float f) {
+__device__ __forceinline__ bool store_gradient(T* d, const T* base, int c0, int C, uint4 raw, Power<T> power, float f) {
   constexpr int VE = Vec<T>::N;
   float g[VE], v[VE];
   unpack<T>(raw, v);
 #pragma unroll
-  for (int i = 0; i < VE; ++i) g[i] = __builtin_amdgcn_exp2f((v[i] - M) * k) * f;
+  for (int i = 0; i < VE; ++i) g[i] = power(v[i]) * f;
   if (base) {
     float bv[VE];
     unpack<T>(load_row(base, c0, C, 0.f), bv);
@@ -410,7 +438,8 @@ __device__ __forceinline__ bool store_base(T* d, const T* base, int c0, int C) {
 // Four waves a SIMD: one row's loads and stores under another's arithmetic.  2048
 // rows of 50001 classes, bf16: 512 threads of 16 vectors 130 us, 1024 of 8 (two
 // rows a compute unit at 64 registers, with spills) 149, 256 of 32 170, segments
-// 146; with streaming stores 117.
+// 146; with streaming stores 117, with the
+// waves' parts joined by a power each instead of two 111.
 template <typename T, int NT, int NV>
 __global__ __launch_bounds__(NT, 4) void distill_row_kernel(DistillParams p) {
   constexpr int VE = Vec<T>::N;
@@ -435,29 +464,30 @@ __global__ __launch_bounds__(NT, 4) void distill_row_kernel(DistillParams p) {
   MaxSum mine{-INFINITY, 0.f};
 #pragma unroll
   for (int v = 0; v < NV; ++v) mine.m = fmaxf(mine.m, vector_max<T>(raw[v]));
-  const float M = mine.m > -INFINITY ? mine.m : 0.f;
+  const Power<T> own(mine.m > -INFINITY ? mine.m : 0.f, k);
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     forget(raw[v]);
-    mine.s += vector_sum<T>(raw[v], M, k);
+    mine.s += vector_sum<T>(raw[v], own);
     forget(raw[v]);
   }
+  mine.s *= own.factor();
   mine = wave_join(mine, k);
   if (lane == 0) s_part[wave] = mine;
   __syncthreads();
-  MaxSum all = s_part[0];
-#pragma unroll
-  for (int i = 1; i < NW; ++i) all = join(all, s_part[i], k);
+  const MaxSum all = join_all(s_part, k);
   const bool counts = e.counts(s_tab);
   e.weigh(s_tab, all, k, p.inv_T);
   const float sc = p.scale * (p.loss_scale ? *p.loss_scale : 1.f);
   const float inv_s = 1.f / all.s;
   if (d) {
+    const Power<T> power(all.m, k);
+    const float f = inv_s * sc * power.factor();
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       const int c0 = (v * NT + t) * VE;
       if (c0 >= C) break;
-      bad |= counts ? store_gradient(d, base, c0, C, raw[v], all.m, k, inv_s * sc) : store_base(d, base, c0, C);
+      bad |= counts ? store_gradient(d, base, c0, C, raw[v], power, f) : store_base(d, base, c0, C);
     }
   }
   __syncthreads();                                   // the row is written, the weights known
@@ -495,20 +525,18 @@ __global__ __launch_bounds__(256) void distill_part_kernel(DistillParams p) {
 #pragma unroll
     for (int q = 1; q < 4; ++q) m = fmaxf(m, vector_max<T>(raw[q]));
     m = fmaxf(mine.m, m);
-    const float M = m > -INFINITY ? m : 0.f;
+    const Power<T> power(m > -INFINITY ? m : 0.f, k);
     mine.s *= mine.m > -INFINITY ? __builtin_amdgcn_exp2f((mine.m - m) * k) : 1.f;
     mine.m = m;
+    float s = 0.f;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) mine.s += vector_sum<T>(raw[q], M, k);
+    for (int q = 0; q < 4; ++q) s += vector_sum<T>(raw[q], power);
+    mine.s += s * power.factor();
   }
   mine = wave_join(mine, k);
   if ((t & 63) == 0) s_part[t >> 6] = mine;
   __syncthreads();
-  if (t == 0) {
-    MaxSum a = s_part[0];
-    for (int i = 1; i < 4; ++i) a = join(a, s_part[i], k);
-    reinterpret_cast<MaxSum*>(p.part_ms)[g.row * p.segs + g.s] = a;
-  }
+  if (t == 0) reinterpret_cast<MaxSum*>(p.part_ms)[g.row * p.segs + g.s] = join_all(s_part, k);
 }
 
 template <typename T>
@@ -538,6 +566,8 @@ __global__ __launch_bounds__(256) void distill_segment_kernel(DistillParams p) {
   const float sc = p.scale * (p.loss_scale ? *p.loss_scale : 1.f);
   const float inv_s = 1.f / all.s;
   if (d) {
+    const Power<T> power(all.m, k);
+    const float f = inv_s * sc * power.factor();
     for (int b = g.lo + t; b < g.hi; b += 4 * 256) {
       uint4 raw[4];
 #pragma unroll
@@ -546,7 +576,7 @@ __global__ __launch_bounds__(256) void distill_segment_kernel(DistillParams p) {
       for (int q = 0; q < 4; ++q) {
         const int c0 = (b + q * 256) * VE;
         if (b + q * 256 >= g.hi) continue;
-        bad |= counts ? store_gradient(d, base, c0, C, raw[q], all.m, k, inv_s * sc) : store_base(d, base, c0, C);
+        bad |= counts ? store_gradient(d, base, c0, C, raw[q], power, f) : store_base(d, base, c0, C);
       }
     }
   }
