@@ -14,7 +14,7 @@
 // class, long ones by their passes over the row.  Measured on MI355X, whole
 // calls, against what a copy of as many bytes takes: 2^21 rows of 64 classes,
 // fp16, every filter 268 us (51), without filters 101 us (57); 2048 rows of 7
-// classes, fp32 8.5 us; 1024 rows of 50001, bf16, top-p 108-115 us (20), top-k and
+// classes, fp32 8.5 us; 1024 rows of 50001, bf16, top-p 102-115 us (20), top-k and
 // top-p 45 us; one row of 131072, fp32, top-k and top-p 20 us.
 #include <algorithm>
 
