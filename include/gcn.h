@@ -564,6 +564,99 @@ gcn_status gcn_optimizer_step_half(int64_t count, void* w, const float* grad, vo
                                    gcn_scaler* state, int32_t* overflow_flag, void* stream);
 
 /* ===========================================================================
+ * Rows in 8 bits: activations kept as a checkpoint for the backward pass, and
+ * products of them with weights in 8-bit integers for a trained model's answers
+ * (the 16-bit levels of Section "Background and Motivation" taken further: half
+ * of the 16-bit levels' bytes for what is kept, twice their matrix rate).
+ *
+ * A row of f values h_k is kept as f codes q_k of one byte and a scale s (fp32),
+ * and stands for the values s q_k.  trunc16(x) is x cut off after 16 significant
+ * bits, so that s q_k is exact in fp32:
+ *   GCN_Q8_SIGNED: s = max(trunc16(max |h_k| / 127), 2^-126); q_k = h_k / s
+ *                  rounded to the nearest whole number, ties to even, in
+ *                  [-127, 127] (int8).
+ *   GCN_Q8_RELU:   for rows after ReLU: s = max(trunc16(max(h_k, 0) / 255),
+ *                  2^-126); q_k = 0 where h_k <= 0, elsewhere h_k / s rounded
+ *                  likewise, at least 1, in [0, 255] (uint8).  q_k > 0 is then
+ *                  h_k > 0 exactly, the mask of ReLU and dropout.
+ * A row that holds a NaN or an infinity gets the scale NaN and codes 0, and sets
+ * *overflow.  Codes lie row by row with leading dimension ld_q, ld_q % 16 == 0
+ * (16-byte loads); columns [f, ld_q) are ignored where codes are read and may
+ * be overwritten with 0 where they are written.  n is at most 2^31 - 1 and a
+ * width at most 65536 (sums of 8-bit products stay within 32 bits;
+ * GCN_ERR_UNSUPPORTED above).  Results do not depend on the timing of the run.
+ * ======================================================================== */
+typedef enum gcn_q8_kind { GCN_Q8_SIGNED = 0, GCN_Q8_RELU = 1 } gcn_q8_kind;
+#define GCN_Q8_MAX_WIDTH 65536
+
+/* gcn_quantize: the codes and scales of the n rows of H (n x f, ld, prec).
+ * Hq: n x f codes (ld_q), scale: fp32 [n].  Asynchronous. */
+gcn_status gcn_quantize(int64_t n, int64_t f, int32_t prec, const void* H, int64_t ld, int32_t kind,
+                        void* Hq, int64_t ld_q, float* scale, int32_t* overflow, void* stream);
+
+/* gcn_dequantize: the values that codes and scales stand for, s q_k rounded
+ * to prec (H: n x f, ld).  *overflow is set if a stored element is not finite
+ * (a row of scale NaN).  Asynchronous. */
+gcn_status gcn_dequantize(int64_t n, int64_t f, int32_t kind, const void* Hq, int64_t ld_q, const float* scale,
+                          int32_t prec, void* H, int64_t ld, int32_t* overflow, void* stream);
+
+/* gcn_quantize_weights: a weight matrix W (f_in x f_out, ld_w, prec) as the
+ * 8-bit product reads it, laid out once for all products with it: column j
+ * becomes a row of GCN_Q8_SIGNED codes.
+ *   Wq:      f_out x f_in codes (int8, ld_wq, ld_wq % 16 == 0)
+ *   w_scale: fp32 [f_out], a scale for each column
+ *   w_sum:   int32 [f_out], the sum of each column's codes
+ * Asynchronous. */
+gcn_status gcn_quantize_weights(int64_t f_in, int64_t f_out, int32_t prec, const void* W, int64_t ld_w,
+                                void* Wq, int64_t ld_wq, float* w_scale, int32_t* w_sum, int32_t* overflow,
+                                void* stream);
+
+/* gcn_transform_q8: gcn_transform from rows and weights in 8 bits,
+ *   S_ij = h_scale[i] w_scale[j] sum_k Hq_ik Wq_jk     (n x f_out, ld_s, prec)
+ * The sum is exact (32-bit integers); it is converted to fp32 and scaled there
+ * (the scales' exponents are added apart, so nothing between overflows), then
+ * rounded to prec.  w_sum (as gcn_quantize_weights writes it) is read with
+ * GCN_Q8_RELU only and may otherwise be NULL.  *overflow is set if a stored
+ * element is not finite.  No workspace.  Asynchronous. */
+gcn_status gcn_transform_q8(int64_t n, int64_t f_in, int64_t f_out, int32_t kind, const void* Hq, int64_t ld_q,
+                            const float* h_scale, const void* Wq, int64_t ld_wq, const float* w_scale,
+                            const int32_t* w_sum, int32_t prec, void* S, int64_t ld_s, int32_t* overflow,
+                            void* stream);
+
+/* gcn_transform_bwd_q8: the backward pass of S = H W (the part of gcn_layer_bwd
+ * behind its aggregation) with H kept in 8 bits.  With H~ = the rows as
+ * gcn_dequantize gives them in prec, and G_S (n x f_out, ld_gs, prec):
+ *   dW       = H~^T G_S            (f_in x ld_w fp32; cols >= f_out set to 0)
+ *   dZ_below = (G_S W^T) * [Hq > 0] / (1 - p_below)   if act_below == RELU
+ *            =  G_S W^T                               if act_below == NONE
+ *              (n x f_in, ld_dz, prec; NULL skips it; not G_S itself)
+ *   dbias_below = column sums of dZ_below before it is rounded (fp32 [f_in
+ *              rounded up to 8], entries past f_in set to 0; may be NULL, needs
+ *              dZ_below)
+ * The mask of RELU is that of the codes: GCN_Q8_RELU only
+ * (GCN_ERR_UNSUPPORTED with GCN_Q8_SIGNED, whose codes round small values to 0).
+ * *overflow is set if a stored element is not finite.  dW and dbias_below are
+ * summed in a fixed order.  workspace: at least
+ * gcn_transform_bwd_q8_workspace_size() bytes.  Asynchronous. */
+gcn_status gcn_transform_bwd_q8_workspace_size(int64_t n, int64_t f_in, int64_t f_out, int32_t prec, size_t* bytes);
+gcn_status gcn_transform_bwd_q8(int64_t n, int64_t f_in, int64_t f_out, int32_t prec, int32_t kind, const void* Hq,
+                                int64_t ld_q, const float* h_scale, const void* W, int64_t ld_w, const void* GS,
+                                int64_t ld_gs, int32_t act_below, float p_below, float* dW, void* dZ_below,
+                                int64_t ld_dz, float* dbias_below, int32_t* overflow, void* workspace,
+                                size_t workspace_bytes, void* stream);
+
+/* gcn_layer_bwd_q8: gcn_layer_bwd with the layer's input kept in 8 bits:
+ * G_S = A_hat dZ and dbias as there, then gcn_transform_bwd_q8 with the
+ * leading dimensions of L (dbias_below has ld_in entries).  An identity input
+ * has nothing to keep (GCN_ERR_INVALID_ARG).  workspace: at least
+ * gcn_layer_bwd_q8_workspace_size() bytes.  Asynchronous. */
+gcn_status gcn_layer_bwd_q8_workspace_size(const gcn_adj* A, const gcn_layer* L, int32_t prec, size_t* bytes);
+gcn_status gcn_layer_bwd_q8(const gcn_adj* A, const gcn_layer* L, int32_t prec, int32_t kind, const void* Hq,
+                            int64_t ld_q, const float* h_scale, const void* W, const void* dZ, int32_t act_below,
+                            float p_below, float* dW, float* dbias, void* dZ_below, float* dbias_below, void* GS,
+                            int32_t* overflow, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ===========================================================================
  * Link prediction: the graph auto-encoder of Section "Graph Auto-Encoders",
  * Eq. (2), A' = sigmoid(Z Z^T) with Z = GCN(A_hat, X), evaluated on sampled
  * vertex pairs (k = 0 .. K-1, K = n_pos + n_neg; pairs k < n_pos are

@@ -822,6 +822,231 @@ gcn_status gcn_sample_labels(int64_t n, int64_t C, int64_t ld, int32_t prec, con
   return finish(hipSuccess, s);
 }
 
+// ---------------------------------------------------------------------------
+// Rows in 8 bits.
+
+namespace {
+
+bool valid_kind(int32_t k) { return k == GCN_Q8_SIGNED || k == GCN_Q8_RELU; }
+
+// n rows of f codes.
+gcn_status check_codes(int64_t n, int64_t f, int32_t kind, int64_t ld_q) {
+  if (!valid_kind(kind)) return GCN_ERR_INVALID_ARG;
+  if (n <= 0 || f <= 0 || ld_q < f) return GCN_ERR_SHAPE;
+  if (ld_q % 16) return GCN_ERR_ALIGNMENT;
+  if (n > INT32_MAX || f > GCN_Q8_MAX_WIDTH) return GCN_ERR_UNSUPPORTED;
+  return GCN_OK;
+}
+
+// An operand of f columns in the storage type.
+gcn_status check_ld(int64_t f, int64_t ld) {
+  if (f <= 0 || ld < f) return GCN_ERR_SHAPE;
+  if (ld % 8) return GCN_ERR_ALIGNMENT;
+  return f > GCN_Q8_MAX_WIDTH ? GCN_ERR_UNSUPPORTED : GCN_OK;
+}
+
+// The weight gradient's partial sums are reduced by one launch.
+constexpr int64_t MAX_DW = (int64_t)1 << 29;
+
+gcn_status check_bwd_q8(int64_t n, int64_t f_in, int64_t f_out, int32_t prec, int32_t kind, const void* Hq,
+                        int64_t ld_q, const float* h_scale, const void* W, int64_t ld_w, const void* GS, int64_t ld_gs,
+                        int32_t act_below, float p_below, const float* dW, const void* dZ_below, int64_t ld_dz,
+                        const float* dbias_below) {
+  if (!valid_prec(prec)) return GCN_ERR_INVALID_ARG;
+  gcn_status st = check_codes(n, f_in, kind, ld_q);
+  if (st == GCN_OK) st = check_ld(f_out, ld_w);
+  if (st == GCN_OK) st = check_ld(f_out, ld_gs);
+  if (st == GCN_OK && dZ_below) st = check_ld(f_in, ld_dz);
+  if (st != GCN_OK) return st;
+  if (f_in * ld_w > MAX_DW) return GCN_ERR_UNSUPPORTED;
+  if (!Hq || !h_scale || !W || !GS || !dW || (dbias_below && !dZ_below)) return GCN_ERR_INVALID_ARG;
+  if (act_below != GCN_ACT_NONE && act_below != GCN_ACT_RELU) return GCN_ERR_INVALID_ARG;
+  if (!(p_below >= 0.f && p_below < 1.f)) return GCN_ERR_INVALID_ARG;
+  if (dZ_below && act_below == GCN_ACT_RELU && kind != GCN_Q8_RELU) return GCN_ERR_UNSUPPORTED;
+  if (!aligned16(Hq) || !aligned16(h_scale) || !aligned16(W) || !aligned16(GS) || !aligned16(dW) ||
+      (dZ_below && !aligned16(dZ_below)) || (dbias_below && !aligned16(dbias_below)))
+    return GCN_ERR_ALIGNMENT;
+  return GCN_OK;
+}
+
+hipError_t run_bwd_q8(int64_t n, int64_t f_in, int64_t f_out, int32_t prec, int32_t kind, const void* Hq, int64_t ld_q,
+                      const float* h_scale, const void* W, int64_t ld_w, const void* GS, int64_t ld_gs,
+                      int32_t act_below, float p_below, float* dW, void* dZ_below, int64_t ld_dz, float* dbias_below,
+                      int32_t* overflow, float* ws, hipStream_t s) {
+  BwdQ8Params p{};
+  p.n = n; p.M = f_in; p.N = f_out; p.kind = kind;
+  p.Hq = static_cast<const uint8_t*>(Hq); p.ld_q = ld_q; p.scale = h_scale;
+  p.W = W; p.ldw = ld_w; p.G = GS; p.ldg = ld_gs; p.dZ = dZ_below; p.ldz = ld_dz;
+  p.relu = act_below == GCN_ACT_RELU;
+  p.keep = p.relu ? 1.f / (1.f - p_below) : 1.f;
+  p.flag = overflow;
+  const Epilogue ew = base_epi(dW, ld_w, f_in, f_out, EPI_F32, overflow);
+  const Epilogue eb = base_epi(dbias_below, (f_in + 7) / 8 * 8, 1, f_in, EPI_F32, overflow);
+  return bwd_q8_launch(prec, p, ew, dbias_below ? &eb : nullptr, ws, s);
+}
+
+// Scratch of gcn_layer_bwd_q8: column sums of dZ, then the aggregation's or the
+// product's.
+struct LayerQ8Plan { int64_t cs, step; };
+LayerQ8Plan plan_layer_q8(const gcn_adj* A, const gcn_layer* L, int32_t prec) {
+  LayerQ8Plan p;
+  p.cs = A->format != GCN_CSR ? dense_agg_colsum_rows(prec, A->n) * L->f_out : colsum_partials_floats(A->n, L->ld_out);
+  p.cs = (p.cs + 63) / 64 * 64;
+  p.step = std::max<int64_t>((int64_t)(aggregate_bytes(A, prec, L->f_out) / sizeof(float)),
+                             bwd_q8_floats(prec, A->n, L->f_in, L->f_out));
+  return p;
+}
+size_t plan_bytes(const LayerQ8Plan& p) { return (size_t)(p.cs + p.step) * sizeof(float) + 256; }
+
+}  // namespace
+
+gcn_status gcn_quantize(int64_t n, int64_t f, int32_t prec, const void* H, int64_t ld, int32_t kind, void* Hq,
+                        int64_t ld_q, float* scale, int32_t* overflow, void* stream) {
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (!valid_prec(prec)) return GCN_ERR_INVALID_ARG;
+  gcn_status st = check_codes(n, f, kind, ld_q);
+  if (st == GCN_OK) st = check_ld(f, ld);
+  if (st != GCN_OK) return st;
+  if (!H || !Hq || !scale) return GCN_ERR_INVALID_ARG;
+  if (!aligned16(H) || !aligned16(Hq) || !aligned16(scale)) return GCN_ERR_ALIGNMENT;
+  GCN_HIP(quantize_launch(prec, kind, n, f, H, ld, Hq, ld_q, scale, overflow, s));
+  return finish(hipSuccess, s);
+}
+
+gcn_status gcn_dequantize(int64_t n, int64_t f, int32_t kind, const void* Hq, int64_t ld_q, const float* scale,
+                          int32_t prec, void* H, int64_t ld, int32_t* overflow, void* stream) {
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (!valid_prec(prec)) return GCN_ERR_INVALID_ARG;
+  gcn_status st = check_codes(n, f, kind, ld_q);
+  if (st == GCN_OK) st = check_ld(f, ld);
+  if (st != GCN_OK) return st;
+  if (!H || !Hq || !scale) return GCN_ERR_INVALID_ARG;
+  if (!aligned16(H) || !aligned16(Hq) || !aligned16(scale)) return GCN_ERR_ALIGNMENT;
+  GCN_HIP(dequantize_launch(prec, kind, n, f, Hq, ld_q, scale, H, ld, overflow, s));
+  return finish(hipSuccess, s);
+}
+
+gcn_status gcn_quantize_weights(int64_t f_in, int64_t f_out, int32_t prec, const void* W, int64_t ld_w, void* Wq,
+                                int64_t ld_wq, float* w_scale, int32_t* w_sum, int32_t* overflow, void* stream) {
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (!valid_prec(prec)) return GCN_ERR_INVALID_ARG;
+  gcn_status st = check_codes(f_out, f_in, GCN_Q8_SIGNED, ld_wq);
+  if (st == GCN_OK) st = check_ld(f_out, ld_w);
+  if (st != GCN_OK) return st;
+  if (!W || !Wq || !w_scale || !w_sum) return GCN_ERR_INVALID_ARG;
+  if (!aligned16(W) || !aligned16(Wq) || !aligned16(w_scale) || !aligned16(w_sum)) return GCN_ERR_ALIGNMENT;
+  GCN_HIP(quantize_weights_launch(prec, f_in, f_out, W, ld_w, Wq, ld_wq, w_scale, w_sum, overflow, s));
+  return finish(hipSuccess, s);
+}
+
+gcn_status gcn_transform_q8(int64_t n, int64_t f_in, int64_t f_out, int32_t kind, const void* Hq, int64_t ld_q,
+                            const float* h_scale, const void* Wq, int64_t ld_wq, const float* w_scale,
+                            const int32_t* w_sum, int32_t prec, void* S, int64_t ld_s, int32_t* overflow,
+                            void* stream) {
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (!valid_prec(prec)) return GCN_ERR_INVALID_ARG;
+  gcn_status st = check_codes(n, f_in, kind, ld_q);
+  if (st == GCN_OK) st = check_codes(f_out, f_in, GCN_Q8_SIGNED, ld_wq);
+  if (st == GCN_OK) st = check_ld(f_out, ld_s);
+  if (st != GCN_OK) return st;
+  if (!Hq || !h_scale || !Wq || !w_scale || !S || (kind == GCN_Q8_RELU && !w_sum)) return GCN_ERR_INVALID_ARG;
+  if (!aligned16(Hq) || !aligned16(h_scale) || !aligned16(Wq) || !aligned16(w_scale) || !aligned16(S) ||
+      (w_sum && !aligned16(w_sum)))
+    return GCN_ERR_ALIGNMENT;
+  ProductQ8Params p{};
+  p.n = n; p.K = f_in; p.N = f_out; p.relu = kind == GCN_Q8_RELU;
+  p.Hq = static_cast<const uint8_t*>(Hq); p.ld_q = ld_q; p.h_scale = h_scale;
+  p.Wq = static_cast<const uint8_t*>(Wq); p.ld_wq = ld_wq; p.w_scale = w_scale; p.w_sum = w_sum;
+  p.S = S; p.ld_s = ld_s; p.flag = overflow;
+  GCN_HIP(product_q8_launch(prec, p, s));
+  return finish(hipSuccess, s);
+}
+
+gcn_status gcn_transform_bwd_q8_workspace_size(int64_t n, int64_t f_in, int64_t f_out, int32_t prec, size_t* bytes) {
+  if (!bytes || !valid_prec(prec)) return GCN_ERR_INVALID_ARG;
+  const int64_t f8 = (f_out + 7) / 8 * 8;
+  gcn_status st = check_codes(n, f_in, GCN_Q8_RELU, (f_in + 15) / 16 * 16);
+  if (st == GCN_OK) st = check_ld(f_out, f8);
+  if (st != GCN_OK) return st;
+  if (f_in * f8 > MAX_DW) return GCN_ERR_UNSUPPORTED;
+  *bytes = (size_t)bwd_q8_floats(prec, n, f_in, f_out) * sizeof(float) + 256;
+  return GCN_OK;
+}
+
+gcn_status gcn_transform_bwd_q8(int64_t n, int64_t f_in, int64_t f_out, int32_t prec, int32_t kind, const void* Hq,
+                                int64_t ld_q, const float* h_scale, const void* W, int64_t ld_w, const void* GS,
+                                int64_t ld_gs, int32_t act_below, float p_below, float* dW, void* dZ_below,
+                                int64_t ld_dz, float* dbias_below, int32_t* overflow, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  gcn_status st = check_bwd_q8(n, f_in, f_out, prec, kind, Hq, ld_q, h_scale, W, ld_w, GS, ld_gs, act_below, p_below,
+                               dW, dZ_below, ld_dz, dbias_below);
+  if (st != GCN_OK) return st;
+  if (!workspace || workspace_bytes < (size_t)bwd_q8_floats(prec, n, f_in, f_out) * sizeof(float) + 256)
+    return GCN_ERR_WORKSPACE;
+  if (!aligned16(workspace)) return GCN_ERR_ALIGNMENT;
+  GCN_HIP(run_bwd_q8(n, f_in, f_out, prec, kind, Hq, ld_q, h_scale, W, ld_w, GS, ld_gs, act_below, p_below, dW, dZ_below,
+                     ld_dz, dbias_below, overflow, static_cast<float*>(workspace), s));
+  return finish(hipSuccess, s);
+}
+
+gcn_status gcn_layer_bwd_q8_workspace_size(const gcn_adj* A, const gcn_layer* L, int32_t prec, size_t* bytes) {
+  if (!bytes || !valid_prec(prec)) return GCN_ERR_INVALID_ARG;
+  gcn_status st = check_adj(A, prec);
+  if (st == GCN_OK) st = check_layer(L);
+  if (st == GCN_OK && L->identity_input) st = GCN_ERR_INVALID_ARG;
+  if (st == GCN_OK) st = check_codes(A->n, L->f_in, GCN_Q8_RELU, (L->f_in + 15) / 16 * 16);
+  if (st == GCN_OK && (L->f_out > GCN_Q8_MAX_WIDTH || L->f_in * L->ld_out > MAX_DW)) st = GCN_ERR_UNSUPPORTED;
+  if (st != GCN_OK) return st;
+  *bytes = plan_bytes(plan_layer_q8(A, L, prec));
+  return GCN_OK;
+}
+
+gcn_status gcn_layer_bwd_q8(const gcn_adj* A, const gcn_layer* L, int32_t prec, int32_t kind, const void* Hq,
+                            int64_t ld_q, const float* h_scale, const void* W, const void* dZ, int32_t act_below,
+                            float p_below, float* dW, float* dbias, void* dZ_below, float* dbias_below, void* GS,
+                            int32_t* overflow, void* workspace, size_t workspace_bytes, void* stream) {
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (!valid_prec(prec)) return GCN_ERR_INVALID_ARG;
+  gcn_status st = check_adj(A, prec);
+  if (st == GCN_OK) st = check_layer(L);
+  if (st == GCN_OK && L->identity_input) st = GCN_ERR_INVALID_ARG;
+  if (st == GCN_OK)
+    st = check_bwd_q8(A->n, L->f_in, L->f_out, prec, kind, Hq, ld_q, h_scale, W, L->ld_out, GS, L->ld_out, act_below,
+                      p_below, dW, dZ_below, L->ld_in, dbias_below);
+  if (st != GCN_OK) return st;
+  if (!dZ) return GCN_ERR_INVALID_ARG;
+  if (!aligned16(dZ) || (dbias && !aligned16(dbias))) return GCN_ERR_ALIGNMENT;
+  const LayerQ8Plan plan = plan_layer_q8(A, L, prec);
+  if (!workspace || workspace_bytes < plan_bytes(plan)) return GCN_ERR_WORKSPACE;
+  if (!aligned16(workspace)) return GCN_ERR_ALIGNMENT;
+  float* cs = static_cast<float*>(workspace);
+  float* ws = cs + plan.cs;
+  const int64_t n = A->n;
+  const bool dense = A->format != GCN_CSR;
+  const Epilogue eg = base_epi(GS, L->ld_out, n, L->f_out, EPI_STORE, overflow);
+  GCN_HIP(aggregate(A, prec, dZ, L->ld_out, L->f_out, eg, ws, (size_t)plan.step * sizeof(float),
+                    dbias && dense ? cs : nullptr, s));
+  if (dbias) {
+    Epilogue eb = base_epi(dbias, L->ld_out, 1, L->f_out, EPI_F32, overflow);
+    RedJob jb;
+    if (dense) {
+      jb = make_job(cs, (int)dense_agg_colsum_rows(prec, n), 1, L->f_out, eb);
+    } else {
+      int nb = 0;
+      GCN_HIP(colsum_partial_launch(prec, dZ, n, L->f_out, L->ld_out, cs, L->ld_out, &nb, s));
+      eb.cols = L->ld_out;
+      jb = make_job(cs, nb, 1, L->ld_out, eb);
+    }
+    GCN_HIP(reduce_partials2(prec, jb, nullptr, s));
+  }
+  GCN_HIP(run_bwd_q8(n, L->f_in, L->f_out, prec, kind, Hq, ld_q, h_scale, W, L->ld_out, GS, L->ld_out, act_below, p_below,
+                     dW, dZ_below, L->ld_in, dbias_below, overflow, ws, s));
+  if (dbias_below && L->ld_in > (L->f_in + 7) / 8 * 8)      // the layer's bias gradient has ld_in entries
+    GCN_HIP(fill_zero(dbias_below + (L->f_in + 7) / 8 * 8, (size_t)(L->ld_in - (L->f_in + 7) / 8 * 8) * sizeof(float), s));
+  return finish(hipSuccess, s);
+}
+
 gcn_status gcn_optimizer_step(int64_t count, float* master, const float* grad, float* m, float* v, void* working,
                               int32_t prec, const gcn_adam_config* cfg, gcn_scaler* state, int32_t* overflow_flag,
                               void* stream) {

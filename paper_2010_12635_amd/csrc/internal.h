@@ -121,6 +121,10 @@ hipError_t tsgemm_launch(int prec, const void* A, int64_t lda, const void* B, in
 int wgrad_splits(int prec, int64_t n, int64_t M, int64_t N);
 hipError_t wgrad_launch(int prec, const void* H, int64_t ldh, const void* G, int64_t ldg, int64_t n, int64_t M,
                         int64_t N, int splits, float* partials, hipStream_t s);
+// The same with H in 8 bits (codes, ldq, a scale for each row; kind as in
+// gcn.h), each value rounded to the storage type before it is multiplied.
+hipError_t wgrad_q8_launch(int prec, const void* Hq, int64_t ldq, const float* scale, int kind, const void* G,
+                           int64_t ldg, int64_t n, int64_t M, int64_t N, int splits, float* partials, hipStream_t s);
 
 // ------------------------------------------------ dense-A_hat aggregation ----
 // Y = epilogue(A_hat X) for dense A_hat (n x lda); ws holds the padded
@@ -252,6 +256,44 @@ hipError_t fill_zero(void* p, size_t bytes, hipStream_t s);
 // segment_scan_scratch_elems(count) int64.
 int64_t segment_scan_scratch_elems(int64_t count);
 hipError_t segment_scan_exclusive(int64_t* data, int64_t count, int64_t* scratch, hipStream_t s);
+
+// ------------------------------------------------------- rows in 8 bits ----
+// The definitions are in gcn.h (gcn_quantize and what follows it).
+hipError_t quantize_launch(int prec, int kind, int64_t n, int64_t f, const void* H, int64_t ld, void* Hq, int64_t ld_q,
+                           float* scale, int32_t* flag, hipStream_t s);
+hipError_t dequantize_launch(int prec, int kind, int64_t n, int64_t f, const void* Hq, int64_t ld_q, const float* scale,
+                             void* H, int64_t ld, int32_t* flag, hipStream_t s);
+hipError_t quantize_weights_launch(int prec, int64_t f_in, int64_t f_out, const void* W, int64_t ld_w, void* Wq,
+                                   int64_t ld_wq, float* scale, int32_t* sum, int32_t* flag, hipStream_t s);
+struct ProductQ8Params {
+  int64_t n, K, N;
+  int relu;                            // codes 0 .. 255 instead of -127 .. 127
+  const uint8_t* Hq; int64_t ld_q;
+  const float* h_scale;                // [n]
+  const uint8_t* Wq; int64_t ld_wq;    // N x K
+  const float* w_scale;                // [N]
+  const int32_t* w_sum;                // [N], relu only
+  void* S; int64_t ld_s;
+  int32_t* flag;
+};
+hipError_t product_q8_launch(int prec, const ProductQ8Params& p, hipStream_t s);
+struct BwdQ8Params {
+  int64_t n, M, N;                     // M columns of H, N of G
+  int kind;
+  const uint8_t* Hq; int64_t ld_q;
+  const float* scale;                  // [n]
+  const void* W; int64_t ldw;          // M x N
+  const void* G; int64_t ldg;
+  void* dZ; int64_t ldz;               // NULL: the weight gradient alone
+  int relu;                            // dZ only where Hq > 0
+  float keep;                          // 1 / (1 - p)
+  int32_t* flag;
+};
+// dw, db: where the weight gradient and (may be NULL) the column sums of dZ go,
+// EPI_F32.  ws: bwd_q8_floats() floats.
+int64_t bwd_q8_floats(int prec, int64_t n, int64_t M, int64_t N);
+hipError_t bwd_q8_launch(int prec, const BwdQ8Params& p, const Epilogue& dw, const Epilogue* db, float* ws,
+                         hipStream_t s);
 
 // ------------------------------------------------------ link prediction ----
 // Pair decoder of Eq. (2) on sampled pairs (see gcn.h for the definitions).

@@ -48,6 +48,11 @@ struct WgParams {
   int64_t n, M, N;
   int64_t span;                           // vertices per workgroup (multiple of KT)
   float* partials;                        // [splits][M][N]
+  // H in 8 bits (format in gcn.h): H is then the codes, ldh in bytes, and a
+  // code byte b stands for scale * ((b ^ flip) - zero), rounded to T
+  const float* scale;                     // [n]
+  uint32_t flip;                          // 0x80808080 for signed codes, else 0
+  float zero;                             // 128 for signed codes, else 0
 };
 
 // One k tile of H and G_S (KT vertices x 128 columns each) cut into VE x VE
@@ -61,12 +66,16 @@ struct WgParams {
 // contiguous bytes of each row), the next ones the other row blocks: with a
 // whole row of column blocks side by side the LDS stores of a wave fell on 16
 // (fp32) or 8 (16-bit) of the 64 banks.
-template <typename T, int NB>
+//   Q8: a thread's block of H comes as VE x VE codes and VE scales, 8 (16-bit) or
+//   4 bytes a row, and is turned into numbers when it is parked in LDS.
+template <typename T, int NB, bool Q8>
 struct Tile {
   static constexpr int VE = Vec<T>::N;
   static constexpr int KT = 8 * VE;                // 64 (16-bit) / 32 (fp32)
   static constexpr int NBLK = VE == 8 ? 1 : 2;     // blocks per thread
   uint4 r[NBLK][VE];
+  uint2 q[Q8 ? VE : 1];                            // Q8: the codes of block 0,
+  float sc[Q8 ? VE : 1];                           // and its rows' scales
   int vrows[NBLK];                                 // rows of the block inside the span
   int vcols[NBLK];                                 // columns of the block inside the operand
 
@@ -99,9 +108,48 @@ struct Tile {
       r[b][i] = ldg16(colp + gk * ld);
     }
   }
+  // The same for a block of codes.
+  __device__ __forceinline__ void load_codes(const WgParams& p, const T* H, int64_t c0, int64_t k0, int64_t kend,
+                                             int64_t kfirst, int blk) {
+    if constexpr (Q8) {
+      int rb, cb;
+      place<WG_B>(blk, rb, cb);
+      const int64_t gc = c0 + (int64_t)cb * VE;
+      const int64_t r0 = k0 + rb * VE;
+      const int64_t nr = kend - r0, ncol = p.M - gc;
+      vrows[0] = nr <= 0 ? 0 : nr >= VE ? VE : (int)nr;
+      vcols[0] = ncol <= 0 ? 0 : ncol >= VE ? VE : (int)ncol;
+      const uint8_t* colp = reinterpret_cast<const uint8_t*>(H) + (gc < p.M ? gc : 0);   // ldh % 16 == 0
+#pragma unroll
+      for (int i = 0; i < VE; ++i) {
+        const int64_t gk = r0 + i < kend ? r0 + i : kfirst;
+        if (VE == 8) q[i] = *reinterpret_cast<const uint2*>(colp + gk * p.ldh);
+        else q[i].x = *reinterpret_cast<const uint32_t*>(colp + gk * p.ldh);
+        sc[i] = p.scale[gk];
+      }
+    }
+  }
+  __device__ __forceinline__ void decode(const WgParams& p) {
+    if constexpr (Q8) {
+#pragma unroll
+      for (int i = 0; i < VE; ++i) {
+        float x[VE];
+#pragma unroll
+        for (int e = 0; e < VE; ++e) {
+          const uint32_t w = (e < 4 ? q[i].x : q[i].y) ^ p.flip;
+          x[e] = ((float)((w >> (8 * (e & 3))) & 0xffu) - p.zero) * sc[i];
+        }
+        r[0][i] = pack<T>(x);
+      }
+    }
+  }
   __device__ __forceinline__ void load(const WgParams& p, const T* H, const T* G, int64_t m0, int64_t n0,
                                        int64_t k0, int64_t kend, int64_t kfirst, int tid) {
-    if (VE == 8) {
+    if constexpr (Q8) {
+      if (VE != 8 || tid < 128) load_codes(p, H, m0, k0, kend, kfirst, tid);
+      if (VE == 8 && tid >= 128 && tid < 128 + NB) load_block<NB>(0, G, p.ldg, n0, p.N, k0, kend, kfirst, tid - 128);
+      if (VE != 8 && tid < 2 * NB) load_block<NB>(NBLK - 1, G, p.ldg, n0, p.N, k0, kend, kfirst, tid);
+    } else if (VE == 8) {
       if (tid < 128) load_block<WG_B>(0, H, p.ldh, m0, p.M, k0, kend, kfirst, tid);
       else if (tid < 128 + NB) load_block<NB>(0, G, p.ldg, n0, p.N, k0, kend, kfirst, tid - 128);
     } else {
@@ -142,7 +190,8 @@ struct Tile {
 #pragma unroll
     for (int j = 0; j < VE; ++j) *reinterpret_cast<uint4*>(dst + j * (KT + VE)) = t[j];
   }
-  __device__ __forceinline__ void store(T* __restrict__ sA, T* __restrict__ sB, int tid) {
+  __device__ __forceinline__ void store(const WgParams& p, T* __restrict__ sA, T* __restrict__ sB, int tid) {
+    if (Q8 && (VE != 8 || tid < 128)) decode(p);
     if (VE == 8) {
       if (tid < 128) store_block<WG_B>(0, sA, tid);
       else if (tid < 128 + NB) store_block<NB>(0, sB, tid - 128);
@@ -159,9 +208,9 @@ struct Tile {
 // every N <= 64 the matrix instructions and the LDS stores bound fp32: n =
 // 200000, 128 x 40, 50.0 us, now 40.8; 134 MB, 27 us at a copy's rate; fp16 n =
 // 2048, 512 x 16 10.1 us, now 6.6).
-template <typename T, int NB>
+template <typename T, int NB, bool Q8>
 __global__ __launch_bounds__(256) void wgrad_kernel(WgParams p) {
-  typedef Tile<T, NB> TileT;
+  typedef Tile<T, NB, Q8> TileT;
   constexpr bool NARROW = NB <= 64;
   constexpr int VE = Vec<T>::N;
   constexpr int KT = TileT::KT;
@@ -209,7 +258,7 @@ __global__ __launch_bounds__(256) void wgrad_kernel(WgParams p) {
   // tile t + 2, multiply tile t
   auto step = [&](TileT& x, int64_t t) {
     const int st = (int)(t & 1);
-    x.store(sA[st], sB[st], tid);
+    x.store(p, sA[st], sB[st], tid);
     __syncthreads();
     if (t + 2 < nt) load(x, t + 2);
     compute(st);
@@ -237,14 +286,14 @@ __global__ __launch_bounds__(256) void wgrad_kernel(WgParams p) {
       }
 }
 
-template <typename T>
+template <typename T, bool Q8>
 hipError_t launch_t(const WgParams& p, int splits, hipStream_t s) {
   dim3 grid((unsigned)splits, (unsigned)((p.M + WG_B - 1) / WG_B), (unsigned)((p.N + WG_B - 1) / WG_B));
-  if (p.N <= 16) hipLaunchKernelGGL((wgrad_kernel<T, 16>), grid, dim3(256), 0, s, p);
-  else if (p.N <= 32) hipLaunchKernelGGL((wgrad_kernel<T, 32>), grid, dim3(256), 0, s, p);
-  else if (p.N <= 48) hipLaunchKernelGGL((wgrad_kernel<T, 48>), grid, dim3(256), 0, s, p);
-  else if (p.N <= 64) hipLaunchKernelGGL((wgrad_kernel<T, 64>), grid, dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((wgrad_kernel<T, 128>), grid, dim3(256), 0, s, p);
+  if (p.N <= 16) hipLaunchKernelGGL((wgrad_kernel<T, 16, Q8>), grid, dim3(256), 0, s, p);
+  else if (p.N <= 32) hipLaunchKernelGGL((wgrad_kernel<T, 32, Q8>), grid, dim3(256), 0, s, p);
+  else if (p.N <= 48) hipLaunchKernelGGL((wgrad_kernel<T, 48, Q8>), grid, dim3(256), 0, s, p);
+  else if (p.N <= 64) hipLaunchKernelGGL((wgrad_kernel<T, 64, Q8>), grid, dim3(256), 0, s, p);
+  else hipLaunchKernelGGL((wgrad_kernel<T, 128, Q8>), grid, dim3(256), 0, s, p);
   return hipGetLastError();
 }
 
@@ -266,13 +315,28 @@ int wgrad_splits(int prec, int64_t n, int64_t M, int64_t N) {
 hipError_t wgrad_launch(int prec, const void* H, int64_t ldh, const void* G, int64_t ldg, int64_t n, int64_t M,
                         int64_t N, int splits, float* partials, hipStream_t s) {
   const int64_t kt = wgrad_kt(prec);
-  WgParams p;
+  WgParams p{};
   p.H = H; p.ldh = ldh; p.G = G; p.ldg = ldg; p.n = n; p.M = M; p.N = N; p.partials = partials;
   p.span = ((n + splits - 1) / splits + kt - 1) / kt * kt;
   switch (prec) {
-    case 0: return launch_t<float>(p, splits, s);
-    case 1: return launch_t<f16>(p, splits, s);
-    case 2: return launch_t<bf16>(p, splits, s);
+    case 0: return launch_t<float, false>(p, splits, s);
+    case 1: return launch_t<f16, false>(p, splits, s);
+    case 2: return launch_t<bf16, false>(p, splits, s);
+  }
+  return hipErrorInvalidValue;
+}
+
+hipError_t wgrad_q8_launch(int prec, const void* Hq, int64_t ldq, const float* scale, int kind, const void* G,
+                           int64_t ldg, int64_t n, int64_t M, int64_t N, int splits, float* partials, hipStream_t s) {
+  const int64_t kt = wgrad_kt(prec);
+  WgParams p{};
+  p.H = Hq; p.ldh = ldq; p.G = G; p.ldg = ldg; p.n = n; p.M = M; p.N = N; p.partials = partials;
+  p.scale = scale; p.flip = kind == GCN_Q8_SIGNED ? 0x80808080u : 0u; p.zero = kind == GCN_Q8_SIGNED ? 128.f : 0.f;
+  p.span = ((n + splits - 1) / splits + kt - 1) / kt * kt;
+  switch (prec) {
+    case 0: return launch_t<float, true>(p, splits, s);
+    case 1: return launch_t<f16, true>(p, splits, s);
+    case 2: return launch_t<bf16, true>(p, splits, s);
   }
   return hipErrorInvalidValue;
 }

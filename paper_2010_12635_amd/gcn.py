@@ -25,12 +25,17 @@ __all__ = [
     "gcn_pair_backward", "gcn_pair_metrics_workspace_size", "gcn_pair_metrics",
     "gcn_top_logits_workspace_size", "gcn_top_logits", "gcn_distill_workspace_size", "gcn_distill",
     "gcn_sample_labels_workspace_size", "gcn_sample_labels",
+    "GCN_Q8_SIGNED", "GCN_Q8_RELU",
+    "gcn_quantize", "gcn_dequantize", "gcn_quantize_weights", "gcn_transform_q8",
+    "gcn_transform_bwd_q8_workspace_size", "gcn_transform_bwd_q8",
+    "gcn_layer_bwd_q8_workspace_size", "gcn_layer_bwd_q8",
 ]
 
 GCN_F32, GCN_F16, GCN_BF16 = 0, 1, 2
 GCN_I32, GCN_I64 = 0, 1
 GCN_CSR, GCN_DENSE, GCN_DENSE_TILED = 0, 1, 2
 GCN_ACT_NONE, GCN_ACT_RELU = 0, 1
+GCN_Q8_SIGNED, GCN_Q8_RELU = 0, 1
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libgcn.so")
 
@@ -46,6 +51,9 @@ EXPORTED = (
     "gcn_cast", "gcn_optimizer_step_half",
     "gcn_top_logits_workspace_size", "gcn_top_logits", "gcn_distill_workspace_size", "gcn_distill",
     "gcn_sample_labels_workspace_size", "gcn_sample_labels",
+    "gcn_quantize", "gcn_dequantize", "gcn_quantize_weights", "gcn_transform_q8",
+    "gcn_transform_bwd_q8_workspace_size", "gcn_transform_bwd_q8",
+    "gcn_layer_bwd_q8_workspace_size", "gcn_layer_bwd_q8",
 )
 
 _DTYPES = {GCN_F32: torch.float32, GCN_F16: torch.float16, GCN_BF16: torch.bfloat16}
@@ -104,6 +112,7 @@ class GcnAdamConfig(ctypes.Structure):
 
 ABI_VERSION = 11          # GCN_ABI_VERSION of the structs and signatures here
 FIX_BIG_PIECES = 32       # GCN_FIX_BIG_PIECES
+Q8_MAX_WIDTH = 65536     # GCN_Q8_MAX_WIDTH
 
 _lib = None
 
@@ -144,6 +153,15 @@ def lib():
         "gcn_distill": (I32, [I64, I64, I64, I32, P, I64, I64, I32, P, P, P, I64, F, F, P, P, P, P, P, P, P, SZ, P]),
         "gcn_sample_labels_workspace_size": (I32, [I64, I64, I32, PSZ]),
         "gcn_sample_labels": (I32, [I64, I64, I64, I32, P, P, P, F, I64, F, F, P, P, P, P, SZ, P]),
+        "gcn_quantize": (I32, [I64, I64, I32, P, I64, I32, P, I64, P, P, P]),
+        "gcn_dequantize": (I32, [I64, I64, I32, P, I64, P, I32, P, I64, P, P]),
+        "gcn_quantize_weights": (I32, [I64, I64, I32, P, I64, P, I64, P, P, P, P]),
+        "gcn_transform_q8": (I32, [I64, I64, I64, I32, P, I64, P, P, I64, P, P, I32, P, I64, P, P]),
+        "gcn_transform_bwd_q8_workspace_size": (I32, [I64, I64, I64, I32, PSZ]),
+        "gcn_transform_bwd_q8": (I32, [I64, I64, I64, I32, I32, P, I64, P, P, I64, P, I64, I32, F, P, P, I64, P, P, P, SZ,
+                                       P]),
+        "gcn_layer_bwd_q8_workspace_size": (I32, [PADJ, PLAY, I32, PSZ]),
+        "gcn_layer_bwd_q8": (I32, [PADJ, PLAY, I32, I32, P, I64, P, P, P, I32, F, P, P, P, P, P, P, P, SZ, P]),
         "gcn_optimizer_step": (I32, [I64, P, P, P, P, P, I32, ctypes.POINTER(GcnAdamConfig), P, P, P]),
         "gcn_transform_workspace_size": (I32, [I64, I64, I64, I32, PSZ]),
         "gcn_transform": (I32, [I64, I64, I64, I32, P, I64, P, I64, P, I64, P, P, SZ, P]),
@@ -326,6 +344,58 @@ def gcn_sample_labels(n, C, ld, prec, logits, mask, u, temperature, top_k, top_p
                                  _ptr(labels), _ptr(prob), _ptr(overflow), _ptr(workspace),
                                  workspace.numel() * workspace.element_size(), _stream(stream))
     _check(st, "gcn_sample_labels")
+
+
+def gcn_quantize(n, f, prec, H, ld, kind, Hq, ld_q, scale, overflow, stream=None):
+    _check(lib().gcn_quantize(n, f, prec, _ptr(H), ld, kind, _ptr(Hq), ld_q, _ptr(scale), _ptr(overflow),
+                              _stream(stream)), "gcn_quantize")
+
+
+def gcn_dequantize(n, f, kind, Hq, ld_q, scale, prec, H, ld, overflow, stream=None):
+    _check(lib().gcn_dequantize(n, f, kind, _ptr(Hq), ld_q, _ptr(scale), prec, _ptr(H), ld, _ptr(overflow),
+                                _stream(stream)), "gcn_dequantize")
+
+
+def gcn_quantize_weights(f_in, f_out, prec, W, ld_w, Wq, ld_wq, w_scale, w_sum, overflow, stream=None):
+    _check(lib().gcn_quantize_weights(f_in, f_out, prec, _ptr(W), ld_w, _ptr(Wq), ld_wq, _ptr(w_scale), _ptr(w_sum),
+                                      _ptr(overflow), _stream(stream)), "gcn_quantize_weights")
+
+
+def gcn_transform_q8(n, f_in, f_out, kind, Hq, ld_q, h_scale, Wq, ld_wq, w_scale, w_sum, prec, S, ld_s, overflow,
+                     stream=None):
+    _check(lib().gcn_transform_q8(n, f_in, f_out, kind, _ptr(Hq), ld_q, _ptr(h_scale), _ptr(Wq), ld_wq, _ptr(w_scale),
+                                  _ptr(w_sum), prec, _ptr(S), ld_s, _ptr(overflow), _stream(stream)),
+           "gcn_transform_q8")
+
+
+def gcn_transform_bwd_q8_workspace_size(n, f_in, f_out, prec) -> int:
+    b = ctypes.c_size_t(0)
+    _check(lib().gcn_transform_bwd_q8_workspace_size(n, f_in, f_out, prec, ctypes.byref(b)),
+           "gcn_transform_bwd_q8_workspace_size")
+    return b.value
+
+
+def gcn_transform_bwd_q8(n, f_in, f_out, prec, kind, Hq, ld_q, h_scale, W, ld_w, GS, ld_gs, act_below, p_below, dW,
+                         dZ_below, ld_dz, dbias_below, overflow, workspace, stream=None):
+    _check(lib().gcn_transform_bwd_q8(n, f_in, f_out, prec, kind, _ptr(Hq), ld_q, _ptr(h_scale), _ptr(W), ld_w, _ptr(GS),
+                                      ld_gs, act_below, p_below, _ptr(dW), _ptr(dZ_below), ld_dz, _ptr(dbias_below),
+                                      _ptr(overflow), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                      _stream(stream)), "gcn_transform_bwd_q8")
+
+
+def gcn_layer_bwd_q8_workspace_size(adj: GcnAdj, layer: GcnLayer, prec: int) -> int:
+    b = ctypes.c_size_t(0)
+    _check(lib().gcn_layer_bwd_q8_workspace_size(ctypes.byref(adj), ctypes.byref(layer), prec, ctypes.byref(b)),
+           "gcn_layer_bwd_q8_workspace_size")
+    return b.value
+
+
+def gcn_layer_bwd_q8(adj, layer, prec, kind, Hq, ld_q, h_scale, W, dZ, act_below, p_below, dW, dbias, dZ_below, GS,
+                     overflow, workspace, stream=None, dbias_below=None):
+    _check(lib().gcn_layer_bwd_q8(ctypes.byref(adj), ctypes.byref(layer), prec, kind, _ptr(Hq), ld_q, _ptr(h_scale),
+                                  _ptr(W), _ptr(dZ), act_below, p_below, _ptr(dW), _ptr(dbias), _ptr(dZ_below),
+                                  _ptr(dbias_below), _ptr(GS), _ptr(overflow), _ptr(workspace),
+                                  workspace.numel() * workspace.element_size(), _stream(stream)), "gcn_layer_bwd_q8")
 
 
 def gcn_optimizer_step(count, master, grad, m, v, working, prec, cfg: GcnAdamConfig, state, overflow,
