@@ -1,9 +1,9 @@
 // Backward pass of S = H W from H in 8 bits (gcn_transform_bwd_q8):
 //   dW = H~^T G, dZ = (G W^T) * [Hq > 0] / (1 - p), db = column sums of dZ.
 //
-// Both products read G and both need the codes, so up to 128 columns of G one
-// kernel makes all three from one pass over them (n (f_in + (f_in + f_out) s)
-// bytes; bound by HBM in 16 bits, by the matrix instructions in fp32):
+// Both products read G and both need the codes, so up to 256 columns of G (128 in
+// fp32) one kernel makes all three from one pass over them (n (f_in + (f_in +
+// f_out) s) bytes; bound by HBM in 16 bits, by the matrix instructions in fp32):
 //  * A workgroup walks tiles of 64 rows.  Codes and G come straight from memory
 //    into LDS, a tile ahead.  Each wave owns 32 columns of H for good: 32 rows
 //    of W in registers for dZ, a 32 x f_out block of dW in accumulators.  The
@@ -27,6 +27,7 @@
 #include "xpose.h"
 
 #include <algorithm>
+#include <cmath>
 
 namespace gcn {
 
@@ -55,6 +56,10 @@ __device__ __forceinline__ int piece_at(int v, int c) { return (v * C + (c ^ swz
 __device__ __forceinline__ void to_lds_1k(const void* src, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(lds) : "memory", "m0");
 }
+// The same for 4 bytes a lane.
+__device__ __forceinline__ void to_lds_256(const void* src, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(src), "s"(lds) : "memory", "m0");
+}
 typedef __attribute__((address_space(3))) uint8_t lds_byte;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef int i32x2 __attribute__((ext_vector_type(2)));
@@ -64,39 +69,68 @@ typedef int i32x2 __attribute__((ext_vector_type(2)));
 template <typename T> struct Turned { uint4 v; };
 template <> struct Turned<float> { float v[8]; };
 
-template <typename T>
-__device__ __forceinline__ f32x4 turned_mfma(const Turned<T>& a, const Turned<T>& b, f32x4 c) {
+template <typename T, int FI, int NT>
+__device__ __forceinline__ void turned_mfma(const Turned<T> (&a)[FI], const Turned<T>& b, f32x4 (&acc)[FI][NT], int j) {
   if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[j], b.v[j], c, 0, 0, 0);
-    return c;
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int i = 0; i < FI; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i].v[e], b.v[e], acc[i][j], 0, 0, 0);
   } else {
-    return NtMfma<T>::run(a.v, b.v, c);
+#pragma unroll
+    for (int i = 0; i < FI; ++i) acc[i][j] = NtMfma<T>::run(a[i].v, b.v, acc[i][j]);
   }
 }
 
-template <typename T, int NB, int WM>
-__global__ __launch_bounds__(64 * WM) void bwd_q8_kernel(BwdQ8Params p, int64_t tiles, float* partials, float* colsum) {
-  constexpr int VE = Vec<T>::N, FB = 32 * WM;              // columns of H a workgroup takes
+// The smallest size that rounds to infinity in T: its largest number and half a
+// step, a tie that goes to the even side.
+template <typename T> __device__ __forceinline__ float overflow_at() { return __builtin_inff(); }
+template <> __device__ __forceinline__ float overflow_at<f16>() { return 65520.f; }
+template <> __device__ __forceinline__ float overflow_at<bf16>() { return __uint_as_float(0x7f7f8000u); }
+
+// E = 4 or 8 consecutive elements of a row, rounded to T, in 8- or 16-byte
+// stores.
+template <typename T, int E>
+__device__ __forceinline__ void store_cols(T* dst, const float (&x)[E]) {
+  typedef T V __attribute__((ext_vector_type(E)));
+  V v;
+#pragma unroll
+  for (int i = 0; i < E; ++i) v[i] = from_f32<T>(x[i]);
+  if constexpr (E * sizeof(T) == 32) {
+    const uint4* h = reinterpret_cast<const uint4*>(&v);
+    stg16(dst, h[0]);
+    stg16(dst + 4, h[1]);
+  } else {
+    *reinterpret_cast<V*>(dst) = v;
+  }
+}
+
+template <typename T, int NB, int WM, int FI>
+__global__ __launch_bounds__(64 * WM) __attribute__((amdgpu_waves_per_eu(2))) void bwd_q8_kernel(BwdQ8Params p, int64_t tiles, float* partials, int64_t stride, int sums) {
+  constexpr int VE = Vec<T>::N, FW = 16 * FI, FB = FW * WM;  // columns of H a wave and a workgroup take
+  constexpr int XE = 4 * FI;                               // columns of a row of dZ a lane ends with
   constexpr int CC = FB / 16, GC = NB * (int)sizeof(T) / 16;   // 16-byte pieces of a row of codes, of G
   constexpr int CB = TV * FB, GB = TV * GC * 16, STAGE = CB + GB;
+  // fp32: the factor 1 / (1 - p) goes into W, one rounding as it would be in dZ
+  constexpr bool FOLD = sizeof(T) == 4;
   constexpr int KS = (GC + 3) / 4;                         // steps of 64 bytes along f_out
   constexpr int NT = NB / 16;
-  constexpr int STORES = TV / 16 * (int)(8 * sizeof(T) / 16);   // stores of dZ a wave issues for a tile
+  constexpr int HALVES = sizeof(T) == 4 && NB >= 128 ? 1 : 2;   // of a tile at once for dW, registers allowing
+  constexpr int STORES = TV / 16 * (XE * sizeof(T) > 16 ? 2 : 1);   // stores of dZ a wave issues for a tile
   __shared__ __align__(1024) uint8_t lds[2 * STAGE];
   __shared__ __align__(16) float scales[2][TV];
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t m0 = (int64_t)blockIdx.y * FB;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_byte*)lds;
+  const uint32_t scales0 = (uint32_t)(uintptr_t)(lds_byte*)scales;
+  const int64_t step = gridDim.x;
 
-  // this wave's 1 KiB pieces of tile t into a stage; rows past the last one are
-  // copies of it (their scale is 0), pieces past the widths copies of the first
+  // this wave's 1 KiB pieces of tile t into a stage, by wave 0 its scales; rows
+  // past the last one are copies of it, pieces past the widths of the first
   auto issue = [&](int64_t t, int st) {
-#pragma unroll
-    for (int q = 0; q < (STAGE / 1024 + WM - 1) / WM; ++q) {
-      const int pc = q * WM + wave;
-      if (pc >= STAGE / 1024) break;
+#pragma unroll 1
+    for (int pc = wave; pc < STAGE / 1024; pc += WM) {
       const void* src;
       if (pc < CB / 1024) {
         const int at = pc * 64 + lane, row = at / CC;
@@ -109,109 +143,145 @@ __global__ __launch_bounds__(64 * WM) void bwd_q8_kernel(BwdQ8Params p, int64_t 
       }
       to_lds_1k(src, lds0 + st * STAGE + pc * 1024);
     }
+    if (wave == 0) to_lds_256(p.scale + min(t * TV + lane, p.n - 1), scales0 + st * (TV * 4));
   };
-  auto scale_of = [&](int64_t t) { return t * TV + tid < p.n ? p.scale[t * TV + tid] : 0.f; };   // tid < TV
 
-  // 32 rows of W: operand i's row m is column m0 + 32 wave + 8 (m / 4) + 4 i + m % 4 of H
-  const int64_t f0 = m0 + wave * 32;
-  uint4 w[2][KS];
+  // rows of W: operand i's row m is column f0 + XE (m / 4) + 4 i + m % 4 of H
+  const int64_t f0 = m0 + wave * FW;
+  uint4 w[FI][KS];
   int live[KS];                                            // columns of G in this lane's pieces
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) {
     const int64_t left = p.N - (ks * 4 + lg) * VE;
     live[ks] = left <= 0 ? 0 : left >= VE ? VE : (int)left;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int64_t f = min(f0 + 8 * (l16 >> 2) + 4 * i + (l16 & 3), p.M - 1);
+    for (int i = 0; i < FI; ++i) {
+      const int64_t f = min(f0 + XE * (l16 >> 2) + 4 * i + (l16 & 3), p.M - 1);
       w[i][ks] = make_uint4(0, 0, 0, 0);
       if (p.dZ && live[ks]) w[i][ks] = keep_first<T>(ldg16(static_cast<const T*>(p.W) + f * p.ldw + (ks * 4 + lg) * VE), live[ks]);
+      if constexpr (FOLD) {
+        float y[4];
+        unpack<float>(w[i][ks], y);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] *= p.keep;
+        w[i][ks] = pack<float>(y);
+      }
     }
   }
   const bool ragged = p.N < NB;
   const uint32_t flip = p.kind == Q8_SIGNED ? 0x80808080u : 0u;
   const float zero = p.kind == Q8_SIGNED ? -128.f : 0.f;
 
-  f32x4 acc[2][NT];
+  f32x4 acc[FI][NT];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < FI; ++i)
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float sum[8] = {};
-  bool bad = false;
+  // this lane's columns of dZ, within the workgroup's and of all, and those of
+  // them that are columns of H, a byte each
+  const int cc = wave * FW + XE * lg;
+  const int64_t c = m0 + cc;
+  uint32_t cols[FI];
+#pragma unroll
+  for (int i = 0; i < FI; ++i) {
+    const int64_t left = p.M - c - 4 * i;
+    cols[i] = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
+  }
+  const uint32_t every = p.relu ? 0u : ~0u;                // no mask: every code counts
+  float sum[XE] = {}, most = 0.f;                          // sums, and the largest size of any element
 
   // stores of this wave behind the loads waited for: all STORES of the tile
   // before where every column of the wave is stored
-  const bool counted = p.dZ && f0 + 32 <= p.M;
+  const bool counted = p.dZ && f0 + FW <= p.M;
   int64_t t = blockIdx.x;
-  if (tid < TV) scales[0][tid] = scale_of(t);              // the launch has no more workgroups than tiles
-  issue(t, 0);
+  issue(t, 0);                                             // the launch has no more workgroups than tiles
   bool first = true;
-  for (int st = 0; t < tiles; t += gridDim.x, st ^= 1) {
+  for (int st = 0; t < tiles; t += step, st ^= 1) {
     if (counted && !first) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(STORES) : "memory");
     else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
     first = false;
-    const int64_t tn = t + gridDim.x;
-    float next_scale = 0.f;
-    if (tn < tiles) {
-      if (tid < TV) next_scale = scale_of(tn);
-      issue(tn, st ^ 1);
+    if (t + step < tiles) issue(t + step, st ^ 1);
+    if (t * TV + TV > p.n) {                               // rows past the last one: of scale 0
+      if (tid < TV && t * TV + tid >= p.n) scales[st][tid] = 0.f;
+      __syncthreads();
     }
     const uint8_t* cod = lds + st * STAGE;
     const uint8_t* g = cod + CB;
 
     if (p.dZ) {
-#pragma unroll
+#pragma unroll 1
       for (int vt = 0; vt < TV / 16; ++vt) {
         const int v = vt * 16 + l16;
-        f32x4 z[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+        f32x4 z[FI];
+#pragma unroll
+        for (int i = 0; i < FI; ++i) z[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        uint4 gv[KS];
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-          uint4 b = make_uint4(0, 0, 0, 0);
-          if (GC >= 4 || lg < GC) b = *reinterpret_cast<const uint4*>(g + piece_at<GC>(v, ks * 4 + lg));
-          if (ragged) b = keep_first<T>(b, live[ks]);
-#pragma unroll
-          for (int i = 0; i < 2; ++i) z[i] = NtMfma<T>::run(w[i][ks], b, z[i]);
+          gv[ks] = make_uint4(0, 0, 0, 0);
+          if (GC >= 4 || lg < GC) gv[ks] = *reinterpret_cast<const uint4*>(g + piece_at<GC>(v, ks * 4 + lg));
         }
-        uint2 q = make_uint2(~0u, ~0u);
-        if (p.relu) q = *reinterpret_cast<const uint2*>(cod + piece_at<CC>(v, wave * 2 + (lg >> 1)) + 8 * (lg & 1));
-        const int64_t r = t * TV + v, c = f0 + 8 * lg;
-        float x[8];
+        uint32_t q[FI];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint32_t code = ((e < 4 ? q.x : q.y) >> (8 * (e & 3))) & 0xffu;
-          x[e] = code && c + e < p.M ? z[e >> 2][e & 3] * p.keep : 0.f;
+        for (int i = 0; i < FI; ++i)
+          q[i] = *reinterpret_cast<const uint32_t*>(cod + piece_at<CC>(v, cc >> 4) + (cc & 15) + 4 * i);
+        if (ragged) {
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) gv[ks] = keep_first<T>(gv[ks], live[ks]);
+        }
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const uint4 b = gv[ks];
+          if constexpr (sizeof(T) == 4) {                  // in turn: each sum waits for its last addition
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+              for (int i = 0; i < FI; ++i)
+                z[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float((&w[i][ks].x)[e]),
+                                                            __uint_as_float((&b.x)[e]), z[i], 0, 0, 0);
+          } else {
+#pragma unroll
+            for (int i = 0; i < FI; ++i) z[i] = NtMfma<T>::run(w[i][ks], b, z[i]);
+          }
+        }
+        const int64_t r = t * TV + v;
+        float x[XE];
+#pragma unroll
+        for (int i = 0; i < FI; ++i) {
+          uint32_t k = (q[i] | every) & cols[i];
+          k |= (k & 0x7f7f7f7fu) + 0x7f7f7f7fu;            // the top bit of every byte that is not 0
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float y = FOLD ? z[i][e] : z[i][e] * p.keep;
+            x[4 * i + e] = __uint_as_float(__float_as_uint(y) & (uint32_t)((int32_t)(k << (24 - 8 * e)) >> 31));
+          }
         }
         if (r < p.n && c < p.M) {
-          T* dst = static_cast<T*>(p.dZ) + r * p.ldz + c;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) sum[e] += x[e];
-          if constexpr (sizeof(T) == 4) {
-            stg16(dst, pack<float>(x));
-            stg16(dst + 4, pack<float>(x + 4));
-          } else {
-            stg16(dst, pack<T>(x));
+          for (int e = 0; e < XE; ++e) {
+            sum[e] += x[e];
+            most = fmaxf(most, fabsf(x[e]));
           }
-#pragma unroll
-          for (int e = 0; e < 8; ++e) bad |= !finite_f32(to_f32<T>(from_f32<T>(x[e])));
+          store_cols<T, XE>(static_cast<T*>(p.dZ) + r * p.ldz + c, x);
         }
       }
     }
 
-#pragma unroll
+#pragma unroll HALVES
     for (int ks = 0; ks < TV / 32; ++ks) {
       const int v0 = ks * 32 + lg * 8;
       float sc[8];
       *reinterpret_cast<float4*>(sc) = *reinterpret_cast<const float4*>(&scales[st][v0]);
       *reinterpret_cast<float4*>(sc + 4) = *reinterpret_cast<const float4*>(&scales[st][v0 + 4]);
-      Turned<T> a[2];
+      Turned<T> a[FI];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < FI; ++i) {
         const int v = v0 + (l16 >> 1);
         const i32x2 q = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-            (__attribute__((address_space(3))) i32x2*)(cod + piece_at<CC>(v, wave * 2 + i) + 8 * (l16 & 1)));
+            (__attribute__((address_space(3))) i32x2*)(cod + piece_at<CC>(v, wave * FI + i) + 8 * (l16 & 1)));
         float x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -241,18 +311,20 @@ __global__ __launch_bounds__(64 * WM) void bwd_q8_kernel(BwdQ8Params p, int64_t 
                                                            8 * (l16 & 1)));
           __builtin_memcpy(&b.v, h, 16);
         }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) acc[i][j] = turned_mfma<T>(a[i], b, acc[i][j]);
+        turned_mfma<T, FI, NT>(a, b, acc, j);
       }
     }
-    if (tid < TV) scales[st ^ 1][tid] = next_scale;
   }
+  // an element that T cannot hold, or a NaN, which ends in its column's sum
+  bool bad = most >= overflow_at<T>();
+#pragma unroll
+  for (int e = 0; e < XE; ++e) bad |= sum[e] != sum[e];
   if (bad) raise_flag(p.flag);
 
   // rows 4 (lane / 16) + v, column lane % 16 of each 16 x 16 block
-  float* out = partials + (int64_t)blockIdx.x * p.M * p.N;
+  float* out = partials + (int64_t)blockIdx.x * stride;
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < FI; ++i)
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
@@ -260,41 +332,115 @@ __global__ __launch_bounds__(64 * WM) void bwd_q8_kernel(BwdQ8Params p, int64_t 
         const int64_t m = f0 + i * 16 + lg * 4 + v, n = j * 16 + l16;
         if (m < p.M && n < p.N) out[m * p.N + n] = acc[i][j][v];
       }
-  if (!colsum) return;
+  if (!sums) return;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
+  for (int e = 0; e < XE; ++e) {
     const float s = group_sum<16>(sum[e]);
-    if (l16 == 0 && f0 + 8 * lg + e < p.M) colsum[(int64_t)blockIdx.x * p.M + f0 + 8 * lg + e] = s;
+    if (l16 == 0 && f0 + XE * lg + e < p.M) out[p.M * p.N + f0 + XE * lg + e] = s;
   }
 }
 
-constexpr int64_t FUSED_MAX_N = 128;
+// The workgroups' partial sums (`splits` rows of `stride` floats: dW, then db)
+// added in a fixed order: 64 outputs a workgroup, sixteen groups of rows each
+// added in order, then the groups in order.  The workgroups behind the sums
+// clear the padding of dW and db.
+__global__ __launch_bounds__(256) void sum_partials_kernel(const float* __restrict__ partials, int64_t splits,
+                                                           int64_t stride, int64_t M, int64_t N, float* dW, int64_t ldw,
+                                                           float* db, int64_t blocks, int32_t* flag) {
+  const int64_t dw_len = M * N, len = dw_len + (db ? M : 0), db_len = (M + 7) / 8 * 8;
+  if ((int64_t)blockIdx.x >= blocks) {
+    const int64_t at = ((int64_t)blockIdx.x - blocks) * 256 + threadIdx.x, pad = ldw - N;
+    if (at < M * pad) dW[at / pad * ldw + N + at % pad] = 0.f;
+    else if (db && at - M * pad < db_len - M) db[M + at - M * pad] = 0.f;
+    return;
+  }
+  __shared__ __align__(16) float part[16][64];
+  const int c = threadIdx.x & 15, grp = threadIdx.x >> 4;
+  const int64_t base = (int64_t)blockIdx.x * 64, per = (splits + 15) / 16;
+  const int64_t s0 = min(grp * per, splits), s1 = min(s0 + per, splits);
+  const float* src = partials + base + 4 * c;
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+  int64_t s = s0;
+  for (; s + 8 <= s1; s += 8) {
+    float4 v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const float4*>(src + (s + i) * stride);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { a.x += v[i].x; a.y += v[i].y; a.z += v[i].z; a.w += v[i].w; }
+  }
+  for (; s < s1; ++s) {
+    const float4 v = *reinterpret_cast<const float4*>(src + s * stride);
+    a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
+  }
+  *reinterpret_cast<float4*>(&part[grp][4 * c]) = a;
+  __syncthreads();
+  const int64_t at = base + threadIdx.x;
+  if (threadIdx.x >= 64 || at >= len) return;
+  float z = part[0][threadIdx.x];
+#pragma unroll
+  for (int i = 1; i < 16; ++i) z += part[i][threadIdx.x];
+  if (at < dw_len) dW[at / N * ldw + at % N] = z;
+  else db[at - dw_len] = z;
+  if (!finite_f32(z)) raise_flag(flag);
+}
 
-// Workgroups along the rows, each with its own partial sums.
-int64_t fused_splits(int64_t n, int64_t M) {
-  const int64_t fb = M <= 32 ? 32 : M <= 64 ? 64 : 128, blocks = (M + fb - 1) / fb;
-  return std::min((n + TV - 1) / TV, std::max<int64_t>(32, 1024 / blocks));
+int64_t pad64(int64_t x) { return (x + 63) / 64 * 64; }
+int64_t partial_stride(int64_t M, int64_t N) { return pad64(M * N + M); }
+
+hipError_t sum_partials(const float* partials, int64_t splits, const BwdQ8Params& p, const Epilogue& dw,
+                        const Epilogue* db, hipStream_t s) {
+  const int64_t len = p.M * p.N + (db ? p.M : 0), blocks = (len + 63) / 64;
+  const int64_t pad = p.M * (dw.ldo - p.N) + (db ? 7 : 0);
+  hipLaunchKernelGGL(sum_partials_kernel, dim3((unsigned)(blocks + (pad + 255) / 256)), dim3(256), 0, s, partials, splits,
+                     partial_stride(p.M, p.N), p.M, p.N, static_cast<float*>(dw.out), dw.ldo,
+                     db ? static_cast<float*>(db->out) : nullptr, blocks, p.flag);
+  return hipGetLastError();
+}
+
+// fp32 stops at 128: 256 columns would take half as many accumulators again as a
+// wave has registers.
+int64_t fused_max_n(int prec) { return prec == 0 ? 128 : 256; }
+
+int64_t fused_columns(int64_t M) { return M <= 32 ? 32 : M <= 64 ? 64 : 128; }
+
+// Workgroups along the rows, each with its own partial sums: eight waves a
+// compute unit, or fewer where a tile more for each costs less than another row
+// of partial sums to write and read back.  With a tile at 1 us and partial sums
+// at 4 TB/s both ways, tiles / w + w 8 M N / 4e6 is least at w = sqrt(5e5 tiles /
+// (M N)).  Measured (us; 256, 512, 768, 1024 workgroups in all): 2^21 rows, 128 <-
+// 64 fp16 277, 220, 224, 229; 32768 rows, 2048 <- 16 fp16 66, 54, 54, 59; 16384
+// rows, 500 <- 64 bf16 13.4 with 64 along the rows, 20 with 192.
+int64_t fused_splits(int64_t n, int64_t M, int64_t N) {
+  const int64_t fb = fused_columns(M), blocks = (M + fb - 1) / fb, tiles = (n + TV - 1) / TV;
+  const int64_t held = 512 * (128 / fb) / blocks;
+  const int64_t cheap = (int64_t)std::sqrt(5e5 * (double)tiles / ((double)M * (double)N));
+  return std::min({tiles, std::max<int64_t>(1, held), std::max<int64_t>(1, cheap)});
 }
 
 template <typename T, int NB>
-hipError_t fused_nb(const BwdQ8Params& p, float* partials, float* colsum, hipStream_t s) {
-  const int64_t tiles = (p.n + TV - 1) / TV;
-  const int wm = p.M <= 32 ? 1 : p.M <= 64 ? 2 : 4;
-  const dim3 grid((unsigned)fused_splits(p.n, p.M), (unsigned)((p.M + 32 * wm - 1) / (32 * wm)));
-  switch (wm) {
-    case 1: hipLaunchKernelGGL((bwd_q8_kernel<T, NB, 1>), grid, dim3(64), 0, s, p, tiles, partials, colsum); break;
-    case 2: hipLaunchKernelGGL((bwd_q8_kernel<T, NB, 2>), grid, dim3(128), 0, s, p, tiles, partials, colsum); break;
-    default: hipLaunchKernelGGL((bwd_q8_kernel<T, NB, 4>), grid, dim3(256), 0, s, p, tiles, partials, colsum);
+hipError_t fused_nb(const BwdQ8Params& p, float* partials, int sums, hipStream_t s) {
+  // 16 columns of H a wave where 32 would leave registers for one wave a SIMD only
+  constexpr int FI = NB >= 128 ? 1 : 2, W1 = 2 / FI;
+  const int64_t stride = partial_stride(p.M, p.N), tiles = (p.n + TV - 1) / TV;
+  const int fb = (int)fused_columns(p.M);
+  const dim3 grid((unsigned)fused_splits(p.n, p.M, p.N), (unsigned)((p.M + fb - 1) / fb));
+  const dim3 block(64 * W1 * fb / 32);
+  switch (fb) {
+    case 32: hipLaunchKernelGGL((bwd_q8_kernel<T, NB, W1, FI>), grid, block, 0, s, p, tiles, partials, stride, sums); break;
+    case 64: hipLaunchKernelGGL((bwd_q8_kernel<T, NB, 2 * W1, FI>), grid, block, 0, s, p, tiles, partials, stride, sums); break;
+    default: hipLaunchKernelGGL((bwd_q8_kernel<T, NB, 4 * W1, FI>), grid, block, 0, s, p, tiles, partials, stride, sums);
   }
   return hipGetLastError();
 }
 
 template <typename T>
-hipError_t fused_t(const BwdQ8Params& p, float* partials, float* colsum, hipStream_t s) {
-  if (p.N <= 16) return fused_nb<T, 16>(p, partials, colsum, s);
-  if (p.N <= 32) return fused_nb<T, 32>(p, partials, colsum, s);
-  if (p.N <= 64) return fused_nb<T, 64>(p, partials, colsum, s);
-  return fused_nb<T, 128>(p, partials, colsum, s);
+hipError_t fused_t(const BwdQ8Params& p, float* partials, int sums, hipStream_t s) {
+  if (p.N <= 16) return fused_nb<T, 16>(p, partials, sums, s);
+  if (p.N <= 32) return fused_nb<T, 32>(p, partials, sums, s);
+  if (p.N <= 64) return fused_nb<T, 64>(p, partials, sums, s);
+  if constexpr (sizeof(T) == 2)
+    if (p.N > 128) return fused_nb<T, 256>(p, partials, sums, s);
+  return fused_nb<T, 128>(p, partials, sums, s);
 }
 
 // dZ of 64 rows x 64 columns at a time; a workgroup walks the row blocks
@@ -361,43 +507,39 @@ hipError_t dz_t(const BwdQ8Params& p, float* colsum, hipStream_t s) {
   return hipGetLastError();
 }
 
-int64_t pad64(int64_t x) { return (x + 63) / 64 * 64; }
-
 }  // namespace
 
 int64_t bwd_q8_floats(int prec, int64_t n, int64_t M, int64_t N) {
-  if (N <= FUSED_MAX_N) return pad64(fused_splits(n, M) * M * N) + pad64(fused_splits(n, M) * M);
+  if (N <= fused_max_n(prec)) return fused_splits(n, M, N) * partial_stride(M, N);
   return pad64((int64_t)wgrad_splits(prec, n, M, N) * M * N) + pad64(dz_blocks(n, M) * M);
 }
 
 hipError_t bwd_q8_launch(int prec, const BwdQ8Params& p, const Epilogue& dw, const Epilogue* db, float* ws,
                          hipStream_t s) {
-  const bool fused = p.N <= FUSED_MAX_N;
-  const int splits = fused ? (int)fused_splits(p.n, p.M) : wgrad_splits(prec, p.n, p.M, p.N);
-  const int sums = fused ? splits : (int)dz_blocks(p.n, p.M);
+  hipError_t e = hipErrorInvalidValue;
+  if (p.N <= fused_max_n(prec)) {
+    switch (prec) {
+      case 0: e = fused_t<float>(p, ws, db != nullptr, s); break;
+      case 1: e = fused_t<f16>(p, ws, db != nullptr, s); break;
+      case 2: e = fused_t<bf16>(p, ws, db != nullptr, s); break;
+    }
+    return e != hipSuccess ? e : sum_partials(ws, fused_splits(p.n, p.M, p.N), p, dw, db, s);
+  }
+  const int splits = wgrad_splits(prec, p.n, p.M, p.N);
   float* cs = ws + pad64((int64_t)splits * p.M * p.N);
   float* colsum = db ? cs : nullptr;
-  hipError_t e = hipErrorInvalidValue;
-  if (fused) {
+  e = wgrad_q8_launch(prec, p.Hq, p.ld_q, p.scale, p.kind, p.G, p.ldg, p.n, p.M, p.N, splits, ws, s);
+  if (e == hipSuccess && p.dZ) {
     switch (prec) {
-      case 0: e = fused_t<float>(p, ws, colsum, s); break;
-      case 1: e = fused_t<f16>(p, ws, colsum, s); break;
-      case 2: e = fused_t<bf16>(p, ws, colsum, s); break;
-    }
-  } else {
-    e = wgrad_q8_launch(prec, p.Hq, p.ld_q, p.scale, p.kind, p.G, p.ldg, p.n, p.M, p.N, splits, ws, s);
-    if (e == hipSuccess && p.dZ) {
-      switch (prec) {
-        case 0: e = dz_t<float>(p, colsum, s); break;
-        case 1: e = dz_t<f16>(p, colsum, s); break;
-        case 2: e = dz_t<bf16>(p, colsum, s); break;
-      }
+      case 0: e = dz_t<float>(p, colsum, s); break;
+      case 1: e = dz_t<f16>(p, colsum, s); break;
+      case 2: e = dz_t<bf16>(p, colsum, s); break;
     }
   }
   if (e != hipSuccess) return e;
   const RedJob jw = make_job(ws, splits, p.M, p.N, dw);
   if (!db) return reduce_partials2(prec, jw, nullptr, s);
-  const RedJob jb = make_job(cs, sums, 1, p.M, *db);
+  const RedJob jb = make_job(cs, (int)dz_blocks(p.n, p.M), 1, p.M, *db);
   return reduce_partials2(prec, jw, &jb, s);
 }
 
