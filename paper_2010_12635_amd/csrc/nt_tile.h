@@ -81,11 +81,10 @@ struct NtOperands {
 
 // The 64 x 64 tile at (row0, col0) by 2 x 2 waves; acc[i][j]: columns col0 + 32
 // (wave % 2) + 16 i .., rows row0 + 32 (wave / 2) + 16 j ... lds: 16 KB.  Rows
-// and columns outside the operands hold copies of their last ones.  flip: bits
-// of A's dwords turned over.
+// and columns outside the operands hold copies of their last ones.
 template <typename T>
 __device__ __forceinline__ void nt_tile(const NtOperands& p, int64_t row0, int64_t col0, uint8_t* lds,
-                                        typename NtMfma<T>::Acc (&acc)[2][2], uint32_t flip = 0) {
+                                        typename NtMfma<T>::Acc (&acc)[2][2]) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int piece_row = (tid >> 6) * 16 + (tid & 15), off = ((tid >> 4) & 3) * 16;
   const uint8_t* a = p.A + min(row0 + piece_row, p.n - 1) * p.lda;
@@ -102,7 +101,7 @@ __device__ __forceinline__ void nt_tile(const NtOperands& p, int64_t row0, int64
   uint4 va = load(a, 0), vb = load(b, 0);
   int st = 0;
   for (int64_t k = 0; k < p.kbytes; k += 64, st ^= 8192) {
-    *reinterpret_cast<uint4*>(lds + st + tid * 16) = make_uint4(va.x ^ flip, va.y ^ flip, va.z ^ flip, va.w ^ flip);
+    *reinterpret_cast<uint4*>(lds + st + tid * 16) = va;
     *reinterpret_cast<uint4*>(lds + st + 4096 + tid * 16) = vb;
     __syncthreads();
     if (k + 64 < p.kbytes) {
