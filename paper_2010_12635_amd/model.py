@@ -142,16 +142,26 @@ class GCN2:
     A model's scores make a teacher (top_logits), a student learns from one
     beside its labels (set_teacher), and labels can be drawn from a model's own
     distribution (sample_labels).
+
+    Hidden activations can be kept in 8 bits for the backward pass
+    (checkpoint8), and a trained model can answer from 8-bit features,
+    activations and weights (quantize, forward8).
     """
 
     def __init__(self, graph: DeviceGraph, X, labels, mask, W1, W2, b1=None, b2=None, prec=G.GCN_F16,
                  dropout=0.5, seed=0, loss_scale=65536.0, adam: AdamConfig | None = None, device="cuda",
-                 level: str | None = None, device_epoch: bool = False):
+                 level: str | None = None, device_epoch: bool = False, checkpoint8: bool = False):
         """device_epoch: the dropout counter of an epoch is read on the device
         from the loss-scale state (optimiser calls so far) instead of being
         passed by the host, so that one captured epoch (capture()) can be
         replayed; the epoch argument of step() is then ignored, and epochs
-        count from 0 at construction."""
+        count from 0 at construction.
+
+        checkpoint8: the hidden activations are kept for the backward pass as
+        8-bit codes with a scale for each vertex (gcn_quantize) instead of in
+        the storage type; W2's gradient is taken from them (gcn_layer_bwd_q8),
+        the mask of ReLU and dropout stays exact.  H1 and dZ1 then share one
+        buffer: H1 is gone after loss_and_backward()."""
         dev = torch.device(device)
         if level is None:
             level = "O0" if prec == G.GCN_F32 else "O2"
@@ -247,9 +257,14 @@ class GCN2:
         self.loss = torch.zeros(1, dtype=torch.float32, device=dev)
         self.n_correct = torch.zeros(1, dtype=torch.int32, device=dev)
         # activations
-        self.H1 = torch.empty((n, self.ld_h), dtype=self.dt, device=dev)
+        self.checkpoint8 = bool(checkpoint8)
+        self.ld_q = (self.f_h + 15) // 16 * 16
+        self.H1q = self.H1s = None      # H1 in 8 bits: codes and a scale for each vertex
+        if self.checkpoint8:
+            self._alloc_h1q(dev)
         self.SG1 = torch.empty((n, self.ld_h), dtype=self.dt, device=dev)   # S1, later G_S1
         self.dZ1 = torch.empty((n, self.ld_h), dtype=self.dt, device=dev)
+        self.H1 = self.dZ1 if self.checkpoint8 else torch.empty((n, self.ld_h), dtype=self.dt, device=dev)
         self.Z2 = torch.empty((n, self.ld_c), dtype=self.dt, device=dev)
         self.SG2 = torch.empty((n, self.ld_c), dtype=self.dt, device=dev)   # S2, later G_S2
         self.dZ2 = torch.empty((n, self.ld_c), dtype=self.dt, device=dev)
@@ -267,6 +282,7 @@ class GCN2:
         self.graph = None
         ws = max(G.gcn_layer_workspace_size(self.adj, self.L1, prec),
                  G.gcn_layer_workspace_size(self.adj, self.L2, prec),
+                 G.gcn_layer_bwd_q8_workspace_size(self.adj, self.L2, prec) if self.checkpoint8 else 0,
                  G.gcn_loss_workspace_size(n, self.C),
                  0 if self.featureless else G.gcn_transform_workspace_size(n, self.f_in, self.f_h, prec),
                  G.gcn_transform_workspace_size(n, self.f_h, self.C, prec),
@@ -278,7 +294,8 @@ class GCN2:
         self.ws = torch.empty(ws // 4 + 64, dtype=torch.float32, device=dev)
         self.adam_c = self.adam.c()
         self.teacher = None
-        # raised by top_logits and sample_labels (scores that are not finite);
+        self.q8 = None        # what quantize() lays out for forward8()
+        # raised by top_logits, sample_labels and forward8 (scores that are not finite);
         # `overflow` is the training step's, which the optimiser answers by
         # skipping the step
         self.scores_overflow = torch.zeros(1, dtype=torch.int32, device=dev)
@@ -299,6 +316,14 @@ class GCN2:
     def scale_ptr(self):
         return self.scaler.data_ptr()   # first field of gcn_scaler is the float scale
 
+    def _alloc_h1q(self, dev):
+        self.H1q = torch.empty((self.n, self.ld_q), dtype=torch.uint8, device=dev)
+        self.H1s = torch.empty(self.n, dtype=torch.float32, device=dev)
+
+    def _keep_h1(self, flag, stream):
+        G.gcn_quantize(self.n, self.f_h, self.prec, self.H1, self.ld_h, G.GCN_Q8_RELU, self.H1q, self.ld_q, self.H1s, flag,
+                       stream)
+
     def forward(self, epoch: int, training: bool = True, stream=None, agg_timer=None, gemm_timer=None):
         """Both layers.  With ``agg_timer`` (a callable returning a context
         manager), each layer runs as gcn_transform + gcn_aggregate and the
@@ -315,6 +340,8 @@ class GCN2:
         if agg_timer is None:
             G.gcn_layer_fwd(a, self.L1, self.prec, training, self.X, self.W1w(), self.b1m(), self.seed, epoch,
                             self.SG1, self.H1, self.overflow, self.ws, stream)
+            if self.checkpoint8 and training:
+                self._keep_h1(self.overflow, stream)
             G.gcn_layer_fwd(a, self.L2, self.prec, training, self.H1, self.W2w(), self.b2m(), self.seed, epoch,
                             self.SG2, self.Z2, self.overflow, self.ws, stream)
             return
@@ -329,6 +356,8 @@ class GCN2:
             with agg_timer():
                 G.gcn_aggregate(a, L.f_out, self.prec, S, L.ld_out, b, L.act, L.dropout_p, training, self.seed,
                                 L.layer_id, epoch, out, L.ld_out, self.overflow, self.ws, stream)
+            if self.checkpoint8 and training and L is self.L1:
+                self._keep_h1(self.overflow, stream)
 
     def cast_inputs(self, stream=None):
         """O1: the 16-bit copies of X and A_hat that this forward pass's
@@ -363,11 +392,77 @@ class GCN2:
                 self._distill(self.prec, self.Z2, self.dZ2, self.db2(), stream)
             db2 = None
         # db1 (the column sums of dZ1) comes from the call that writes dZ1
-        G.gcn_layer_bwd(a, self.L2, self.prec, self.H1, self.W2w(), self.dZ2, G.GCN_ACT_RELU, self.p,
-                        self.dW2(), db2, self.dZ1, self.SG2, self.overflow, self.ws, stream,
-                        dbias_below=self.db1())
+        if self.checkpoint8:
+            G.gcn_layer_bwd_q8(a, self.L2, self.prec, G.GCN_Q8_RELU, self.H1q, self.ld_q, self.H1s, self.W2w(), self.dZ2,
+                               G.GCN_ACT_RELU, self.p, self.dW2(), db2, self.dZ1, self.SG2, self.overflow, self.ws,
+                               stream, dbias_below=self.db1())
+        else:
+            G.gcn_layer_bwd(a, self.L2, self.prec, self.H1, self.W2w(), self.dZ2, G.GCN_ACT_RELU, self.p,
+                            self.dW2(), db2, self.dZ1, self.SG2, self.overflow, self.ws, stream,
+                            dbias_below=self.db1())
         G.gcn_layer_bwd(a, self.L1, self.prec, self.X, self.W1w(), self.dZ1, G.GCN_ACT_NONE, 0.0,
                         self.dW1(), None, None, self.SG1, self.overflow, self.ws, stream)
+
+    def quantize(self, stream=None):
+        """Lays out in 8 bits what forward8() reads: the features, once, and the
+        weights as they are now (again after further training).  A value that
+        is not finite raises ``scores_overflow``.  Asynchronous."""
+        dev = self.loss.device
+        if self.q8 is None:
+            q = {}
+            if not self.featureless:
+                ld = (self.f_in + 15) // 16 * 16
+                q["X"] = (torch.empty((self.n, ld), dtype=torch.uint8, device=dev),
+                          torch.empty(self.n, dtype=torch.float32, device=dev))
+            for name, L in (("W1", self.L1), ("W2", self.L2)):
+                if not L.identity_input:
+                    q[name] = (torch.empty((L.f_out, (L.f_in + 15) // 16 * 16), dtype=torch.uint8, device=dev),
+                               torch.empty(L.f_out, dtype=torch.float32, device=dev),
+                               torch.empty(L.f_out, dtype=torch.int32, device=dev))
+            if self.H1q is None:
+                self._alloc_h1q(dev)
+            if stream is not None:      # allocated for the current stream
+                stream.wait_stream(torch.cuda.current_stream())
+                for t in [t for ts in q.values() for t in ts] + [self.H1q, self.H1s]:
+                    t.record_stream(stream)
+            if not self.featureless:
+                prec, X = (G.GCN_F32, self.X32) if self.level == "O1" else (self.prec, self.X)
+                G.gcn_quantize(self.n, self.f_in, prec, X, self.ld_x, G.GCN_Q8_SIGNED, q["X"][0], q["X"][0].shape[1],
+                               q["X"][1], self.scores_overflow, stream)
+            self.q8 = q
+        for name, L, W in (("W1", self.L1, self.W1w()), ("W2", self.L2, self.W2w())):
+            if name in self.q8:
+                wq, ws, wsum = self.q8[name]
+                G.gcn_quantize_weights(L.f_in, L.f_out, self.prec, W, L.ld_out, wq, wq.shape[1], ws, wsum,
+                                       self.scores_overflow, stream)
+
+    def forward8(self, stream=None):
+        """The scores of every vertex (Z2, without dropout) from what quantize()
+        laid out: both products in 8-bit integers (gcn_transform_q8), the
+        aggregations, biases and the activation as in forward().  H1, Z2 and the
+        scratch are those of forward(), and so are the rules: not between a
+        step's forward and backward pass.  Scores that are not finite raise
+        ``scores_overflow``."""
+        if self.q8 is None:
+            raise ValueError("forward8() answers from what quantize() lays out: call it first")
+        n, flag, a = self.n, self.scores_overflow, self.adj
+        if self.level == "O1":          # A_hat's 16-bit copy, as in forward()
+            self.cast_inputs(stream)
+        if self.featureless:            # I W1 = W1 is read in place
+            S1 = self.W1w()
+        else:
+            S1, (Xq, Xs) = self.SG1, self.q8["X"]
+            wq, ws, wsum = self.q8["W1"]
+            G.gcn_transform_q8(n, self.f_in, self.f_h, G.GCN_Q8_SIGNED, Xq, Xq.shape[1], Xs, wq, wq.shape[1], ws, wsum,
+                               self.prec, S1, self.ld_h, flag, stream)
+        G.gcn_aggregate(a, self.f_h, self.prec, S1, self.ld_h, self.b1m(), G.GCN_ACT_RELU, 0.0, 0, 0, 0, 0, self.H1,
+                        self.ld_h, flag, self.ws, stream)
+        self._keep_h1(flag, stream)
+        wq, ws, wsum = self.q8["W2"]
+        G.gcn_transform_q8(n, self.f_h, self.C, G.GCN_Q8_RELU, self.H1q, self.ld_q, self.H1s, wq, wq.shape[1], ws, wsum,
+                           self.prec, self.SG2, self.ld_c, flag, stream)
+        G.gcn_aggregate(a, self.C, self.prec, self.SG2, self.ld_c, self.b2m(), G.GCN_ACT_NONE, 0.0, 0, 0, 0, 0, self.Z2,
+                        self.ld_c, flag, self.ws, stream)
 
     def set_teacher(self, top_values, top_classes, mask=None, temperature: float = 2.0, weight: float = 1.0):
         """From now on every step also learns from a teacher's top scores
