@@ -12,7 +12,6 @@
 #include "q8.h"
 
 #include <algorithm>
-#include <type_traits>
 
 namespace gcn {
 
@@ -43,20 +42,49 @@ template <typename T> __device__ __forceinline__ float too_large() { return __bu
 template <> __device__ __forceinline__ float too_large<f16>() { return 65520.f; }
 template <> __device__ __forceinline__ float too_large<bf16>() { return __uint_as_float(0x7f7f8000u); }
 
-// One lane's XE results, columns c .. of row r; those past N, padding, are 0.
-// `most` keeps the largest size.
-template <typename T, bool RAGGED = true>
-__device__ __forceinline__ void store_results(const ProductQ8Params& p, int64_t r, int64_t c, float (&z)[Deal<T>::XE],
-                                              float& most) {
-  constexpr int XE = Deal<T>::XE;
-  if (RAGGED && c + XE > p.N) {
+// A wave's 16 rows of 16 NT results on their way out.  They pass through LDS, in
+// 16-byte parts whose places change with the row (for the banks), so that each
+// store covers whole rows or whole lines of them: stored as the matrix
+// instructions leave them, neighbouring lanes in different rows, 2^21 x 128 by 128
+// took 180 us instead of 153 (fp32 348 instead of 265).
+template <typename T, int NT>
+struct ResultRows {
+  static constexpr int XE = Deal<T>::XE, PARTS = NT * (int)sizeof(T), BYTES = 16 * PARTS * 16;
+  uint8_t* stage;
+  int lane;
+  float most = 0.f;                                        // the largest size of any result
+  __device__ __forceinline__ ResultRows(uint8_t* s, int l) : stage(s), lane(l) {}
+  // Group q's XE columns of this lane's row, of which `left` are columns of S;
+  // the others are padding: 0.
+  __device__ __forceinline__ void put(int q, float (&z)[XE], int left, int strip = 0) {
+    if (left < XE) {
 #pragma unroll
-    for (int e = 0; e < XE; ++e) z[e] = c + e < p.N ? z[e] : 0.f;
+      for (int e = 0; e < XE; ++e) z[e] = e < left ? z[e] : 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < XE; ++e) most = fmaxf(most, fabsf(z[e]));
+    const int row = lane & 15;
+    stg16(stage + strip * BYTES + (row * PARTS + ((q * 4 + (lane >> 4)) ^ (row & (PARTS - 1)))) * 16, pack<T>(z));
   }
+  // The rows from row0 on, 16 a strip; those past the last one are copies of it.
+  template <int STRIPS = 1>
+  __device__ __forceinline__ void store(const ProductQ8Params& p, int64_t row0, int64_t col0) {
+    constexpr int RPS = 64 / PARTS;                        // rows of a store
+    const int row = lane / PARTS, part = lane % PARTS;
+    const int64_t c = col0 + part * Vec<T>::N;
+    const bool all = row0 + 16 * STRIPS <= p.n, here = c < p.N;
+    T* dst = static_cast<T*>(p.S) + (all ? row0 + row : 0) * p.ld_s + c;
+    __builtin_amdgcn_wave_barrier();
 #pragma unroll
-  for (int e = 0; e < XE; ++e) most = fmaxf(most, fabsf(z[e]));
-  stg16(static_cast<T*>(p.S) + r * p.ld_s + c, pack<T>(z));
-}
+    for (int k = 0; k < 16 * STRIPS / RPS; ++k) {
+      const int rk = row + k * RPS;
+      const uint4 v = ldg16(stage + (rk * PARTS + (part ^ (rk & (PARTS - 1)))) * 16);
+      T* at = all ? dst + k * RPS * p.ld_s : dst + min(row0 + rk, p.n - 1) * p.ld_s;
+      if (here) stg16(at, v);
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+};
 
 // Many rows, weights that fit LDS.  A workgroup keeps 16 NT columns of the
 // weights in LDS in the order the matrix instructions take them, with zeros
@@ -95,11 +123,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void p
   }
   large = __syncthreads_or(large);
 
-  constexpr int P = 2;
   const int64_t tiles = (p.n + 15) / 16, step = (int64_t)gridDim.x * 4;
   int64_t t = (int64_t)blockIdx.x * 4 + wave;
-  uint4 a[P][GK];
-  float rs[P];
+  uint4 a[2][GK];
+  float rs[2];
   auto load = [&](uint4 (&x)[GK], float& s, int64_t tile, int g) {
     const int64_t r = min(tile * 16 + l16, p.n - 1);       // past the last row: read, not used
     const uint8_t* row = p.Hq + r * p.ld_q;
@@ -111,7 +138,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void p
     s = p.h_scale[r];
   };
   i32x4 acc[NT];
-  float most = 0.f;
   auto clear = [&]() {                                     // 4 consecutive columns a tile and lane
 #pragma unroll
     for (int i = 0; i < NT; ++i)
@@ -126,16 +152,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void p
       for (int i = 0; i < NT; ++i) acc[i] = NtMfma<int8_t>::run(*reinterpret_cast<const uint4*>(w + i * 1024), f, acc[i]);
     }
   };
-  // whole: every column is stored.  Lanes past the last row hold that row's codes
-  // and store its results again, so that no store lies in a branch and the wait
-  // for codes can count the stores behind them.
-  auto finish = [&](int64_t tile, float s, auto whole) {
-    const int64_t r = min(tile * 16 + l16, p.n - 1);
+  ResultRows<T, NT> out(reinterpret_cast<uint8_t*>(first + BN) + wave * ResultRows<T, NT>::BYTES, lane);
+  const int left = (int)min(p.N - col0 - D::XE * lg, (int64_t)BN);
+  auto finish = [&](int64_t tile, float s) {               // lanes past the last row hold it again
     bad |= !finite_f32(s);
 #pragma unroll
     for (int q = 0; q < NT / D::FI; ++q) {
       const int c = q * 16 * D::FI + D::XE * lg;
-      if (!whole.value && col0 + c >= p.N) continue;
       float z[D::XE];
 #pragma unroll
       for (int e = 0; e < D::XE; ++e) z[e] = ((float)acc[q * D::FI + e / 4][e % 4] * fa[c + e]) * s;
@@ -143,39 +166,35 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void p
 #pragma unroll
         for (int e = 0; e < D::XE; ++e) z[e] *= fb[c + e];
       }
-      store_results<T, !whole.value>(p, r, col0 + c, z, most);
+      out.put(q, z, left - q * 16 * D::FI);
     }
+    out.store(p, tile * 16, col0);
   };
-  // the (tile, group) pairs in order, the codes of the P - 1 pairs after one on
-  // their way while it is multiplied
-  auto walk = [&](auto whole) {
-    int g = 0, ga = 0;
-    int64_t ta = t;
-    auto ahead = [&](int i) {
-      load(a[i], rs[i], ta, ga);
-      if (++ga == groups) { ga = 0; ta += step; }
-    };
+  // the (tile, group) pairs in order, the next pair's codes on their way while
+  // one is multiplied
+  int g = 0, ga = 0;
+  int64_t ta = t;
+  auto ahead = [&](int i) {
+    load(a[i], rs[i], ta, ga);
+    if (++ga == groups) { ga = 0; ta += step; }
+  };
+  ahead(0);
+  clear();
+  while (t < tiles) {
 #pragma unroll
-    for (int i = 0; i < P - 1; ++i) ahead(i);
-    clear();
-    while (true) {
-#pragma unroll
-      for (int i = 0; i < P; ++i) {
-        if (t >= tiles) return;
-        ahead((i + P - 1) % P);
-        multiply(a[i], g);
-        if (++g == groups) {
-          finish(t, rs[i], whole);
-          clear();
-          g = 0;
-          t += step;
-        }
+    for (int i = 0; i < 2; ++i) {
+      if (t >= tiles) break;
+      ahead(1 - i);
+      multiply(a[i], g);
+      if (++g == groups) {
+        finish(t, rs[i]);
+        clear();
+        g = 0;
+        t += step;
       }
     }
-  };
-  if (col0 + BN <= p.N) walk(std::true_type());
-  else walk(std::false_type());
-  if (bad || most >= too_large<T>()) raise_flag(p.flag);
+  }
+  if (bad || out.most >= too_large<T>()) raise_flag(p.flag);
 }
 
 // Few rows: the weights are all there is to read.  A workgroup takes 16 FI
@@ -241,7 +260,12 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void product_few_kernel(ProductQ8Pa
     bad |= !finite_f32(sc);
     z[e] = ((float)(sum[e] + (p.relu ? p.w_sum[ce] * 128 : 0)) * f.a) * s * f.b;
   }
-  store_results<T>(p, r, c, z, most);
+#pragma unroll
+  for (int e = 0; e < D::XE; ++e) {
+    z[e] = c + e < p.N ? z[e] : 0.f;                       // padding
+    most = fmaxf(most, fabsf(z[e]));
+  }
+  stg16(static_cast<T*>(p.S) + r * p.ld_s + c, pack<T>(z));
   if (bad || most >= too_large<T>()) raise_flag(p.flag);
 }
 
@@ -406,34 +430,63 @@ void product_mm_kernel(ProductQ8Params p, int64_t tiles, int64_t per_xcd) {
     bad |= !finite_f32(s);
     large = f.b != 1.f;
   }
-  // lanes past the last row hold that row's results and store them again
-  int64_t r[TM];
   float rs[TM];
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
-    r[i] = min(row0 + ((wave >> 1) * TM + i) * 16 + l16, p.n - 1);
-    rs[i] = p.h_scale[r[i]];
+    rs[i] = p.h_scale[min(row0 + ((wave >> 1) * TM + i) * 16 + l16, p.n - 1)];
     bad |= !finite_f32(rs[i]);
   }
   large = __syncthreads_or(large);
+  const int c0 = (wave & 1) * 16 * TN;                     // the wave's columns within the tile
+  const int left = (int)min(p.N - col0 - c0 - D::XE * lg, (int64_t)BN);
   float most = 0.f;
-  const bool whole = col0 + BN <= p.N;
+  auto results = [&](int i, int q, float (&z)[D::XE]) {
+    const int c = c0 + q * 16 * D::FI + D::XE * lg;
 #pragma unroll
-  for (int q = 0; q < TN / D::FI; ++q) {
-    const int cw = (wave & 1) * 16 * TN + q * 16 * D::FI + D::XE * lg;
-    if (col0 + cw >= p.N) continue;
+    for (int e = 0; e < D::XE; ++e) z[e] = ((float)(acc[i][q * D::FI + e / 4][e % 4] + first[c + e]) * fa[c + e]) * rs[i];
+    if (large) {
+#pragma unroll
+      for (int e = 0; e < D::XE; ++e) z[e] *= fb[c + e];
+    }
+  };
+  if constexpr (sizeof(T) == 4) {                          // 2^15 x 700 by 1000: 67 us, stored directly 99
+    typedef ResultRows<T, TN> Out;
+    constexpr int STRIPS = 2;
+    static_assert(TM % STRIPS == 0 && 4 * STRIPS * Out::BYTES + 12 * BN <= S * NP * 1024, "the ring holds them");
+    Out out(reinterpret_cast<uint8_t*>(first + BN) + wave * (STRIPS * Out::BYTES), lane);
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-      float z[D::XE];
 #pragma unroll
-      for (int e = 0; e < D::XE; ++e)
-        z[e] = ((float)(acc[i][q * D::FI + e / 4][e % 4] + first[cw + e]) * fa[cw + e]) * rs[i];
-      if (large) {
-#pragma unroll
-        for (int e = 0; e < D::XE; ++e) z[e] *= fb[cw + e];
+      for (int q = 0; q < TN / D::FI; ++q) {
+        float z[D::XE];
+        results(i, q, z);
+        out.put(q, z, left - q * 16 * D::FI, i % STRIPS);
       }
-      if (whole) store_results<T, false>(p, r[i], col0 + cw, z, most);
-      else store_results<T, true>(p, r[i], col0 + cw, z, most);
+      if ((i + 1) % STRIPS == 0) out.template store<STRIPS>(p, row0 + ((wave >> 1) * TM + i + 1 - STRIPS) * 16, col0 + c0);
+    }
+    most = out.most;
+  } else {                                                 // 32768 x 2048 by 2048: 160 us, through LDS 165
+    // lanes past the last row hold that row's results and store them again
+    T* dst[TM];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+      dst[i] = static_cast<T*>(p.S) + min(row0 + ((wave >> 1) * TM + i) * 16 + l16, p.n - 1) * p.ld_s + col0 + c0 + D::XE * lg;
+#pragma unroll
+    for (int q = 0; q < TN / D::FI; ++q) {
+      const int lq = left - q * 16 * D::FI;
+      if (lq <= 0) continue;
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        float z[D::XE];
+        results(i, q, z);
+        if (lq < D::XE) {
+#pragma unroll
+          for (int e = 0; e < D::XE; ++e) z[e] = e < lq ? z[e] : 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < D::XE; ++e) most = fmaxf(most, fabsf(z[e]));
+        stg16(dst[i] + q * 16 * D::FI, pack<T>(z));
+      }
     }
   }
   if (bad || most >= too_large<T>()) raise_flag(p.flag);
@@ -441,7 +494,7 @@ void product_mm_kernel(ProductQ8Params p, int64_t tiles, int64_t per_xcd) {
 
 template <typename T, int NT, int GK>
 hipError_t rows_ntgk(const ProductQ8Params& p, int groups, int64_t wgs, hipStream_t s) {
-  const size_t lds = (size_t)groups * GK * NT * 1024 + 16 * NT * 12;
+  const size_t lds = (size_t)groups * GK * NT * 1024 + 16 * NT * (12 + 64 * sizeof(T));
   auto k = product_rows_kernel<T, NT, GK>;
   if (lds > 64 * 1024) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -460,7 +513,8 @@ hipError_t rows_nt(const ProductQ8Params& p, int64_t wgs, hipStream_t s) {
 }
 
 // 80 KB of LDS a workgroup at most, so that two share a compute unit.
-bool rows_fit(int64_t bn, int64_t kb) { return bn * (kb + 12) <= 80 * 1024; }
+template <typename T>
+bool rows_fit(int64_t bn, int64_t kb) { return bn * (kb + 12 + 64 * (int64_t)sizeof(T)) <= 80 * 1024; }
 
 template <typename T, int TM, int TN>
 hipError_t mm_t(const ProductQ8Params& p, hipStream_t s) {
@@ -493,13 +547,13 @@ hipError_t product_t(const ProductQ8Params& p, hipStream_t s) {
   auto cut = [](int64_t x, int64_t by) { return (x + by - 1) / by; };
   // rows: the widest block that fits LDS, narrower where few rows leave compute units idle
   int64_t bn = WIDTH;
-  while (bn < 128 && bn < p.N && rows_fit(2 * bn, kb)) bn *= 2;
+  while (bn < 128 && bn < p.N && rows_fit<T>(2 * bn, kb)) bn *= 2;
   while (bn > WIDTH && cut(p.n, 64) * cut(p.N, bn) < 256) bn /= 2;
   const int64_t blocks = cut(p.N, bn);
   enum { ROWS = 4, FEW = 5 };
   int kind = p.n <= 64 ? FEW : ROWS;
   if (kind == ROWS && p.K >= 64 * MM_MIN_STEPS) {
-    double best = rows_fit(bn, kb) ? (double)p.n * (double)(p.K * blocks + p.N * (int64_t)sizeof(T)) / 4.5e6 + (double)(bn * kb) / 1.6e4
+    double best = rows_fit<T>(bn, kb) ? (double)p.n * (double)(p.K * blocks + p.N * (int64_t)sizeof(T)) / 4.5e6 + (double)(bn * kb) / 1.6e4
                                    : 1e30;
     auto offer = [&](int k, double us) { if (us < best) { best = us; kind = k; } };
     offer(FEW, (double)cut(cut(p.N, WIDTH) * cut(p.n, 32), 256) * (0.11 * steps + 1.5));

@@ -11,15 +11,15 @@ namespace gcn {
 
 namespace {
 
-// Eight consecutive elements of a row from column c0 on as numbers; those past
+// Eight consecutive elements of a row, at column c0, as numbers; those past
 // f count as 0.  ld % 8 == 0, so the whole group lies in the row.
 template <typename T>
-__device__ __forceinline__ void load8(const T* __restrict__ row, int64_t c0, int64_t f, float (&x)[8]) {
+__device__ __forceinline__ void load8(const T* __restrict__ at, int64_t c0, int64_t f, float (&x)[8]) {
   if constexpr (sizeof(T) == 4) {
-    unpack<float>(ldg16_nt(row + c0), x);
-    unpack<float>(ldg16_nt(row + c0 + 4), x + 4);
+    unpack<float>(ldg16_nt(at), x);
+    unpack<float>(ldg16_nt(at + 4), x + 4);
   } else {
-    unpack<T>(ldg16_nt(row + c0), x);
+    unpack<T>(ldg16_nt(at), x);
   }
   if (c0 + 8 > f) {
 #pragma unroll
@@ -28,26 +28,47 @@ __device__ __forceinline__ void load8(const T* __restrict__ row, int64_t c0, int
 }
 
 // What the scale is taken from, as an integer that orders like it: the bits of
-// the largest value (of |h|, or of h where that is positive), or those of a NaN
+// the largest value (of |h|, or of h where that is positive), and from TOP_NAN on
 // if any value is not finite.
+constexpr int TOP_NAN = 0x7f800000;
 template <int KIND>
-__device__ __forceinline__ int top_of(const float (&x)[8], int top) {
+__device__ __forceinline__ int top_of(const float (&x)[8]) {
+  int most = 0, size = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int b = __float_as_int(x[i]), m = b & 0x7fffffff;
-    top = max(top, KIND == Q8_SIGNED ? m : b);
-    if (m >= 0x7f800000) top = 0x7fc00000;
+    const int b = __float_as_int(x[i]);
+    size = max(size, b & 0x7fffffff);
+    if (KIND == Q8_RELU) most = max(most, b);
   }
-  return top;
+  return KIND == Q8_SIGNED || size >= TOP_NAN ? size : most;
 }
-constexpr int TOP_NAN = 0x7f800000;        // and above: not finite
 
+// Eight codes.  h * inv is rounded to a whole number by adding 1.5 2^23, whose
+// low byte is then the code; inv is off by less than 2^-22 of itself, the product
+// by less than 2^-14, so only a lane with a product that near to half takes the
+// exact way (one row in sixteen of 512 values has one).
 template <int KIND>
 __device__ __forceinline__ uint2 codes8(const float (&x)[8], float s, float inv) {
-  uint32_t w[2] = {0, 0};
+  constexpr float WHOLE = 12582912.f;                      // 1.5 2^23
+  uint32_t q[8];
+  float off = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) w[i >> 2] |= ((uint32_t)(int)q8_code<KIND>(x[i], s, inv) & 0xffu) << (8 * (i & 3));
-  return make_uint2(w[0], w[1]);
+  for (int i = 0; i < 8; ++i) {
+    const float h = KIND == Q8_RELU ? fmaxf(x[i], 0.f) : x[i];
+    float r = fmaf(h, inv, WHOLE);
+    off = fmaxf(off, fabsf(fmaf(h, inv, WHOLE - r)));
+    if (KIND == Q8_RELU) r = fmaxf(r, h > 0.f ? WHOLE + 1.f : WHOLE);
+    q[i] = __float_as_uint(r);
+  }
+  if (off > 0.5f - 0x1p-13f) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[i] = (uint32_t)(int)q8_code<KIND>(x[i], s, inv);
+  }
+  auto bytes = [](uint32_t b0, uint32_t b1, uint32_t b2, uint32_t b3) {
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(b3, b2, 0x0c0c0400u), __builtin_amdgcn_perm(b1, b0, 0x0c0c0400u),
+                                 0x05040100u);
+  };
+  return make_uint2(bytes(q[0], q[1], q[2], q[3]), bytes(q[4], q[5], q[6], q[7]));
 }
 
 struct QuantParams {
@@ -69,26 +90,35 @@ __device__ __forceinline__ int group_max_i(int v) {
   return v;
 }
 
-// Rows of up to 8 LPR elements: LPR lanes a row, eight elements a lane.
+// Rows of up to 8 LPR elements: LPR lanes a row, eight elements a lane, ROWS
+// rows' loads on their way at a time.  Bound by HBM, n f (s + 1) bytes.
+constexpr int ROWS = 4;
 template <typename T, int KIND, int LPR>
 __global__ __launch_bounds__(256) void quantize_kernel(QuantParams p) {
   const int li = threadIdx.x % LPR;
-  const int64_t rows = 256 / LPR;
+  const int64_t rows = 256 / LPR, step = (int64_t)gridDim.x * rows;
   const int64_t c0 = (int64_t)li * 8;
   const bool here = c0 < p.f;
+  const T* H = reinterpret_cast<const T*>(p.H) + (here ? c0 : 0);
   bool bad = false;
-  for (int64_t r = (int64_t)blockIdx.x * rows + threadIdx.x / LPR; r < p.n; r += (int64_t)gridDim.x * rows) {
-    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (here) load8<T>(reinterpret_cast<const T*>(p.H) + r * p.ld, c0, p.f, x);
-    const int top = group_max_i<LPR>(top_of<KIND>(x, 0));
-    const bool fin = top < TOP_NAN;
-    const float s = q8_scale<KIND>(__int_as_float(fin ? top : 0)), inv = __builtin_amdgcn_rcpf(s);
-    if (here) {
-      const uint2 w = codes8<KIND>(x, s, inv);
-      *reinterpret_cast<uint2*>(p.Hq + r * p.ld_q + c0) = fin ? w : make_uint2(0, 0);
+  for (int64_t r0 = (int64_t)blockIdx.x * rows + threadIdx.x / LPR; r0 < p.n; r0 += ROWS * step) {
+    float x[ROWS][8];
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k)                         // past the last row: it again, not stored
+      load8<T>(H + min(r0 + k * step, p.n - 1) * p.ld, here ? c0 : 0, p.f, x[k]);
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) {
+      const int64_t r = r0 + k * step;
+      const int top = group_max_i<LPR>(top_of<KIND>(x[k]));
+      const bool fin = top < TOP_NAN;
+      const float s = q8_scale<KIND>(__int_as_float(fin ? top : 0)), inv = __builtin_amdgcn_rcpf(s);
+      const uint2 w = codes8<KIND>(x[k], s, inv);
+      if (r < p.n) {
+        if (here) *reinterpret_cast<uint2*>(p.Hq + r * p.ld_q + c0) = fin ? w : make_uint2(0, 0);
+        if (li == 0) p.scale[r] = fin ? s : __int_as_float(0x7fc00000);
+        bad |= !fin;
+      }
     }
-    if (li == 0) p.scale[r] = fin ? s : __int_as_float(0x7fc00000);
-    bad |= !fin;
   }
   if (bad) raise_flag(p.flag);
 }
@@ -102,15 +132,15 @@ __global__ __launch_bounds__(256) void quantize_long_kernel(QuantParams p) {
   int top = 0;
   for (int64_t c0 = (int64_t)threadIdx.x * 8; c0 < p.f; c0 += 2048) {
     float x[8];
-    load8<T>(row, c0, p.f, x);
-    top = top_of<KIND>(x, top);
+    load8<T>(row + c0, c0, p.f, x);
+    top = max(top, top_of<KIND>(x));
   }
   top = block_reduce<4>(top, sh, MaxF());
   const bool fin = top < TOP_NAN;
   const float s = q8_scale<KIND>(__int_as_float(fin ? top : 0)), inv = __builtin_amdgcn_rcpf(s);
   for (int64_t c0 = (int64_t)threadIdx.x * 8; c0 < p.f; c0 += 2048) {
     float x[8];
-    load8<T>(row, c0, p.f, x);
+    load8<T>(row + c0, c0, p.f, x);
     const uint2 w = codes8<KIND>(x, s, inv);
     *reinterpret_cast<uint2*>(p.Hq + r * p.ld_q + c0) = fin ? w : make_uint2(0, 0);
   }
@@ -127,7 +157,7 @@ hipError_t quantize_t(const QuantParams& p, hipStream_t s) {
   const int64_t u = (p.f + 7) / 8;
 #define GCN_Q(LPR)                                                                                             \
   if (u <= LPR) {                                                                                              \
-    hipLaunchKernelGGL((quantize_kernel<T, KIND, LPR>), dim3(few((p.n * LPR + 255) / 256)), dim3(256), 0, s, p); \
+    hipLaunchKernelGGL((quantize_kernel<T, KIND, LPR>), dim3(few((p.n * LPR + 256 * ROWS - 1) / (256 * ROWS))), dim3(256), 0, s, p); \
     return hipGetLastError();                                                                                  \
   }
   GCN_Q(1) GCN_Q(2) GCN_Q(4) GCN_Q(8) GCN_Q(16) GCN_Q(32) GCN_Q(64)
