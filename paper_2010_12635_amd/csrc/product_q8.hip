@@ -44,9 +44,9 @@ template <> __device__ __forceinline__ float too_large<bf16>() { return __uint_a
 
 // A wave's 16 rows of 16 NT results on their way out.  They pass through LDS, in
 // 16-byte parts whose places change with the row (for the banks), so that each
-// store covers whole rows or whole lines of them: stored as the matrix
-// instructions leave them, neighbouring lanes in different rows, 2^21 x 128 by 128
-// took 180 us instead of 153 (fp32 348 instead of 265).
+// store covers whole lines of them: stored as the matrix instructions leave them,
+// neighbouring lanes in different rows, 2^21 x 128 by 128 took 180 us instead of
+// 152 (fp32 348 instead of 254).
 template <typename T, int NT>
 struct ResultRows {
   static constexpr int XE = Deal<T>::XE, PARTS = NT * (int)sizeof(T), BYTES = 16 * PARTS * 16;
@@ -86,12 +86,18 @@ struct ResultRows {
   }
 };
 
+// 16-column operands whose results leave together in the kernel below: a line of
+// 128 bytes of each row.
+template <typename T, int NT>
+constexpr int ROW_NT = NT * sizeof(T) < 8 ? NT : 8 / (int)sizeof(T);
+
 // Many rows, weights that fit LDS.  A workgroup keeps 16 NT columns of the
 // weights in LDS in the order the matrix instructions take them, with zeros
 // behind the last k, and their factors and first sums (128 times the columns'
 // sums for ReLU codes) beside them; its waves walk 16 rows at a time, whose codes
 // come straight into the second operand, GK steps of 64 bytes ahead.  Nothing is
-// shared after the weights.  Bound by HBM: n (f_in + s f_out) bytes.
+// shared after the weights.  Bound by HBM, n (f_in + s f_out) bytes: 2^21 x 128 by
+// 128 152 us in fp16 (5.3 TB/s), 254 in fp32.
 template <typename T, int NT, int GK>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void product_rows_kernel(ProductQ8Params p, int groups) {
   typedef Deal<T> D;
@@ -152,12 +158,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void p
       for (int i = 0; i < NT; ++i) acc[i] = NtMfma<int8_t>::run(*reinterpret_cast<const uint4*>(w + i * 1024), f, acc[i]);
     }
   };
-  ResultRows<T, NT> out(reinterpret_cast<uint8_t*>(first + BN) + wave * ResultRows<T, NT>::BYTES, lane);
+  typedef ResultRows<T, ROW_NT<T, NT>> Out;
+  Out out(reinterpret_cast<uint8_t*>(first + BN) + wave * Out::BYTES, lane);
   const int left = (int)min(p.N - col0 - D::XE * lg, (int64_t)BN);
   auto finish = [&](int64_t tile, float s) {               // lanes past the last row hold it again
     bad |= !finite_f32(s);
 #pragma unroll
     for (int q = 0; q < NT / D::FI; ++q) {
+      constexpr int GROUPS = ROW_NT<T, NT> / D::FI;        // that go out together
       const int c = q * 16 * D::FI + D::XE * lg;
       float z[D::XE];
 #pragma unroll
@@ -166,9 +174,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void p
 #pragma unroll
         for (int e = 0; e < D::XE; ++e) z[e] *= fb[c + e];
       }
-      out.put(q, z, left - q * 16 * D::FI);
+      out.put(q % GROUPS, z, left - q * 16 * D::FI);
+      if ((q + 1) % GROUPS == 0) out.store(p, tile * 16, col0 + (q + 1 - GROUPS) * 16 * D::FI);
     }
-    out.store(p, tile * 16, col0);
   };
   // the (tile, group) pairs in order, the next pair's codes on their way while
   // one is multiplied
@@ -198,8 +206,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(3))) void p
 }
 
 // Few rows: the weights are all there is to read.  A workgroup takes 16 FI
-// columns and up to 16 RT rows; its eight waves split k (every second piece of
-// 128 bytes), and the sums meet in LDS, exact in any order.
+// columns and up to 16 RT rows; its eight waves split k (steps of 64 bytes in
+// turn), and the sums meet in LDS, exact in any order.  One row by 2048 x 2048:
+// 5.4 us (4.2 MB; in 64 x 64 tiles without the split 13).
 constexpr int FEW_WAVES = 8;
 template <typename T, int RT>
 __global__ __launch_bounds__(64 * FEW_WAVES) void product_few_kernel(ProductQ8Params p) {
@@ -492,9 +501,11 @@ void product_mm_kernel(ProductQ8Params p, int64_t tiles, int64_t per_xcd) {
   if (bad || most >= too_large<T>()) raise_flag(p.flag);
 }
 
+constexpr int64_t ROWS_OUT = 4 * 16 * 128;                 // bytes of LDS for four waves' results
+
 template <typename T, int NT, int GK>
 hipError_t rows_ntgk(const ProductQ8Params& p, int groups, int64_t wgs, hipStream_t s) {
-  const size_t lds = (size_t)groups * GK * NT * 1024 + 16 * NT * (12 + 64 * sizeof(T));
+  const size_t lds = (size_t)groups * GK * NT * 1024 + 16 * NT * 12 + ROWS_OUT;
   auto k = product_rows_kernel<T, NT, GK>;
   if (lds > 64 * 1024) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -513,8 +524,7 @@ hipError_t rows_nt(const ProductQ8Params& p, int64_t wgs, hipStream_t s) {
 }
 
 // 80 KB of LDS a workgroup at most, so that two share a compute unit.
-template <typename T>
-bool rows_fit(int64_t bn, int64_t kb) { return bn * (kb + 12 + 64 * (int64_t)sizeof(T)) <= 80 * 1024; }
+bool rows_fit(int64_t bn, int64_t kb) { return bn * (kb + 12) + ROWS_OUT <= 80 * 1024; }
 
 template <typename T, int TM, int TN>
 hipError_t mm_t(const ProductQ8Params& p, hipStream_t s) {
@@ -529,14 +539,16 @@ hipError_t mm_t(const ProductQ8Params& p, hipStream_t s) {
 //    at half the pace each), each `step` for 64 bytes of k and `ends` for its
 //    start and its results;
 //  * rows: every column block reads all codes, from HBM or the caches alike at
-//    4.5 TB/s with the results' writes, and fills LDS with its weights first;
+//    4.6 TB/s with the results' writes, and fills LDS with its weights first;
 //  * few: one round per 256 workgroups of 32 rows.
-// Measured (us; few, rows, mm 256 x 256, 256 x 128, 128 x 128, 128 x 64; fp16
-// results, ReLU codes, 2048 columns of H): 256 rows, 2048 columns of weights 11,
-// 16, 31, 20, 14, 11; 2048 rows 70, 70, 31, 21, 16, 20; 8192 rows 279, 174, 41,
-// 58, 58, 80; 32768 rows 1094, 658, 159, 231, 221, 311; 2^18 rows, 128 columns of
-// weights 595, 474, 160, 145, 155, 187, 64 columns 316, 245, 144, 129, 134, 127;
-// 32768 rows, 16 columns 21, 18, 37, 29, 20, 18.
+// Measured (us, with the call; few, rows, mm 256 x 256, 256 x 128, 128 x 128, 128
+// x 64; fp16 results, ReLU codes, 2048 columns of H): 256 rows, 2048 columns of
+// weights 11, 16, 31, 20, 14, 11; 2048 rows 70, 70, 31, 21, 16, 20; 8192 rows 279,
+// 174, 42, 58, 58, 80; 32768 rows 1094, 658, 160, 231, 221, 311; 2^18 rows, 64
+// columns of weights 316, 234, 139, 128, 132, 127; 32 columns -, 120, 129, 115,
+// 116, 111; 32768 rows, 16 columns 21, 17, 37, 29, 20, 18.  512 columns of H, 2^18
+// rows, 256 columns of weights -, 84, 89, 110, 112, 137; 128 columns -, 44, 81, 66,
+// 64, 77.
 struct MmTile { int rows, cols; double step, ends; };
 constexpr MmTile MM_TILES[] = {{256, 256, 0.75, 14.0}, {256, 128, 0.55, 11.0}, {128, 128, 0.30, 4.0}, {128, 64, 0.22, 2.0}};
 
@@ -547,13 +559,13 @@ hipError_t product_t(const ProductQ8Params& p, hipStream_t s) {
   auto cut = [](int64_t x, int64_t by) { return (x + by - 1) / by; };
   // rows: the widest block that fits LDS, narrower where few rows leave compute units idle
   int64_t bn = WIDTH;
-  while (bn < 128 && bn < p.N && rows_fit<T>(2 * bn, kb)) bn *= 2;
+  while (bn < 128 && bn < p.N && rows_fit(2 * bn, kb)) bn *= 2;
   while (bn > WIDTH && cut(p.n, 64) * cut(p.N, bn) < 256) bn /= 2;
   const int64_t blocks = cut(p.N, bn);
   enum { ROWS = 4, FEW = 5 };
   int kind = p.n <= 64 ? FEW : ROWS;
   if (kind == ROWS && p.K >= 64 * MM_MIN_STEPS) {
-    double best = rows_fit<T>(bn, kb) ? (double)p.n * (double)(p.K * blocks + p.N * (int64_t)sizeof(T)) / 4.5e6 + (double)(bn * kb) / 1.6e4
+    double best = rows_fit(bn, kb) ? (double)p.n * (double)(p.K * blocks + p.N * (int64_t)sizeof(T)) / 4.6e6 + (double)(bn * kb) / 1.6e4
                                    : 1e30;
     auto offer = [&](int k, double us) { if (us < best) { best = us; kind = k; } };
     offer(FEW, (double)cut(cut(p.N, WIDTH) * cut(p.n, 32), 256) * (0.11 * steps + 1.5));
