@@ -28,6 +28,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 namespace gcn {
 
@@ -50,15 +51,21 @@ __device__ __forceinline__ int swz(int v) {
 template <int C>
 __device__ __forceinline__ int piece_at(int v, int c) { return (v * C + (c ^ swz<C>(v))) * 16; }
 
-// 1 KiB from memory into LDS: lane l's 16 bytes at its own address go to lds +
-// 16 l.  Counted by vmcnt; no register is written.  As asm, because the compiler
+// 1 KiB from memory into LDS: lane l's 16 bytes at base + off go to lds + 16 l.
+// Counted by vmcnt; no register is written.  As asm, because the compiler
 // otherwise waits for it before any LDS read.
-__device__ __forceinline__ void to_lds_1k(const void* src, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(lds) : "memory", "m0");
+__device__ __forceinline__ void to_lds_1k(const void* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory", "m0");
+}
+// An address that all lanes share, for the scalar registers.
+__device__ __forceinline__ const void* uniform(const void* p) {
+  const uint64_t a = reinterpret_cast<uint64_t>(p);
+  return reinterpret_cast<const void*>((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(a >> 32)) << 32 |
+                                       (uint32_t)__builtin_amdgcn_readfirstlane((int)a));
 }
 // The same for 4 bytes a lane.
-__device__ __forceinline__ void to_lds_256(const void* src, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(src), "s"(lds) : "memory", "m0");
+__device__ __forceinline__ void to_lds_256(const void* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory", "m0");
 }
 typedef __attribute__((address_space(3))) uint8_t lds_byte;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -115,7 +122,6 @@ __global__ __launch_bounds__(64 * WM) __attribute__((amdgpu_waves_per_eu(2))) vo
   constexpr bool FOLD = sizeof(T) == 4;
   constexpr int KS = (GC + 3) / 4;                         // steps of 64 bytes along f_out
   constexpr int NT = NB / 16;
-  constexpr int HALVES = sizeof(T) == 4 && NB >= 128 ? 1 : 2;   // of a tile at once for dW, registers allowing
   constexpr int STORES = TV / 16 * (XE * sizeof(T) > 16 ? 2 : 1);   // stores of dZ a wave issues for a tile
   __shared__ __align__(1024) uint8_t lds[2 * STAGE];
   __shared__ __align__(16) float scales[2][TV];
@@ -126,24 +132,49 @@ __global__ __launch_bounds__(64 * WM) __attribute__((amdgpu_waves_per_eu(2))) vo
   const uint32_t scales0 = (uint32_t)(uintptr_t)(lds_byte*)scales;
   const int64_t step = gridDim.x;
 
-  // this wave's 1 KiB pieces of tile t into a stage, by wave 0 its scales; rows
-  // past the last one are copies of it, pieces past the widths of the first
-  auto issue = [&](int64_t t, int st) {
-#pragma unroll 1
-    for (int pc = wave; pc < STAGE / 1024; pc += WM) {
-      const void* src;
-      if (pc < CB / 1024) {
-        const int at = pc * 64 + lane, row = at / CC;
-        const int64_t r = min(t * TV + row, p.n - 1), c = m0 + (((at % CC) ^ swz<CC>(row)) * 16);
-        src = p.Hq + r * p.ld_q + (c < p.M ? c : 0);
-      } else {
-        const int at = (pc - CB / 1024) * 64 + lane, row = at / GC;
-        const int64_t r = min(t * TV + row, p.n - 1), c = ((at % GC) ^ swz<GC>(row)) * VE;
-        src = static_cast<const T*>(p.G) + r * p.ldg + (c < p.N ? c : 0);
-      }
-      to_lds_1k(src, lds0 + st * STAGE + pc * 1024);
+  // A wave's 1 KiB pieces of a tile, by wave 0 its scales: where a lane's 16 bytes
+  // of piece pc lie from the tile's first row on.  Rows past `last` are copies of
+  // it, pieces past the widths of the first.  The places stay the same from tile
+  // to tile and are kept where registers allow (2^21 rows, 128 <- 64 fp16 220 ->
+  // 208 us).
+  constexpr int PIECES = STAGE / 1024, PPW = (PIECES + WM - 1) / WM;
+  constexpr bool KEEP = PPW <= 6 && NB <= 128;
+  auto place = [&](int pc, int last) -> uint32_t {
+    if (pc < CB / 1024) {
+      const int at = pc * 64 + lane, row = at / CC;
+      const int64_t c = m0 + (((at % CC) ^ swz<CC>(row)) * 16);
+      return (uint32_t)min(row, last) * (uint32_t)p.ld_q + (uint32_t)(c < p.M ? c : 0);
     }
-    if (wave == 0) to_lds_256(p.scale + min(t * TV + lane, p.n - 1), scales0 + st * (TV * 4));
+    const int at = (pc - CB / 1024) * 64 + lane, row = at / GC, c = ((at % GC) ^ swz<GC>(row)) * VE;
+    return ((uint32_t)min(row, last) * (uint32_t)p.ldg + (uint32_t)(c < p.N ? c : 0)) * (uint32_t)sizeof(T);
+  };
+  uint32_t off[KEEP ? PPW : 1];
+  auto place_all = [&](int last) {
+    if constexpr (KEEP) {
+#pragma unroll
+      for (int j = 0; j < PPW; ++j) off[j] = place(j * WM + wave, last);
+    }
+  };
+  auto issue = [&](int64_t t, int st) {
+    const int64_t r0 = t * TV;
+    const int last = (int)min(p.n - 1 - r0, (int64_t)TV - 1);
+    const uint8_t* codes = p.Hq + r0 * p.ld_q;
+    const T* grad = static_cast<const T*>(p.G) + r0 * p.ldg;
+    auto one = [&](int pc, uint32_t at) {
+      to_lds_1k(uniform(pc < CB / 1024 ? (const void*)codes : (const void*)grad), at,
+                __builtin_amdgcn_readfirstlane(lds0 + st * STAGE + pc * 1024));
+    };
+    if constexpr (KEEP) {
+      if (last < TV - 1) place_all(last);                  // the last tile, the last of its workgroup
+#pragma unroll
+      for (int j = 0; j < PPW; ++j)
+        if (PIECES % WM == 0 || j * WM + wave < PIECES) one(j * WM + wave, off[j]);
+    } else {
+#pragma unroll 1
+      for (int pc = wave; pc < PIECES; pc += WM) one(pc, place(pc, last));
+    }
+    if (wave == 0)
+      to_lds_256(uniform(p.scale + r0), (uint32_t)min(lane, last) * 4, __builtin_amdgcn_readfirstlane(scales0 + st * (TV * 4)));
   };
 
   // rows of W: operand i's row m is column f0 + XE (m / 4) + 4 i + m % 4 of H
@@ -187,16 +218,21 @@ __global__ __launch_bounds__(64 * WM) __attribute__((amdgpu_waves_per_eu(2))) vo
     const int64_t left = p.M - c - 4 * i;
     cols[i] = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
   }
+  const uint32_t dz_off = (uint32_t)l16 * (uint32_t)p.ldz + (uint32_t)c;
   const uint32_t every = p.relu ? 0u : ~0u;                // no mask: every code counts
   float sum[XE] = {}, most = 0.f;                          // sums, and the largest size of any element
 
   // stores of this wave behind the loads waited for: all STORES of the tile
   // before where every column of the wave is stored
   const bool counted = p.dZ && f0 + FW <= p.M;
+  const bool mine = c < p.M;                               // some of this lane's columns are
   int64_t t = blockIdx.x;
+  place_all(TV - 1);
   issue(t, 0);                                             // the launch has no more workgroups than tiles
   bool first = true;
-  for (int st = 0; t < tiles; t += step, st ^= 1) {
+  auto tile = [&](auto stage) {
+    const int st = stage;
+    constexpr int HALVES = sizeof(T) == 4 && NB >= 128 ? 1 : 2;   // of a tile at once for dW, registers allowing
     if (counted && !first) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(STORES) : "memory");
     else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
@@ -204,8 +240,9 @@ __global__ __launch_bounds__(64 * WM) __attribute__((amdgpu_waves_per_eu(2))) vo
     __builtin_amdgcn_sched_barrier(0);
     first = false;
     if (t + step < tiles) issue(t + step, st ^ 1);
-    if (t * TV + TV > p.n) {                               // rows past the last one: of scale 0
-      if (tid < TV && t * TV + tid >= p.n) scales[st][tid] = 0.f;
+    const int rows = (int)min(p.n - t * TV, (int64_t)TV);
+    if (rows < TV) {                                       // rows past the last one: of scale 0
+      if (tid < TV && tid >= rows) scales[st][tid] = 0.f;
       __syncthreads();
     }
     const uint8_t* cod = lds + st * STAGE;
@@ -247,7 +284,6 @@ __global__ __launch_bounds__(64 * WM) __attribute__((amdgpu_waves_per_eu(2))) vo
             for (int i = 0; i < FI; ++i) z[i] = NtMfma<T>::run(w[i][ks], b, z[i]);
           }
         }
-        const int64_t r = t * TV + v;
         float x[XE];
 #pragma unroll
         for (int i = 0; i < FI; ++i) {
@@ -259,13 +295,13 @@ __global__ __launch_bounds__(64 * WM) __attribute__((amdgpu_waves_per_eu(2))) vo
             x[4 * i + e] = __uint_as_float(__float_as_uint(y) & (uint32_t)((int32_t)(k << (24 - 8 * e)) >> 31));
           }
         }
-        if (r < p.n && c < p.M) {
+        if (v < rows && mine) {
 #pragma unroll
           for (int e = 0; e < XE; ++e) {
             sum[e] += x[e];
             most = fmaxf(most, fabsf(x[e]));
           }
-          store_cols<T, XE>(static_cast<T*>(p.dZ) + r * p.ldz + c, x);
+          store_cols<T, XE>(static_cast<T*>(p.dZ) + (t * TV + vt * 16) * p.ldz + dz_off, x);
         }
       }
     }
@@ -314,6 +350,17 @@ __global__ __launch_bounds__(64 * WM) __attribute__((amdgpu_waves_per_eu(2))) vo
         turned_mfma<T, FI, NT>(a, b, acc, j);
       }
     }
+    t += step;
+  };
+  if constexpr (NB <= 128) {                               // the stages in turn, each with its own code
+    while (true) {
+      tile(std::integral_constant<int, 0>());
+      if (t >= tiles) break;
+      tile(std::integral_constant<int, 1>());
+      if (t >= tiles) break;
+    }
+  } else {                                                 // registers: twice the code spills
+    for (int st = 0; t < tiles; st ^= 1) tile(st);
   }
   // an element that T cannot hold, or a NaN, which ends in its column's sum
   bool bad = most >= overflow_at<T>();
@@ -510,14 +557,17 @@ hipError_t dz_t(const BwdQ8Params& p, float* colsum, hipStream_t s) {
 }  // namespace
 
 int64_t bwd_q8_floats(int prec, int64_t n, int64_t M, int64_t N) {
-  if (N <= fused_max_n(prec)) return fused_splits(n, M, N) * partial_stride(M, N);
-  return pad64((int64_t)wgrad_splits(prec, n, M, N) * M * N) + pad64(dz_blocks(n, M) * M);
+  const int64_t general = pad64((int64_t)wgrad_splits(prec, n, M, N) * M * N) + pad64(dz_blocks(n, M) * M);
+  return N <= fused_max_n(prec) ? std::max(general, fused_splits(n, M, N) * partial_stride(M, N)) : general;
 }
 
 hipError_t bwd_q8_launch(int prec, const BwdQ8Params& p, const Epilogue& dw, const Epilogue* db, float* ws,
                          hipStream_t s) {
   hipError_t e = hipErrorInvalidValue;
-  if (p.N <= fused_max_n(prec)) {
+  // a tile's addresses are 32-bit offsets from its first row
+  const int64_t es = prec == 0 ? 4 : 2;
+  const bool near = TV * std::max({p.ld_q, p.ldg * es, p.dZ ? p.ldz * es : 0}) < (int64_t)1 << 31;
+  if (p.N <= fused_max_n(prec) && near) {
     switch (prec) {
       case 0: e = fused_t<float>(p, ws, db != nullptr, s); break;
       case 1: e = fused_t<f16>(p, ws, db != nullptr, s); break;

@@ -98,3 +98,34 @@ def test_rows_behind_the_last_stay(prec):
 
 def round_up(x):
     return (x + 7) // 8 * 8
+
+
+@pytest.mark.parametrize("prec", [G.GCN_F32, G.GCN_F16])
+def test_rows_far_apart(prec):
+    """Codes whose rows lie 2^25 bytes apart (a tile of 64 rows spans 2^31): the same bits as with rows side by side
+    where every sum is exact."""
+    n, f, N = 70, 40, 24
+    dt = G.torch_dtype(prec)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    q = torch.randint(0, 256, (n, 48), generator=gen, device="cuda", dtype=torch.uint8)
+    q[torch.rand((n, 48), generator=gen, device="cuda") < 0.4] = 0
+    far = torch.zeros((n, 1 << 25), dtype=torch.uint8, device="cuda")
+    far[:, :48] = q
+    s = torch.full((n,), 0.25, device="cuda")
+    g = torch.randint(-2, 3, (n, N), generator=gen, device="cuda").to(dt)
+    W = torch.randint(-1, 2, (f, N), generator=gen, device="cuda").to(dt)
+    ws = torch.empty(G.gcn_transform_bwd_q8_workspace_size(n, f, N, prec), dtype=torch.uint8, device="cuda")
+    ov, out = flag(), []
+    for codes in (q, far):
+        dW, db = torch.zeros((f, N), device="cuda"), torch.zeros(f, device="cuda")
+        dZ = torch.zeros((n, f), dtype=dt, device="cuda")
+        G.gcn_transform_bwd_q8(n, f, N, prec, G.GCN_Q8_RELU, codes, codes.shape[1], s, W, N, g, N, G.GCN_ACT_RELU, 0.5, dW,
+                               dZ, f, db, ov, ws)
+        out.append((dW, db, dZ))
+    assert all(torch.equal(a, b) for a, b in zip(*out)) and ov.item() == 0 and out[0][0].any()
+    w8 = torch.randint(-127, 128, (N, 48), generator=gen, device="cuda", dtype=torch.int8)
+    S = [torch.zeros((n, N), dtype=dt, device="cuda") for _ in range(2)]
+    for t, codes in zip(S, (q, far)):
+        G.gcn_transform_q8(n, f, N, G.GCN_Q8_RELU, codes, codes.shape[1], s, w8, 48, torch.full((N,), 2.0 ** -12, device="cuda"),
+                           w8[:, :f].sum(1, dtype=torch.int32), prec, t, N, ov)
+    assert torch.equal(*S) and S[0].any()
