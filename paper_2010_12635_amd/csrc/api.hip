@@ -858,7 +858,7 @@ gcn_status check_bwd_q8(int64_t n, int64_t f_in, int64_t f_out, int32_t prec, in
   if (st == GCN_OK) st = check_ld(f_out, ld_gs);
   if (st == GCN_OK && dZ_below) st = check_ld(f_in, ld_dz);
   if (st != GCN_OK) return st;
-  if (f_in * ld_w > MAX_DW) return GCN_ERR_UNSUPPORTED;
+  if (ld_w > MAX_DW / f_in) return GCN_ERR_UNSUPPORTED;
   if (!Hq || !h_scale || !W || !GS || !dW || (dbias_below && !dZ_below)) return GCN_ERR_INVALID_ARG;
   if (act_below != GCN_ACT_NONE && act_below != GCN_ACT_RELU) return GCN_ERR_INVALID_ARG;
   if (!(p_below >= 0.f && p_below < 1.f)) return GCN_ERR_INVALID_ARG;
@@ -996,7 +996,7 @@ gcn_status gcn_layer_bwd_q8_workspace_size(const gcn_adj* A, const gcn_layer* L,
   if (st == GCN_OK) st = check_layer(L);
   if (st == GCN_OK && L->identity_input) st = GCN_ERR_INVALID_ARG;
   if (st == GCN_OK) st = check_codes(A->n, L->f_in, GCN_Q8_RELU, (L->f_in + 15) / 16 * 16);
-  if (st == GCN_OK && (L->f_out > GCN_Q8_MAX_WIDTH || L->f_in * L->ld_out > MAX_DW)) st = GCN_ERR_UNSUPPORTED;
+  if (st == GCN_OK && (L->f_out > GCN_Q8_MAX_WIDTH || L->ld_out > MAX_DW / L->f_in)) st = GCN_ERR_UNSUPPORTED;
   if (st != GCN_OK) return st;
   *bytes = plan_bytes(plan_layer_q8(A, L, prec));
   return GCN_OK;

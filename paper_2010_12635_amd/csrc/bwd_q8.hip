@@ -118,8 +118,6 @@ __global__ __launch_bounds__(64 * WM) __attribute__((amdgpu_waves_per_eu(2))) vo
   constexpr int XE = 4 * FI;                               // columns of a row of dZ a lane ends with
   constexpr int CC = FB / 16, GC = NB * (int)sizeof(T) / 16;   // 16-byte pieces of a row of codes, of G
   constexpr int CB = TV * FB, GB = TV * GC * 16, STAGE = CB + GB;
-  // fp32: the factor 1 / (1 - p) goes into W, one rounding as it would be in dZ
-  constexpr bool FOLD = sizeof(T) == 4;
   constexpr int KS = (GC + 3) / 4;                         // steps of 64 bytes along f_out
   constexpr int NT = NB / 16;
   constexpr int STORES = TV / 16 * (XE * sizeof(T) > 16 ? 2 : 1);   // stores of dZ a wave issues for a tile
@@ -190,18 +188,10 @@ __global__ __launch_bounds__(64 * WM) __attribute__((amdgpu_waves_per_eu(2))) vo
       const int64_t f = min(f0 + XE * (l16 >> 2) + 4 * i + (l16 & 3), p.M - 1);
       w[i][ks] = make_uint4(0, 0, 0, 0);
       if (p.dZ && live[ks]) w[i][ks] = keep_first<T>(ldg16(static_cast<const T*>(p.W) + f * p.ldw + (ks * 4 + lg) * VE), live[ks]);
-      if constexpr (FOLD) {
-        float y[4];
-        unpack<float>(w[i][ks], y);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] *= p.keep;
-        w[i][ks] = pack<float>(y);
-      }
     }
   }
   const bool ragged = p.N < NB;
-  const uint32_t flip = p.kind == Q8_SIGNED ? 0x80808080u : 0u;
-  const float zero = p.kind == Q8_SIGNED ? -128.f : 0.f;
+  const bool with_sign = p.kind == Q8_SIGNED;
 
   f32x4 acc[FI][NT];
 #pragma unroll
@@ -291,7 +281,7 @@ __global__ __launch_bounds__(64 * WM) __attribute__((amdgpu_waves_per_eu(2))) vo
           k |= (k & 0x7f7f7f7fu) + 0x7f7f7f7fu;            // the top bit of every byte that is not 0
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float y = FOLD ? z[i][e] : z[i][e] * p.keep;
+            const float y = z[i][e] * p.keep;
             x[4 * i + e] = __uint_as_float(__float_as_uint(y) & (uint32_t)((int32_t)(k << (24 - 8 * e)) >> 31));
           }
         }
@@ -319,10 +309,12 @@ __global__ __launch_bounds__(64 * WM) __attribute__((amdgpu_waves_per_eu(2))) vo
         const i32x2 q = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
             (__attribute__((address_space(3))) i32x2*)(cod + piece_at<CC>(v, wave * FI + i) + 8 * (l16 & 1)));
         float x[8];
+        if (with_sign) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint32_t b = (((uint32_t)q[e >> 2] ^ flip) >> (8 * (e & 3))) & 0xffu;
-          x[e] = fmaf((float)b, sc[e], zero * sc[e]);      // exact: (b - 128) * scale has 24 bits
+          for (int e = 0; e < 8; ++e) x[e] = (float)((int32_t)((uint32_t)q[e >> 2] << (24 - 8 * (e & 3))) >> 24) * sc[e];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = (float)(((uint32_t)q[e >> 2] >> (8 * (e & 3))) & 0xffu) * sc[e];
         }
         if constexpr (sizeof(T) == 4) {
 #pragma unroll

@@ -336,6 +336,31 @@ def test_backward_overflow(n, M, N):
             assert ov.item() == 1, what
 
 
+@pytest.mark.parametrize("n,M,N", [(1, 40, 7), (1, 130, 64), (1, 33, 300)])
+@pytest.mark.parametrize("prec", [G.GCN_F32, G.GCN_BF16])
+def test_backward_largest_numbers(prec, n, M, N):
+    """A row up to the type's largest number and weights near it, where the results are far inside the range: one
+    product each by a power of two, so they are exact."""
+    dt = G.torch_dtype(prec)
+    rng = np.random.default_rng(M)
+    h = padded(rng.choice([-1.0, 1.0, 0.5], (n, M)) * torch.finfo(dt).max, dt, round8(M))
+    q, s, ov = quantize(h, M, prec, "signed", round16(M))
+    back = torch.zeros_like(h)
+    G.gcn_dequantize(n, M, G.GCN_Q8_SIGNED, q, q.shape[1], s, prec, back, back.shape[1], ov)
+    g = np.zeros((n, N))
+    g[:, N - 1] = 2.0 ** -40
+    w = rng.integers(-3, 4, (M, N)) * 2.0 ** 126
+    dW, dZ, db, ov2 = backward(q, s, padded(w, dt, round8(N)), padded(g, dt, round8(N)), prec, "signed", n, M, N,
+                               G.GCN_ACT_NONE, 0.0)
+    assert np.array_equal(f64(dW, N), f64(back, M).T @ g)
+    assert np.array_equal(f64(dZ, M), g @ w.T)
+    ones = torch.ones_like(q)
+    dW, dZ, db, ov3 = backward(ones, torch.ones(n, device="cuda"), padded(w, dt, round8(N)), padded(g, dt, round8(N)), prec,
+                               "relu", n, M, N, G.GCN_ACT_RELU, 0.75)
+    assert np.array_equal(f64(dZ, M), g @ w.T * 4)
+    assert ov.item() == 0 and ov2.item() == 0 and ov3.item() == 0
+
+
 # ------------------------------------------------------------- the layer's ----
 
 @pytest.mark.parametrize("prec", PRECS)
