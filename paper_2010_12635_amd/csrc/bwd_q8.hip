@@ -18,8 +18,9 @@
 //    multiplies them.
 //  * 16-byte pieces of a row in LDS change places with its row number, so that
 //    no read of 16 rows at the same column meets a bank twice.
-// Wider G goes the general way: the weight gradient's kernel with codes turned
-// into numbers as they come in (wgrad.hip), and a tiled product for dZ.
+// Wider G takes two: a product for dZ, and for dW the same kernel with 256
+// columns of G a workgroup (16 bits) or the weight gradient's kernel with codes
+// turned into numbers as they come in (wgrad.hip).
 #include "internal.h"
 #include "lanes.h"
 #include "nt_tile.h"
@@ -126,6 +127,10 @@ __global__ __launch_bounds__(64 * WM) __attribute__((amdgpu_waves_per_eu(2))) vo
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t m0 = (int64_t)blockIdx.y * FB;
+  // columns of G this workgroup takes: all of them where there is dZ
+  const int64_t n0 = (int64_t)blockIdx.z * NB;
+  const int N = (int)min(p.N - n0, (int64_t)NB);
+  const T* const G = static_cast<const T*>(p.G) + n0;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_byte*)lds;
   const uint32_t scales0 = (uint32_t)(uintptr_t)(lds_byte*)scales;
   const int64_t step = gridDim.x;
@@ -144,7 +149,7 @@ __global__ __launch_bounds__(64 * WM) __attribute__((amdgpu_waves_per_eu(2))) vo
       return (uint32_t)min(row, last) * (uint32_t)p.ld_q + (uint32_t)(c < p.M ? c : 0);
     }
     const int at = (pc - CB / 1024) * 64 + lane, row = at / GC, c = ((at % GC) ^ swz<GC>(row)) * VE;
-    return ((uint32_t)min(row, last) * (uint32_t)p.ldg + (uint32_t)(c < p.N ? c : 0)) * (uint32_t)sizeof(T);
+    return ((uint32_t)min(row, last) * (uint32_t)p.ldg + (uint32_t)(c < N ? c : 0)) * (uint32_t)sizeof(T);
   };
   uint32_t off[KEEP ? PPW : 1];
   auto place_all = [&](int last) {
@@ -157,7 +162,7 @@ __global__ __launch_bounds__(64 * WM) __attribute__((amdgpu_waves_per_eu(2))) vo
     const int64_t r0 = t * TV;
     const int last = (int)min(p.n - 1 - r0, (int64_t)TV - 1);
     const uint8_t* codes = p.Hq + r0 * p.ld_q;
-    const T* grad = static_cast<const T*>(p.G) + r0 * p.ldg;
+    const T* grad = G + r0 * p.ldg;
     auto one = [&](int pc, uint32_t at) {
       to_lds_1k(uniform(pc < CB / 1024 ? (const void*)codes : (const void*)grad), at,
                 __builtin_amdgcn_readfirstlane(lds0 + st * STAGE + pc * 1024));
@@ -181,8 +186,8 @@ __global__ __launch_bounds__(64 * WM) __attribute__((amdgpu_waves_per_eu(2))) vo
   int live[KS];                                            // columns of G in this lane's pieces
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) {
-    const int64_t left = p.N - (ks * 4 + lg) * VE;
-    live[ks] = left <= 0 ? 0 : left >= VE ? VE : (int)left;
+    const int left = N - (ks * 4 + lg) * VE;
+    live[ks] = left <= 0 ? 0 : left >= VE ? VE : left;
 #pragma unroll
     for (int i = 0; i < FI; ++i) {
       const int64_t f = min(f0 + XE * (l16 >> 2) + 4 * i + (l16 & 3), p.M - 1);
@@ -190,7 +195,7 @@ __global__ __launch_bounds__(64 * WM) __attribute__((amdgpu_waves_per_eu(2))) vo
       if (p.dZ && live[ks]) w[i][ks] = keep_first<T>(ldg16(static_cast<const T*>(p.W) + f * p.ldw + (ks * 4 + lg) * VE), live[ks]);
     }
   }
-  const bool ragged = p.N < NB;
+  const bool ragged = N < NB;
   const bool with_sign = p.kind == Q8_SIGNED;
 
   f32x4 acc[FI][NT];
@@ -368,8 +373,9 @@ __global__ __launch_bounds__(64 * WM) __attribute__((amdgpu_waves_per_eu(2))) vo
     for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int v = 0; v < 4; ++v) {
-        const int64_t m = f0 + i * 16 + lg * 4 + v, n = j * 16 + l16;
-        if (m < p.M && n < p.N) out[m * p.N + n] = acc[i][j][v];
+        const int64_t m = f0 + i * 16 + lg * 4 + v;
+        const int n = j * 16 + l16;
+        if (m < p.M && n < N) out[m * p.N + n0 + n] = acc[i][j][v];
       }
   if (!sums) return;
 #pragma unroll
@@ -449,20 +455,21 @@ int64_t fused_columns(int64_t M) { return M <= 32 ? 32 : M <= 64 ? 64 : 128; }
 // (M N)).  Measured (us; 256, 512, 768, 1024 workgroups in all): 2^21 rows, 128 <-
 // 64 fp16 277, 220, 224, 229; 32768 rows, 2048 <- 16 fp16 66, 54, 54, 59; 16384
 // rows, 500 <- 64 bf16 13.4 with 64 along the rows, 20 with 192.
-int64_t fused_splits(int64_t n, int64_t M, int64_t N) {
-  const int64_t fb = fused_columns(M), blocks = (M + fb - 1) / fb, tiles = (n + TV - 1) / TV;
-  const int64_t held = 512 * (128 / fb) / blocks;
+int64_t fused_splits(int prec, int64_t n, int64_t M, int64_t N) {
+  const int64_t fb = fused_columns(M), nb = fused_max_n(prec), tiles = (n + TV - 1) / TV;
+  const int64_t blocks = (M + fb - 1) / fb * ((N + nb - 1) / nb), held = 512 * (128 / fb) / blocks;
   const int64_t cheap = (int64_t)std::sqrt(5e5 * (double)tiles / ((double)M * (double)N));
   return std::min({tiles, std::max<int64_t>(1, held), std::max<int64_t>(1, cheap)});
 }
 
 template <typename T, int NB>
-hipError_t fused_nb(const BwdQ8Params& p, float* partials, int sums, hipStream_t s) {
+hipError_t fused_nb(int prec, const BwdQ8Params& p, float* partials, int64_t stride, int sums, hipStream_t s) {
   // 16 columns of H a wave where 32 would leave registers for one wave a SIMD only
   constexpr int FI = NB >= 128 ? 1 : 2, W1 = 2 / FI;
-  const int64_t stride = partial_stride(p.M, p.N), tiles = (p.n + TV - 1) / TV;
+  const int64_t tiles = (p.n + TV - 1) / TV;
   const int fb = (int)fused_columns(p.M);
-  const dim3 grid((unsigned)fused_splits(p.n, p.M, p.N), (unsigned)((p.M + fb - 1) / fb));
+  const dim3 grid((unsigned)fused_splits(prec, p.n, p.M, p.N), (unsigned)((p.M + fb - 1) / fb),
+                  (unsigned)((p.N + NB - 1) / NB));
   const dim3 block(64 * W1 * fb / 32);
   switch (fb) {
     case 32: hipLaunchKernelGGL((bwd_q8_kernel<T, NB, W1, FI>), grid, block, 0, s, p, tiles, partials, stride, sums); break;
@@ -473,13 +480,22 @@ hipError_t fused_nb(const BwdQ8Params& p, float* partials, int sums, hipStream_t
 }
 
 template <typename T>
-hipError_t fused_t(const BwdQ8Params& p, float* partials, int sums, hipStream_t s) {
-  if (p.N <= 16) return fused_nb<T, 16>(p, partials, sums, s);
-  if (p.N <= 32) return fused_nb<T, 32>(p, partials, sums, s);
-  if (p.N <= 64) return fused_nb<T, 64>(p, partials, sums, s);
+hipError_t fused_t(int prec, const BwdQ8Params& p, float* partials, int64_t stride, int sums, hipStream_t s) {
+  if (p.N <= 16) return fused_nb<T, 16>(prec, p, partials, stride, sums, s);
+  if (p.N <= 32) return fused_nb<T, 32>(prec, p, partials, stride, sums, s);
+  if (p.N <= 64) return fused_nb<T, 64>(prec, p, partials, stride, sums, s);
   if constexpr (sizeof(T) == 2)
-    if (p.N > 128) return fused_nb<T, 256>(p, partials, sums, s);
-  return fused_nb<T, 128>(p, partials, sums, s);
+    if (p.N > 128) return fused_nb<T, 256>(prec, p, partials, stride, sums, s);
+  return fused_nb<T, 128>(prec, p, partials, stride, sums, s);
+}
+
+hipError_t fused(int prec, const BwdQ8Params& p, float* partials, int64_t stride, int sums, hipStream_t s) {
+  switch (prec) {
+    case 0: return fused_t<float>(prec, p, partials, stride, sums, s);
+    case 1: return fused_t<f16>(prec, p, partials, stride, sums, s);
+    case 2: return fused_t<bf16>(prec, p, partials, stride, sums, s);
+  }
+  return hipErrorInvalidValue;
 }
 
 // dZ of 64 rows x 64 columns at a time; a workgroup walks the row blocks
@@ -549,29 +565,36 @@ hipError_t dz_t(const BwdQ8Params& p, float* colsum, hipStream_t s) {
 }  // namespace
 
 int64_t bwd_q8_floats(int prec, int64_t n, int64_t M, int64_t N) {
-  const int64_t general = pad64((int64_t)wgrad_splits(prec, n, M, N) * M * N) + pad64(dz_blocks(n, M) * M);
-  return N <= fused_max_n(prec) ? std::max(general, fused_splits(n, M, N) * partial_stride(M, N)) : general;
+  const int64_t splits = std::max<int64_t>(wgrad_splits(prec, n, M, N), fused_splits(prec, n, M, N));   // either, by the strides
+  const int64_t general = pad64(splits * M * N) + pad64(dz_blocks(n, M) * M);
+  return N <= fused_max_n(prec) ? std::max(general, fused_splits(prec, n, M, N) * partial_stride(M, N)) : general;
 }
 
 hipError_t bwd_q8_launch(int prec, const BwdQ8Params& p, const Epilogue& dw, const Epilogue* db, float* ws,
                          hipStream_t s) {
-  hipError_t e = hipErrorInvalidValue;
+  hipError_t e;
   // a tile's addresses are 32-bit offsets from its first row
   const int64_t es = prec == 0 ? 4 : 2;
   const bool near = TV * std::max({p.ld_q, p.ldg * es, p.dZ ? p.ldz * es : 0}) < (int64_t)1 << 31;
   if (p.N <= fused_max_n(prec) && near) {
-    switch (prec) {
-      case 0: e = fused_t<float>(p, ws, db != nullptr, s); break;
-      case 1: e = fused_t<f16>(p, ws, db != nullptr, s); break;
-      case 2: e = fused_t<bf16>(p, ws, db != nullptr, s); break;
-    }
-    return e != hipSuccess ? e : sum_partials(ws, fused_splits(p.n, p.M, p.N), p, dw, db, s);
+    e = fused(prec, p, ws, partial_stride(p.M, p.N), db != nullptr, s);
+    return e != hipSuccess ? e : sum_partials(ws, fused_splits(prec, p.n, p.M, p.N), p, dw, db, s);
   }
-  const int splits = wgrad_splits(prec, p.n, p.M, p.N);
+  // dW alone (us; one kernel, wgrad): 131072 rows, 300 <- 512 fp16 124, 188; 32768
+  // rows, 1000 <- 300 bf16 88, 107; fp32, at 128 columns a workgroup: 131072 rows,
+  // 256 <- 200 200, 170; 1528 rows, 589 <- 181 28, 21.
+  const bool one = near && prec != 0;
+  const int splits = one ? (int)fused_splits(prec, p.n, p.M, p.N) : wgrad_splits(prec, p.n, p.M, p.N);
   float* cs = ws + pad64((int64_t)splits * p.M * p.N);
-  float* colsum = db ? cs : nullptr;
-  e = wgrad_q8_launch(prec, p.Hq, p.ld_q, p.scale, p.kind, p.G, p.ldg, p.n, p.M, p.N, splits, ws, s);
+  if (one) {
+    BwdQ8Params w = p;
+    w.dZ = nullptr;
+    e = fused(prec, w, ws, p.M * p.N, 0, s);
+  } else {
+    e = wgrad_q8_launch(prec, p.Hq, p.ld_q, p.scale, p.kind, p.G, p.ldg, p.n, p.M, p.N, splits, ws, s);
+  }
   if (e == hipSuccess && p.dZ) {
+    float* colsum = db ? cs : nullptr;
     switch (prec) {
       case 0: e = dz_t<float>(p, colsum, s); break;
       case 1: e = dz_t<f16>(p, colsum, s); break;
