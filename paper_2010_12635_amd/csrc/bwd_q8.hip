@@ -562,11 +562,18 @@ hipError_t dz_t(const BwdQ8Params& p, float* colsum, hipStream_t s) {
   return hipGetLastError();
 }
 
+// dZ by the row-streaming product with the codes as its mask, which keeps W in
+// LDS, from 1024 rows on and where 16 rows of W fit; else in tiles (both
+// products and db, us; streamed, tiles: 131072 rows, 300 <- 512 fp16 268, 326,
+// 256 <- 200 fp32 339, 373; 32768 rows, 1000 <- 300 bf16 167, 172; 1528 rows, 589
+// <- 181 fp32 33, 34).
+bool stream_dz(int prec, int64_t n, int64_t N) { return n >= 1024 && tsgemm_supported(prec, N); }
+
 }  // namespace
 
 int64_t bwd_q8_floats(int prec, int64_t n, int64_t M, int64_t N) {
   const int64_t splits = std::max<int64_t>(wgrad_splits(prec, n, M, N), fused_splits(prec, n, M, N));   // either, by the strides
-  const int64_t general = pad64(splits * M * N) + pad64(dz_blocks(n, M) * M);
+  const int64_t general = pad64(splits * M * N) + pad64(std::max<int64_t>(dz_blocks(n, M), tsgemm_colsum_rows_max()) * M);
   return N <= fused_max_n(prec) ? std::max(general, fused_splits(prec, n, M, N) * partial_stride(M, N)) : general;
 }
 
@@ -593,18 +600,26 @@ hipError_t bwd_q8_launch(int prec, const BwdQ8Params& p, const Epilogue& dw, con
   } else {
     e = wgrad_q8_launch(prec, p.Hq, p.ld_q, p.scale, p.kind, p.G, p.ldg, p.n, p.M, p.N, splits, ws, s);
   }
+  int rows = (int)dz_blocks(p.n, p.M);                     // of partial column sums
   if (e == hipSuccess && p.dZ) {
     float* colsum = db ? cs : nullptr;
-    switch (prec) {
-      case 0: e = dz_t<float>(p, colsum, s); break;
-      case 1: e = dz_t<f16>(p, colsum, s); break;
-      case 2: e = dz_t<bf16>(p, colsum, s); break;
+    if (stream_dz(prec, p.n, p.N)) {
+      Epilogue ez{};
+      ez.out = p.dZ; ez.ldo = p.ldz; ez.rows = p.n; ez.cols = p.M; ez.mode = EPI_QMASK; ez.flag = p.flag;
+      ez.relu = p.relu; ez.keep_scale = p.keep; ez.hmask = p.Hq; ez.ldh = p.ld_q;
+      e = tsgemm_launch(prec, p.G, p.ldg, p.W, p.ldw, true, p.n, p.M, p.N, ez, s, colsum, &rows);
+    } else {
+      switch (prec) {
+        case 0: e = dz_t<float>(p, colsum, s); break;
+        case 1: e = dz_t<f16>(p, colsum, s); break;
+        case 2: e = dz_t<bf16>(p, colsum, s); break;
+      }
     }
   }
   if (e != hipSuccess) return e;
   const RedJob jw = make_job(ws, splits, p.M, p.N, dw);
   if (!db) return reduce_partials2(prec, jw, nullptr, s);
-  const RedJob jb = make_job(cs, (int)dz_blocks(p.n, p.M), 1, p.M, *db);
+  const RedJob jb = make_job(cs, rows, 1, p.M, *db);
   return reduce_partials2(prec, jw, &jb, s);
 }
 

@@ -120,6 +120,7 @@ enum EpiMode : int {
   EPI_AGG = 1,     // out = cvt(dropout(act(acc + bias)))
   EPI_DMASK = 2,   // out = cvt(acc * [H > 0] * keep_scale)  (or acc if !relu_below)
   EPI_F32 = 3,     // out(fp32) = acc
+  EPI_QMASK = 4,   // EPI_DMASK with H's codes in 8 bits as the mask (!relu: every element counts)
 };
 
 struct Epilogue {
@@ -137,8 +138,8 @@ struct Epilogue {
   uint64_t layer;
   uint64_t epoch;
   const int32_t* epoch_ctr;  // if set, two int32 counters added to epoch when the kernel runs
-  // EPI_DMASK
-  const void* hmask;     // H (T), same shape as output
+  // EPI_DMASK, EPI_QMASK
+  const void* hmask;     // H (T, or a code a byte), same shape as output
   int64_t ldh;
   // overflow flag (may be NULL)
   int32_t* flag;

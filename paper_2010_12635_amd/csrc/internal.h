@@ -104,9 +104,10 @@ hipError_t spmm_launch(const CsrView& A, int prec, const void* X, int64_t ldx, i
 
 // ------------------------------------------------- tall-skinny products ----
 // C (M x N) = A (M x K, row-major, lda) . B, B(k, n) = b_kc ? B[n * ldb + k]
-// : B[k * ldb + n]; epilogue EPI_STORE or EPI_DMASK (16-byte row stores).
+// : B[k * ldb + n]; epilogue EPI_STORE, EPI_DMASK or EPI_QMASK (B k-contiguous
+// only; 16-byte row stores).
 // With colsum (B k-contiguous only), each workgroup also writes the column
-// sums of what it stored, as stored, to row w of colsum ([rows][N] floats,
+// sums of what it stored, as stored (EPI_QMASK: before rounding), to row w of colsum ([rows][N] floats,
 // *colsum_rows = the workgroups per column block, at most
 // tsgemm_colsum_rows_max()).
 bool tsgemm_supported(int prec, int64_t K);

@@ -20,6 +20,7 @@
 #include "xpose.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace gcn {
 
@@ -60,7 +61,7 @@ struct TsParams {
 
 // Staging of a wave: 16 rows of VPC output vectors, in fp32 where the epilogue
 // still has to scale the sums, else already rounded to T.
-template <typename T, bool DM, int TNW>
+template <typename T, int DM, int TNW>
 struct TsStage {
   static constexpr int OV = Vec<T>::N;
   static constexpr int VPC = TNW * 16 / OV < 8 ? TNW * 16 / OV : 8;     // vectors per row and step (at most 128 bytes)
@@ -73,14 +74,15 @@ struct TsStage {
 
 // Dynamic LDS: B block [nblk][kpad + VE] (T), then 4 per-wave staging buffers.
 // DM: epilogue multiplies by the ReLU/dropout derivative read from H
-// (EPI_DMASK with relu); otherwise a plain store.
+// (EPI_DMASK with relu: 1) or from its 8-bit codes (EPI_QMASK: 2); otherwise a
+// plain store.
 // CS: the workgroup also sums the stored values (as stored, i.e. rounded to
-// T) of each of its columns: a lane stores the same column vectors of every
+// T; before they are rounded with codes) of each of its columns: a lane stores the same column vectors of every
 // tile and sums them in registers (tiles in order); at the end the lanes of
 // equal columns, then the four waves in wave order, are added into the
 // workgroup's row of p.colsum (bias gradient of the layer below, without a
 // pass of its own over C).
-template <typename T, bool BKC, bool DM, bool CS, int TM, int TNW>
+template <typename T, bool BKC, int DM, bool CS, int TM, int TNW>
 __global__ __launch_bounds__(256) void tsgemm_kernel(TsParams p) {
   using St = TsStage<T, DM, TNW>;
   constexpr int VE = Vec<T>::N;
@@ -155,6 +157,7 @@ __global__ __launch_bounds__(256) void tsgemm_kernel(TsParams p) {
   const int tnw = min(TNW, nblk / 16);              // live column tiles of this block
   constexpr int OV = Vec<T>::N;
   const int sr = lane / St::VPC, sv = lane % St::VPC;   // this lane's row and vector of a staging step
+  const uint32_t every = p.epi.relu ? 0u : ~0u;          // codes: no mask, every element counts
   float creg[St::NCH][OV];                              // CS: sums of its column vectors
 #pragma unroll
   for (int c = 0; c < St::NCH; ++c)
@@ -193,13 +196,15 @@ __global__ __launch_bounds__(256) void tsgemm_kernel(TsParams p) {
     // The ReLU/dropout derivative of the epilogue reads H: for 16-bit types
     // the wave's H vectors are requested together with its A fragments, so
     // the tile costs one memory latency.
-    constexpr bool dmask = DM;
-    constexpr bool HPRE = DM && sizeof(T) == 2;          // H prefetched into registers
+    constexpr bool dmask = DM != 0, codes = DM == 2;
+    constexpr bool HPRE = codes || (DM && sizeof(T) == 2);   // H prefetched into registers
     constexpr int EIT = HPRE ? St::NCH * St::IT : 1;     // vectors per lane per 16 rows
-    uint4 hv[TM][EIT];
+    typedef std::conditional_t<codes, std::conditional_t<OV == 8, uint2, uint32_t>, uint4> HV;
+    HV hv[TM][EIT];
     auto prefetch_h = [&]() {
       if constexpr (HPRE) {
-        const T* hm = reinterpret_cast<const T*>(p.epi.hmask);
+        typedef std::conditional_t<codes, uint8_t, T> HE;
+        const HE* hm = reinterpret_cast<const HE*>(p.epi.hmask);
 #pragma unroll
         for (int tm = 0; tm < TM; ++tm)
 #pragma unroll
@@ -207,7 +212,7 @@ __global__ __launch_bounds__(256) void tsgemm_kernel(TsParams p) {
             const int rr = sr + (64 / St::VPC) * (it % St::IT), cv = sv + St::VPC * (it / St::IT);
             const int64_t row = r0 + tm * 16 + rr, col = n0 + cv * OV;
             const bool ok = rr < 16 && cv * OV < nblk && row < p.M && col < p.N;
-            hv[tm][it] = ldg16(hm + (ok ? row * p.epi.ldh + col : 0));
+            hv[tm][it] = *reinterpret_cast<const HV*>(hm + (ok ? row * p.epi.ldh + col : 0));
           }
       }
     };
@@ -306,11 +311,20 @@ __global__ __launch_bounds__(256) void tsgemm_kernel(TsParams p) {
             float v[OV], h[OV];
 #pragma unroll
             for (int j = 0; j < OV; ++j) v[j] = reinterpret_cast<const float*>(at)[sv * OV + j];
-            if constexpr (HPRE) unpack<T>(hv[tm][c * St::IT + it], h);
+            if constexpr (codes) {
+              uint32_t w[2];
+              __builtin_memcpy(w, &hv[tm][c * St::IT + it], OV);
+#pragma unroll
+              for (int j = 0; j < OV; ++j) h[j] = (float)(((w[j / 4] | every) >> (8 * (j % 4))) & 0xffu);
+            } else if constexpr (HPRE) unpack<T>(hv[tm][c * St::IT + it], h);
             else unpack<T>(ldg16(reinterpret_cast<const T*>(p.epi.hmask) + row * p.epi.ldh + col), h);
 #pragma unroll
             for (int j = 0; j < OV; ++j) v[j] = h[j] > 0.f ? v[j] * p.epi.keep_scale : 0.f;
             o = pack<T>(v);
+            if constexpr (CS && codes) {
+#pragma unroll
+              for (int j = 0; j < OV; ++j) creg[c][j] += j < live ? v[j] : 0.f;
+            }
           } else {
             o = *reinterpret_cast<const uint4*>(at + sv * 16);
           }
@@ -322,7 +336,7 @@ __global__ __launch_bounds__(256) void tsgemm_kernel(TsParams p) {
 #pragma unroll
           for (int j = 0; j < OV; ++j) bad |= !finite_f32(st[j]);
           if (bad) raise_flag(p.epi.flag);
-          if constexpr (CS) {
+          if constexpr (CS && !codes) {
 #pragma unroll
             for (int j = 0; j < OV; ++j) creg[c][j] += st[j];
           }
@@ -400,7 +414,7 @@ int ts_nblk(int64_t M, int64_t N, int64_t kpad, bool dm) {
   return (int)block(parts);
 }
 
-template <typename T, bool BKC, bool DM, bool CS, int TM>
+template <typename T, bool BKC, int DM, bool CS, int TM>
 hipError_t launch_tm(const TsParams& p, int* grid_rows, hipStream_t s) {
   const int tnw = p.nblk / 16;
   const size_t lds = ts_lds_bytes<T>(p.nblk, p.kpad, DM);
@@ -427,7 +441,7 @@ hipError_t launch_tm(const TsParams& p, int* grid_rows, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <typename T, bool BKC, bool DM, bool CS>
+template <typename T, bool BKC, int DM, bool CS>
 hipError_t launch_b(TsParams p, int* grid_rows, hipStream_t s) {
   constexpr int KC = 4 * Vec<T>::N;
   p.kpad = (p.K + KC - 1) / KC * KC;
@@ -450,13 +464,17 @@ hipError_t launch_b(TsParams p, int* grid_rows, hipStream_t s) {
 template <typename T>
 hipError_t launch_t(const TsParams& p, bool bkc, int* grid_rows, hipStream_t s) {
   const bool dm = p.epi.mode == EPI_DMASK && p.epi.relu;
+  if (p.epi.mode == EPI_QMASK) {
+    if (!bkc) return hipErrorInvalidValue;
+    return p.colsum ? launch_b<T, true, 2, true>(p, grid_rows, s) : launch_b<T, true, 2, false>(p, grid_rows, s);
+  }
   if (p.colsum) {
     if (!bkc) return hipErrorInvalidValue;
-    return dm ? launch_b<T, true, true, true>(p, grid_rows, s) : launch_b<T, true, false, true>(p, grid_rows, s);
+    return dm ? launch_b<T, true, 1, true>(p, grid_rows, s) : launch_b<T, true, 0, true>(p, grid_rows, s);
   }
-  if (!bkc && !dm) return launch_b<T, false, false, false>(p, grid_rows, s);
-  if (!dm) return launch_b<T, true, false, false>(p, grid_rows, s);
-  return bkc ? launch_b<T, true, true, false>(p, grid_rows, s) : launch_b<T, false, true, false>(p, grid_rows, s);
+  if (!bkc && !dm) return launch_b<T, false, 0, false>(p, grid_rows, s);
+  if (!dm) return launch_b<T, true, 0, false>(p, grid_rows, s);
+  return bkc ? launch_b<T, true, 1, false>(p, grid_rows, s) : launch_b<T, false, 1, false>(p, grid_rows, s);
 }
 
 }  // namespace
