@@ -614,8 +614,9 @@ gcn_status gcn_quantize_weights(int64_t f_in, int64_t f_out, int32_t prec, const
 /* gcn_transform_q8: gcn_transform from rows and weights in 8 bits,
  *   S_ij = h_scale[i] w_scale[j] sum_k Hq_ik Wq_jk     (n x f_out, ld_s, prec)
  * The sum is exact (32-bit integers); it is converted to fp32 and scaled there
- * (the scales' exponents are added apart, so nothing between overflows), then
- * rounded to prec.  w_sum (as gcn_quantize_weights writes it) is read with
+ * (scales are 2^-126 or more, as the calls above write them: nothing on the way
+ * then leaves fp32's range where the result is inside it), then rounded to
+ * prec.  S overlaps no input.  w_sum (as gcn_quantize_weights writes it) is read with
  * GCN_Q8_RELU only and may otherwise be NULL.  *overflow is set if a stored
  * element is not finite.  No workspace.  Asynchronous. */
 gcn_status gcn_transform_q8(int64_t n, int64_t f_in, int64_t f_out, int32_t kind, const void* Hq, int64_t ld_q,
@@ -629,7 +630,7 @@ gcn_status gcn_transform_q8(int64_t n, int64_t f_in, int64_t f_out, int32_t kind
  *   dW       = H~^T G_S            (f_in x ld_w fp32; cols >= f_out set to 0)
  *   dZ_below = (G_S W^T) * [Hq > 0] / (1 - p_below)   if act_below == RELU
  *            =  G_S W^T                               if act_below == NONE
- *              (n x f_in, ld_dz, prec; NULL skips it; not G_S itself)
+ *              (n x f_in, ld_dz, prec; NULL skips it; it overlaps no input)
  *   dbias_below = column sums of dZ_below before it is rounded (fp32 [f_in
  *              rounded up to 8], entries past f_in set to 0; may be NULL, needs
  *              dZ_below)

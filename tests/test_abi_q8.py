@@ -103,6 +103,7 @@ def test_backward(call, args, status):
     (dict(ldw=0), SHAPE), (dict(ldw=12), ALIGN), (dict(ldg=0), SHAPE), (dict(ldg=12), ALIGN), (dict(ldz=16), SHAPE),
     (dict(ldz=28), ALIGN), (dict(f=WIDE, ldq=WIDE, ldz=WIDE), UNSUPPORTED),
     (dict(fo=WIDE, ldw=WIDE, ldg=WIDE), UNSUPPORTED),
+    (dict(ldw=1 << 60), UNSUPPORTED),
     (dict(f=65536, fo=16384, ldq=65536, ldz=65536, ldw=16384, ldg=16384), UNSUPPORTED)])
 def test_backward_shapes(args, status):
     assert backward(**args) == status
