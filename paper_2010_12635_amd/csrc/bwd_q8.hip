@@ -465,10 +465,11 @@ int64_t fused_splits(int prec, int64_t n, int64_t M, int64_t N) {
   return std::min({tiles, std::max<int64_t>(1, held), std::max<int64_t>(1, cheap)});
 }
 
-template <typename T, int NB>
+// 32 columns of H a wave, or 16 (FI = 1) where 32 would leave registers for one
+// wave a SIMD only.
+template <typename T, int NB, int FI = NB * sizeof(T) >= 512 ? 1 : 2>
 hipError_t fused_nb(int prec, const BwdQ8Params& p, float* partials, int64_t stride, int sums, hipStream_t s) {
-  // 16 columns of H a wave where 32 would leave registers for one wave a SIMD only
-  constexpr int FI = NB >= 128 ? 1 : 2, W1 = 2 / FI;
+  constexpr int W1 = 2 / FI;
   const int64_t tiles = (p.n + TV - 1) / TV;
   const int fb = (int)fused_columns(p.M);
   const dim3 grid((unsigned)fused_splits(prec, p.n, p.M, p.N), (unsigned)((p.M + fb - 1) / fb),
@@ -487,8 +488,15 @@ hipError_t fused_t(int prec, const BwdQ8Params& p, float* partials, int64_t stri
   if (p.N <= 16) return fused_nb<T, 16>(prec, p, partials, stride, sums, s);
   if (p.N <= 32) return fused_nb<T, 32>(prec, p, partials, stride, sums, s);
   if (p.N <= 64) return fused_nb<T, 64>(prec, p, partials, stride, sums, s);
-  if constexpr (sizeof(T) == 2)
+  if constexpr (sizeof(T) == 2) {
     if (p.N > 128) return fused_nb<T, 256>(prec, p, partials, stride, sums, s);
+    // 16 columns a wave, twice the waves, where there is one workgroup a compute
+    // unit (us; 32, 16 columns): 262144 rows, 256 <- 100 fp16 76, 89; 65536 rows 40,
+    // 45 (282 workgroups); 131072 rows, 128 <- 128 34.6, 33.4 (250); 65536 rows, 128
+    // <- 100 27, 25 (200).
+    const int64_t fb = fused_columns(p.M), wgs = fused_splits(prec, p.n, p.M, p.N) * ((p.M + fb - 1) / fb);
+    if (wgs <= 256) return fused_nb<T, 128, 1>(prec, p, partials, stride, sums, s);
+  }
   return fused_nb<T, 128>(prec, p, partials, stride, sums, s);
 }
 

@@ -237,7 +237,8 @@ def test_product_scales_out_of_range(n, N):
 BWD_SIZES = [(1, 1, 1), (1, 40, 7), (2, 16, 16), (3, 128, 64), (15, 9, 3), (16, 64, 32), (17, 65, 33), (63, 100, 7),
              (64, 128, 64), (65, 130, 40), (129, 17, 130), (200, 512, 16), (255, 33, 256), (500, 500, 64), (1000, 16, 7),
              (1025, 256, 64), (3001, 128, 40), (4096, 64, 128), (777, 300, 257), (900, 2048, 16), (300, 70, 600),
-             (20000, 128, 64), (6000, 200, 200), (1030, 33, 300), (2100, 250, 520), (1100, 40, 2600)]
+             (20000, 128, 64), (6000, 200, 200), (1030, 33, 300), (2100, 250, 520), (1100, 40, 2600),
+             (20000, 20, 66), (26000, 40, 70), (18000, 500, 66), (81000, 128, 100)]
 
 
 def backward(q, s, w, g, prec, kind, n, M, N, act, p, below=True, colsum=True, ld_dz=None, stream=None, ws=None):
