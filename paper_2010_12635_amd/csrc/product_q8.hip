@@ -78,7 +78,7 @@ struct ResultRows {
 #pragma unroll
     for (int k = 0; k < 16 * STRIPS / RPS; ++k) {
       const int rk = row + k * RPS;
-      const uint4 v = ldg16(stage + (rk * PARTS + (part ^ (rk & (PARTS - 1)))) * 16);
+      const uint4 v = ldg16(stage + (rk * PARTS + (part ^ (rk & 15 & (PARTS - 1)))) * 16);   // row & 15 of its strip
       T* at = all ? dst + k * RPS * p.ld_s : dst + min(row0 + rk, p.n - 1) * p.ld_s;
       if (here) stg16(at, v);
     }

@@ -198,6 +198,29 @@ def test_product(prec, n, K, N):
         assert (S[:, round8(N):] == 5.0).all()
 
 
+@pytest.mark.parametrize("n,K,N", [(20000, 100, 128), (20000, 500, 128), (20000, 512, 100), (33001, 577, 130),
+                                   (50000, 530, 200), (65001, 600, 250), (16384, 4100, 300), (5000, 640, 40)])
+@pytest.mark.parametrize("prec", PRECS)
+def test_product_many_rows(prec, n, K, N):
+    """As test_product, with the reference in float64 on the GPU (whole sums below 2^53: exact)."""
+    gen = torch.Generator(device="cuda").manual_seed(n + K + N)
+    for kind in KINDS:
+        lo, hi = (-127, 128) if kind == "signed" else (0, 256)
+        q = torch.randint(lo, hi, (n, K), generator=gen, device="cuda", dtype=torch.int32)
+        w = torch.randint(-127, 128, (N, K), generator=gen, device="cuda", dtype=torch.int32)
+        s = (0.5 + 1.5 * torch.rand(n, generator=gen, device="cuda")) * (2.0 ** -9 / K)
+        ws = (0.5 + 1.5 * torch.rand(N, generator=gen, device="cuda")) * 2.0 ** -7
+        tq = torch.full((n, round16(K) + 16), 0x5a, dtype=torch.uint8, device="cuda")
+        tw = torch.full((N, round16(K)), 0x77, dtype=torch.uint8, device="cuda")
+        tq[:, :K], tw[:, :K] = (q & 255).to(torch.uint8), (w & 255).to(torch.uint8)
+        wsum = w.sum(1, dtype=torch.int32) if kind == "relu" else None
+        S, ov = product(tq, s, tw, ws, wsum, prec, kind, n, K, N, round8(N) + 8)
+        want = q.double() @ w.double().t().contiguous() * s.double()[:, None] * ws.double()
+        tol = want.abs() * (HALF_STEP[prec] + 4.01 * 2.0 ** -24) + LEAST[prec]
+        assert ((S[:, :N].double() - want).abs() <= tol).all(), kind
+        assert (S[:, round8(N):] == 5.0).all() and ov.item() == 0
+
+
 @pytest.mark.parametrize("n,K,N", [(1, 65536, 3), (40, 65536, 20), (300, 65536, 70)])
 def test_product_largest_sums(n, K, N):
     """Sums next to the 32-bit border: every code at its largest."""
