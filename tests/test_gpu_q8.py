@@ -314,6 +314,33 @@ def test_backward_whole_numbers(prec, n, M, N):
     assert ov.item() == 0 and ov2.item() == 0
 
 
+@pytest.mark.parametrize("n,M,N", [(60000, 256, 250), (60001, 128, 100), (100000, 16, 16), (30000, 2048, 13),
+                                   (90000, 100, 30), (70000, 60, 200), (50000, 256, 64), (200000, 30, 130),
+                                   (60000, 130, 300)])
+@pytest.mark.parametrize("prec", PRECS)
+def test_backward_many_rows(prec, n, M, N):
+    """Several tiles a workgroup, with the reference in float64 on the GPU: whole numbers whose sums stay below
+    2^24 (|dW| <= 15 n, |dZ| <= 2 N, |db| as asserted), so all are exact."""
+    gen = torch.Generator(device="cuda").manual_seed(n + M + N)
+    dt = G.torch_dtype(prec)
+    for kind, act, p in (("relu", G.GCN_ACT_RELU, 0.5), ("signed", G.GCN_ACT_NONE, 0.0)):
+        q = torch.randint(-15 if kind == "signed" else 0, 16, (n, M), generator=gen, device="cuda", dtype=torch.int32)
+        q *= torch.randint(0, 2, (n, M), generator=gen, device="cuda", dtype=torch.int32)
+        g = torch.randint(-1, 2, (n, N), generator=gen, device="cuda").double()
+        w = torch.randint(-1, 2, (M, N), generator=gen, device="cuda").double()
+        tq = torch.full((n, round16(M)), 0x5a, dtype=torch.uint8, device="cuda")
+        tq[:, :M] = (q & 255).to(torch.uint8)
+        dW, dZ, db, ov = backward(tq, torch.ones(n, device="cuda"), padded(w, dt, round8(N)), padded(g, dt, round8(N)),
+                                  prec, kind, n, M, N, act, p)
+        z = g @ w.t().contiguous()
+        if act:
+            z = z * (q > 0) * 2
+        assert z.abs().sum(0).max() < 2 ** 24
+        assert torch.equal(dW[:, :N].double(), q.t().contiguous().double() @ g), kind
+        assert torch.equal(dZ[:, :M], z.to(dt)), kind
+        assert torch.equal(db[:M].double(), z.sum(0)) and ov.item() == 0, kind
+
+
 @pytest.mark.parametrize("n,M,N", [(3000, 128, 64), (700, 500, 64), (1500, 40, 300), (5000, 24, 7)])
 @pytest.mark.parametrize("prec", PRECS)
 def test_backward_numbers(prec, n, M, N):
