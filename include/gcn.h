@@ -582,7 +582,8 @@ gcn_status gcn_optimizer_step_half(int64_t count, void* w, const float* grad, vo
  * A row that holds a NaN or an infinity gets the scale NaN and codes 0, and sets
  * *overflow.  Codes lie row by row with leading dimension ld_q, ld_q % 16 == 0
  * (16-byte loads); columns [f, ld_q) are ignored where codes are read and may
- * be overwritten with 0 where they are written.  n is at most 2^31 - 1 and a
+ * be overwritten with 0 where they are written, as may the padding of the other
+ * results up to the next multiple of 8 columns.  n is at most 2^31 - 1 and a
  * width at most 65536 (sums of 8-bit products stay within 32 bits;
  * GCN_ERR_UNSUPPORTED above).  Results do not depend on the timing of the run.
  * ======================================================================== */
