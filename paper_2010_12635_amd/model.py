@@ -372,12 +372,14 @@ class GCN2:
         if self.X32 is not None:
             G.gcn_cast(self.n, self.f_in, G.GCN_F32, self.X32, self.ld_x, self.prec, self.X, self.ld_x,
                        self.overflow, stream)
+        self._cast_adjacency(self.overflow, stream)
+
+    def _cast_adjacency(self, flag, stream):
         g = self.g
         if g.adj.format == G.GCN_DENSE:
-            G.gcn_cast(self.n, self.n, G.GCN_F32, g.dense, g.ld_dense, self.prec, self.A16, g.ld_dense,
-                       self.overflow, stream)
+            G.gcn_cast(self.n, self.n, G.GCN_F32, g.dense, g.ld_dense, self.prec, self.A16, g.ld_dense, flag, stream)
         elif self.A16 is not None:
-            G.gcn_cast(1, g.nnz, G.GCN_F32, g.values, 0, self.prec, self.A16, 0, self.overflow, stream)
+            G.gcn_cast(1, g.nnz, G.GCN_F32, g.values, 0, self.prec, self.A16, 0, flag, stream)
 
     def loss_and_backward(self, stream=None):
         a = self.adj
@@ -455,8 +457,8 @@ class GCN2:
         if self.q8 is None:
             raise ValueError("forward8() answers from what quantize() lays out: call it first")
         n, flag, a = self.n, self.scores_overflow, self.adj
-        if self.level == "O1":          # A_hat's 16-bit copy, as in forward()
-            self.cast_inputs(stream)
+        if self.level == "O1":          # A_hat's 16-bit copy, as in forward(); X is read as codes
+            self._cast_adjacency(flag, stream)
         if self.featureless:            # I W1 = W1 is read in place
             S1 = self.W1w()
         else:

@@ -82,3 +82,28 @@ def test_backward_beside_captured_epochs(level, prec):
         a.loss_and_backward()
         b.loss_and_backward()
         same(a, b, k)
+
+
+@pytest.mark.parametrize("dense", [False, True])
+def test_answers_at_o1_leave_the_training_step_alone(dense):
+    """forward8() reads the features as codes, which hold numbers beyond the 16-bit type: no 16-bit copy of them is
+    made, and the flag of the training step is not raised; what cannot be held raises that of the answers."""
+    wl = dict(I.workload("er2k", 0, n_override=600))
+    wl["X"] = np.array(wl["X"], np.float32)
+    wl["X"][3, 5] = 1e6                    # times weights below 1e-2: products inside binary16's range
+    wl["W1"] = wl["W1"] * np.float32(1e-2 / np.abs(wl["W1"]).max())
+    m = make(wl, G.GCN_F16, "O1", dense=dense)
+    m.quantize()
+    m.X.zero_()
+    m.forward8()
+    torch.cuda.synchronize()
+    assert not m.X.any() and m.overflow.item() == 0 and m.scores_overflow.item() == 0
+    s1, x = f64(m.SG1[3, :m.f_h]), f64(m.X32[3, :m.f_in])
+    # a feature's and a weight's code are within one step of their rows' largest value over 127
+    w, wtop = f64(m.W1w()[:, :m.f_h]), np.abs(f64(m.W1w()[:, :m.f_h])).max(0)
+    err = 1e6 / 127 * np.abs(w).sum(0) + wtop / 127 * np.abs(x).sum() + x.size * 1e6 / 127 * wtop / 127
+    assert np.all(np.abs(s1 - x @ w) <= err + 2.0 ** -11 * np.abs(x @ w) + 2.0 ** -24) and np.abs(s1).max() > 0
+    (m.g.dense if dense else m.g.values).view(-1)[0] = 1e6
+    m.forward8()
+    torch.cuda.synchronize()
+    assert m.overflow.item() == 0 and m.scores_overflow.item() == 1
