@@ -583,9 +583,10 @@ gcn_status gcn_optimizer_step_half(int64_t count, void* w, const float* grad, vo
  * *overflow.  Codes lie row by row with leading dimension ld_q, ld_q % 16 == 0
  * (16-byte loads); columns [f, ld_q) are ignored where codes are read and may
  * be overwritten with 0 where they are written, as may the padding of the other
- * results up to the next multiple of 8 columns.  n is at most 2^31 - 1 and a
- * width at most 65536 (sums of 8-bit products stay within 32 bits;
- * GCN_ERR_UNSUPPORTED above).  Results do not depend on the timing of the run.
+ * results up to the next multiple of 8 columns.  n is at most 2^31 - 1, a
+ * width at most 65536 (sums of 8-bit products stay within 32 bits) and a leading
+ * dimension at most 2^48 (GCN_ERR_UNSUPPORTED above).  Results do not depend on
+ * the timing of the run.
  * ======================================================================== */
 typedef enum gcn_q8_kind { GCN_Q8_SIGNED = 0, GCN_Q8_RELU = 1 } gcn_q8_kind;
 #define GCN_Q8_MAX_WIDTH 65536

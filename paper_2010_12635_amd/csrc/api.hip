@@ -829,12 +829,16 @@ namespace {
 
 bool valid_kind(int32_t k) { return k == GCN_Q8_SIGNED || k == GCN_Q8_RELU; }
 
+// The largest leading dimension: no two rows that far apart fit an address space,
+// and what is computed from it (the bytes of 64 rows) stays within 64 bits.
+constexpr int64_t MAX_LD = (int64_t)1 << 48;
+
 // n rows of f codes.
 gcn_status check_codes(int64_t n, int64_t f, int32_t kind, int64_t ld_q) {
   if (!valid_kind(kind)) return GCN_ERR_INVALID_ARG;
   if (n <= 0 || f <= 0 || ld_q < f) return GCN_ERR_SHAPE;
   if (ld_q % 16) return GCN_ERR_ALIGNMENT;
-  if (n > INT32_MAX || f > GCN_Q8_MAX_WIDTH) return GCN_ERR_UNSUPPORTED;
+  if (n > INT32_MAX || f > GCN_Q8_MAX_WIDTH || ld_q > MAX_LD) return GCN_ERR_UNSUPPORTED;
   return GCN_OK;
 }
 
@@ -842,7 +846,7 @@ gcn_status check_codes(int64_t n, int64_t f, int32_t kind, int64_t ld_q) {
 gcn_status check_ld(int64_t f, int64_t ld) {
   if (f <= 0 || ld < f) return GCN_ERR_SHAPE;
   if (ld % 8) return GCN_ERR_ALIGNMENT;
-  return f > GCN_Q8_MAX_WIDTH ? GCN_ERR_UNSUPPORTED : GCN_OK;
+  return f > GCN_Q8_MAX_WIDTH || ld > MAX_LD ? GCN_ERR_UNSUPPORTED : GCN_OK;
 }
 
 // The weight gradient's partial sums are reduced by one launch.
