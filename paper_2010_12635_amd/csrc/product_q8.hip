@@ -53,6 +53,12 @@ struct ResultRows {
   uint8_t* stage;
   int lane;
   float most = 0.f;                                        // the largest size of any result
+  // Lanes read what others of their wave wrote, and then write over it.
+  static __device__ __forceinline__ void lanes_meet() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  }
   __device__ __forceinline__ ResultRows(uint8_t* s, int l) : stage(s), lane(l) {}
   // Group q's XE columns of this lane's row, of which `left` are columns of S;
   // the others are padding: 0.
@@ -74,7 +80,7 @@ struct ResultRows {
     const int64_t c = col0 + part * Vec<T>::N;
     const bool all = row0 + 16 * STRIPS <= p.n, here = c < p.N;
     T* dst = static_cast<T*>(p.S) + (all ? row0 + row : 0) * p.ld_s + c;
-    __builtin_amdgcn_wave_barrier();
+    lanes_meet();
 #pragma unroll
     for (int k = 0; k < 16 * STRIPS / RPS; ++k) {
       const int rk = row + k * RPS;
@@ -82,7 +88,7 @@ struct ResultRows {
       T* at = all ? dst + k * RPS * p.ld_s : dst + min(row0 + rk, p.n - 1) * p.ld_s;
       if (here) stg16(at, v);
     }
-    __builtin_amdgcn_wave_barrier();
+    lanes_meet();
   }
 };
 
