@@ -289,11 +289,16 @@ __global__ __launch_bounds__(256) void wgrad_kernel(WgParams p) {
 template <typename T, bool Q8>
 hipError_t launch_t(const WgParams& p, int splits, hipStream_t s) {
   dim3 grid((unsigned)splits, (unsigned)((p.M + WG_B - 1) / WG_B), (unsigned)((p.N + WG_B - 1) / WG_B));
-  if (p.N <= 16) hipLaunchKernelGGL((wgrad_kernel<T, 16, Q8>), grid, dim3(256), 0, s, p);
-  else if (p.N <= 32) hipLaunchKernelGGL((wgrad_kernel<T, 32, Q8>), grid, dim3(256), 0, s, p);
-  else if (p.N <= 48) hipLaunchKernelGGL((wgrad_kernel<T, 48, Q8>), grid, dim3(256), 0, s, p);
-  else if (p.N <= 64) hipLaunchKernelGGL((wgrad_kernel<T, 64, Q8>), grid, dim3(256), 0, s, p);
-  else hipLaunchKernelGGL((wgrad_kernel<T, 128, Q8>), grid, dim3(256), 0, s, p);
+  // codes come here with more than 128 columns of G in fp32, and with rows too
+  // far apart for the one-pass kernel, of any width: one form serves them
+  if constexpr (!Q8) {
+    if (p.N <= 16) hipLaunchKernelGGL((wgrad_kernel<T, 16, false>), grid, dim3(256), 0, s, p);
+    else if (p.N <= 32) hipLaunchKernelGGL((wgrad_kernel<T, 32, false>), grid, dim3(256), 0, s, p);
+    else if (p.N <= 48) hipLaunchKernelGGL((wgrad_kernel<T, 48, false>), grid, dim3(256), 0, s, p);
+    else if (p.N <= 64) hipLaunchKernelGGL((wgrad_kernel<T, 64, false>), grid, dim3(256), 0, s, p);
+    if (p.N <= 64) return hipGetLastError();
+  }
+  hipLaunchKernelGGL((wgrad_kernel<T, 128, Q8>), grid, dim3(256), 0, s, p);
   return hipGetLastError();
 }
 
