@@ -6,7 +6,8 @@ import torch
 
 from paper_2010_12635_amd import gcn as G
 from paper_2010_12635_amd import inputs as I
-from tests.test_gpu_q8_model import LEVELS, f64, make
+from tests.test_gpu_q8 import LEAST
+from tests.test_gpu_q8_model import LEVELS, f64, make, wide_workload
 
 pytestmark = pytest.mark.gpu
 
@@ -107,3 +108,23 @@ def test_answers_at_o1_leave_the_training_step_alone(dense):
     m.forward8()
     torch.cuda.synchronize()
     assert m.overflow.item() == 0 and m.scores_overflow.item() == 1
+
+
+@pytest.mark.parametrize("level,prec", LEVELS)
+def test_mask(level, prec):
+    """dZ1 is 0 exactly where H1 is, in every type, and nowhere else but where its own value rounds to 0: values
+    that a code's half step would round to 0 count too."""
+    m = make(wide_workload(), prec, level, checkpoint8=True)
+    m.forward(0)
+    h1 = m.H1[:, :m.f_h].clone()
+    m.loss_and_backward()
+    torch.cuda.synchronize()
+    dz, on = m.dZ1[:, :m.f_h], h1 > 0
+    assert not dz[~on].any()
+    assert (on & (h1.double() < 0.5 * m.H1s.double()[:, None])).any()
+    gs, w = f64(m.SG2[:, :m.C]), f64(m.W2w()[:, :m.C])
+    # C products added in fp32, cut off at the worst, and the two roundings by 1 / (1 - p)
+    err = (m.C + 4) * 2.0 ** -23 * (np.abs(gs) @ np.abs(w).T) * 2
+    sure = on.cpu().numpy() & (np.abs(gs @ w.T * 2) > err + LEAST[prec])
+    learns = on.cpu().numpy() & gs.any(1, keepdims=True)      # rows beside one with a label
+    assert np.mean(sure[learns]) > 0.9 and np.all(f64(dz)[sure] != 0)
