@@ -140,8 +140,9 @@ __global__ __launch_bounds__(64 * WM) __attribute__((amdgpu_waves_per_eu(2))) vo
   // A wave's 1 KiB pieces of a tile, by wave 0 its scales: where a lane's 16 bytes
   // of piece pc lie from the tile's first row on.  Rows past `last` are copies of
   // it, pieces past the widths of the first.  The places stay the same from tile
-  // to tile and are kept where registers allow (2^21 rows, 128 <- 64 fp16 220 ->
-  // 208 us).
+  // to tile and are kept up to 128 columns of G and six pieces a wave (2^21 rows,
+  // 128 <- 64 fp16 220 -> 208 us); of these, fp32 with 128 columns of both spills 68
+  // bytes a lane.
   constexpr int PIECES = STAGE / 1024, PPW = (PIECES + WM - 1) / WM;
   constexpr bool KEEP = PPW <= 6 && NB <= 128;
   auto place = [&](int pc, int last) -> uint32_t {
@@ -450,14 +451,17 @@ int64_t fused_max_n(int prec) { return prec == 0 ? 128 : 256; }
 
 int64_t fused_columns(int64_t M) { return M <= 32 ? 32 : M <= 64 ? 64 : 128; }
 
-// Workgroups along the rows, each with its own partial sums: eight waves a
+// Workgroups along the rows, each with its own partial sums: two of four waves a
 // compute unit, or fewer where a tile more for each costs less than another row
 // of partial sums to write and read back.  With a tile at 1 us and partial sums
 // at 4 TB/s both ways, tiles / w + w 8 M N / 4e6 is least at w = sqrt(5e5 tiles /
 // (M N)).  Measured (us; 256, 512, 768, 1024 workgroups in all, before tiles were
 // placed ahead): 2^21 rows, 128 <- 64 fp16 277, 220, 224, 229; 32768 rows, 2048
 // <- 16 fp16 66, 54, 54, 59; 16384 rows, 500 <- 64 bf16 13.4 with 64 along the
-// rows, 20 with 192.
+// rows, 20 with 192 (the rule's 63: 12.9).  The rule does not count rounds: with 16
+// columns a wave, 128 columns of H are eight waves and one workgroup a compute
+// unit (82 KB of LDS), and 2^18 rows, 256 <- 256 get 352 of them, a round of 256 and
+// a third of another; the 63 of 16384 rows walk 256 tiles, four or five each.
 int64_t fused_splits(int prec, int64_t n, int64_t M, int64_t N) {
   const int64_t fb = fused_columns(M), nb = fused_max_n(prec), tiles = (n + TV - 1) / TV;
   const int64_t blocks = (M + fb - 1) / fb * ((N + nb - 1) / nb), held = 512 * (128 / fb) / blocks;
