@@ -163,9 +163,9 @@ class GCN2:
         the mask of ReLU and dropout stays exact.  H1 and dZ1 then share one
         buffer: H1 is gone after loss_and_backward().  An evaluation
         (training=False) keeps nothing; a backward pass behind one quantises
-        its H1 first.  A backward pass recorded into a graph without its
-        forward pass reads what was kept when it was recorded, or quantises H1,
-        whichever held then."""
+        its H1 first.  A graph of a backward pass does what the forward pass
+        recorded before it asks for (without one, the last that ran): replay it
+        behind that kind of pass only."""
         dev = torch.device(device)
         if level is None:
             level = "O0" if prec == G.GCN_F32 else "O2"
@@ -264,7 +264,9 @@ class GCN2:
         self.checkpoint8 = bool(checkpoint8)
         self.ld_q = (self.f_h + 15) // 16 * 16
         self.H1q = self.H1s = None      # H1 in 8 bits: codes and a scale for each vertex
-        self._h1_kept = False           # they are those of the last forward pass
+        # they are those of the last forward pass: of those that ran (False) and
+        # of those recorded into a graph (True)
+        self._h1_kept = {False: False}
         if self.checkpoint8:
             self._alloc_h1q(dev)
         self.SG1 = torch.empty((n, self.ld_h), dtype=self.dt, device=dev)   # S1, later G_S1
@@ -328,7 +330,7 @@ class GCN2:
     def _keep_h1(self, flag, stream):
         G.gcn_quantize(self.n, self.f_h, self.prec, self.H1, self.ld_h, G.GCN_Q8_RELU, self.H1q, self.ld_q, self.H1s, flag,
                        stream)
-        self._h1_kept = True
+        self._h1_kept[torch.cuda.is_current_stream_capturing()] = True
 
     def forward(self, epoch: int, training: bool = True, stream=None, agg_timer=None, gemm_timer=None):
         """Both layers.  With ``agg_timer`` (a callable returning a context
@@ -341,7 +343,7 @@ class GCN2:
             if agg_timer is not None or gemm_timer is not None:
                 raise ValueError("timed split calls take the epoch from the host; use device_epoch=False")
             epoch = 0         # the device counter supplies the epoch
-        self._h1_kept = False
+        self._h1_kept[torch.cuda.is_current_stream_capturing()] = False
         if self.level == "O1":
             self.cast_inputs(stream)
         if agg_timer is None:
@@ -402,8 +404,8 @@ class GCN2:
             db2 = None
         # db1 (the column sums of dZ1) comes from the call that writes dZ1
         if self.checkpoint8:
-            if not self._h1_kept:      # an evaluation's H1
-                self._keep_h1(self.overflow, stream)
+            if not self._h1_kept.get(torch.cuda.is_current_stream_capturing(), self._h1_kept[False]):
+                self._keep_h1(self.overflow, stream)       # an evaluation's H1
             G.gcn_layer_bwd_q8(a, self.L2, self.prec, G.GCN_Q8_RELU, self.H1q, self.ld_q, self.H1s, self.W2w(), self.dZ2,
                                G.GCN_ACT_RELU, self.p, self.dW2(), db2, self.dZ1, self.SG2, self.overflow, self.ws,
                                stream, dbias_below=self.db1())
@@ -587,19 +589,15 @@ class GCN2:
             raise ValueError("capture() needs device_epoch=True")
         torch.cuda.synchronize()
         g = torch.cuda.CUDAGraph()
-        kept = self._h1_kept
-        try:
-            with torch.cuda.graph(g):
-                self.step(0)
-        finally:
-            self._h1_kept = kept
+        with torch.cuda.graph(g):
+            self.step(0)
         self.graph = g
         return g
 
     def replay(self):
         """One training epoch from the captured graph; asynchronous."""
         self.graph.replay()
-        self._h1_kept = True        # where the epoch keeps H1 at all (checkpoint8)
+        self._h1_kept[False] = True     # where the epoch keeps H1 at all (checkpoint8)
 
     def scaler_state(self):
         s = self.scaler.cpu()

@@ -128,3 +128,42 @@ def test_mask(level, prec):
     sure = on.cpu().numpy() & (np.abs(gs @ w.T * 2) > err + LEAST[prec])
     learns = on.cpu().numpy() & gs.any(1, keepdims=True)      # rows beside one with a label
     assert np.mean(sure[learns]) > 0.9 and np.all(f64(dz)[sure] != 0)
+
+
+def test_recorded_passes_run_nothing():
+    """A forward pass recorded between an evaluation and its backward pass changes neither; graphs of an evaluation and
+    of a backward pass, in one or two, do what the passes do."""
+    a, b = pair("O2", G.GCN_F16, device_epoch=True)
+    for m in (a, b):
+        m.step(0)
+
+    def record(*calls):
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            for call in calls:
+                call()
+        return graph
+
+    a.forward(0, training=False)
+    fwd = record(lambda: a.forward(0))
+    b.forward(0)
+    a.loss_and_backward()
+    b.loss_and_backward()
+    same(a, b, "recorded between")
+    bwd = record(a.loss_and_backward)                        # behind the recorded training pass: reads its codes
+    both = record(lambda: a.forward(0, training=False), a.loss_and_backward)
+    for k in range(3):
+        for m in (a, b):
+            m.optimizer_step()
+        fwd.replay()
+        bwd.replay()
+        b.forward(0)
+        b.loss_and_backward()
+        same(a, b, ("two graphs", k))
+        for m in (a, b):
+            m.optimizer_step()
+        both.replay()
+        b.forward(0)
+        b.loss_and_backward()
+        same(a, b, ("one graph", k))
